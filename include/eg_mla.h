@@ -400,6 +400,184 @@ eg_mla_status eg_mla_decode_literal(const eg_mla_dims* dims, int32_t batch, cons
                                     int64_t num_slots, void* workspace, size_t workspace_bytes, void* out,
                                     void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Page tables, slots and positions of a step from the request lengths, on the
+ * GPU: what append, decode and prefill take.  With c_b = cached_lens[b]
+ * (clamped to [0, max_pages_per_seq * P]) and n_b = max(new_lens[b], 0):
+ *   need_b = ceil((c_b + n_b) / P) - ceil(c_b / P)
+ *   new page k of sequence b = free_pages[count - 1 - (sum_{a<b} need_a + k)],
+ *     the top of the free stack first, stored behind the row's
+ *     ceil(c_b / P) entries;
+ *   new token i of sequence b: position position_base[b] + c_b + i (base 0 if
+ *     position_base is NULL), slot page_table[b][t / P] * P + t % P, t = c_b + i.
+ * The step's tokens are packed by sequence: those of b are
+ * cu_seqlens[b] .. cu_seqlens[b+1] - 1 (sums of n, at most max_tokens); behind
+ * the last one positions are 0 and slots -1 up to max_tokens, so that a call
+ * captured with a fixed max_tokens appends nothing there.
+ * A sequence is taken in whole or not at all: it keeps its old length, and its
+ * tokens get slot -1 (which append skips), if c_b + n_b outgrows its row of
+ * the table (it then asks for no page), if its tokens end past max_tokens, or
+ * if it needs pages and the pages needed up to and including it exceed the
+ * free ones.  Entries of the table other than the new pages' are left as they
+ * are.  Whatever stands in the arrays, no index leaves them (a page number
+ * below 0, or one whose slots pass 2^31 - 1, gives slot -1).
+ *
+ *   cached_lens, new_lens [batch]; position_base [batch] or NULL
+ *   page_table   [batch, max_pages_per_seq], updated in place
+ *   free_pages   [free_capacity] page numbers, the first free_count[0] of them
+ *                free (clamped to [0, free_capacity]); left as it is
+ *   seq_lens     [batch]: c_b + n_b, or c_b;  cu_seqlens [batch + 1]
+ *   positions, slots [max_tokens];  free_count_out [1]: pages left
+ * All are int32.  No output may overlap an input or another output
+ * (EG_MLA_ERR_INVALID_ARG).  batch == 0 is a no-op; batch above 4096 is
+ * EG_MLA_ERR_UNSUPPORTED, and capacities, max_tokens and free_capacity above
+ * 2^30 are EG_MLA_ERR_INVALID_ARG.
+ * ------------------------------------------------------------------------- */
+eg_mla_status eg_mla_page_plan(int32_t batch, int32_t page_size, int32_t max_pages_per_seq, int32_t max_tokens,
+                               const int32_t* cached_lens, const int32_t* new_lens, const int32_t* position_base,
+                               int32_t* page_table, const int32_t* free_pages, const int32_t* free_count,
+                               int32_t free_capacity, int32_t* seq_lens, int32_t* cu_seqlens, int32_t* positions,
+                               int32_t* slots, int32_t* free_count_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Return of ended requests' pages to the free stack: for every b with
+ * ended[b] != 0, in order, the first ceil(seq_lens[b] / P) entries of its row
+ * go to free_pages[count], free_pages[count + 1], ... (those that free_capacity
+ * has no room for are dropped); free_count_out[0] is the new count,
+ * seq_lens_out[b] 0 for ended sequences and seq_lens[b] for the others.  The
+ * table is not changed.  Arrays, limits and overlaps as for eg_mla_page_plan.
+ * ------------------------------------------------------------------------- */
+eg_mla_status eg_mla_page_release(int32_t batch, int32_t page_size, int32_t max_pages_per_seq,
+                                  const int32_t* seq_lens, const int32_t* ended, const int32_t* page_table,
+                                  int32_t* free_pages, const int32_t* free_count, int32_t free_capacity,
+                                  int32_t* seq_lens_out, int32_t* free_count_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Norms of queries and keys with the position rotation, in one pass over
+ * projected rows (Sec. 3.1 Eq. (1); App. C Eq. (C.10)).  For token i:
+ *   query head h, [q^C | q^R] of d_h + d_r values:
+ *     q   = q / sqrt(mean(q^2) + 1e-6) * q_norm_w          (only if q_norm_w != NULL)
+ *     q^R = RoPE(q^R, positions[i])
+ *     q_out[i, h] = q, the query rows that decode and prefill take
+ *   key row [c | r] of d_c + d_r values:
+ *     c   = c / sqrt(mean(c^2) + 1e-6) * kv_norm_w         (only if kv_norm_w != NULL)
+ *     k^R = RoPE(r', positions[i]),  r' = r / sqrt(mean(r^2) + 1e-6) * k_norm_w
+ *           (r' = r if k_norm_w == NULL)
+ *     latent_cache[slots[i]] = [c | k^R],  token_id_cache[slots[i]] = token_ids[i]
+ * RoPE as in eg_mla_append (adjacent pairs, angle pos * theta^(-2m/d_r)); the
+ * angle is reduced in 64-bit fixed point, so that it is exact to 2^-30 turns
+ * at any position.  Arithmetic is fp32, rounded once to the storage type.
+ *
+ *   q    [n_tokens] rows of num_heads * (d_h + d_r) values, q_stride elements
+ *        apart, or NULL (no queries: q_norm_w and q_out are not used)
+ *   q_out [n_tokens, num_heads, d_h + d_r]; may be q itself where q_stride is
+ *        num_heads * (d_h + d_r)
+ *   kv   [n_tokens] rows of d_c + d_r values, kv_stride elements apart, or
+ *        NULL (no keys: the cache arguments, token_ids and slots are not used)
+ *   q_norm_w [d_h + d_r], kv_norm_w [d_c], k_norm_w [d_r]: storage type or NULL
+ *   positions, token_ids, slots [n_tokens] int32; slots outside [0, num_slots)
+ *        are skipped, duplicate ones race; positions may be NULL if d_r = 0
+ * q and kv may be views of one projection's rows.  Strides are multiples of 16
+ * bytes and at most 2^32 elements, pointers to floating-point data 16-byte
+ * aligned, and but for q_out = q no output overlaps an input
+ * (EG_MLA_ERR_INVALID_ARG).  rope_theta <= 0 selects 10000.  n_tokens == 0 is a
+ * no-op.
+ * ------------------------------------------------------------------------- */
+eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_tokens, const void* q, int64_t q_stride,
+                                  const void* q_norm_w, void* q_out, const void* kv, int64_t kv_stride,
+                                  const void* kv_norm_w, const void* k_norm_w, const int32_t* token_ids,
+                                  const int32_t* positions, const int32_t* slots, float rope_theta,
+                                  void* latent_cache, int32_t* token_id_cache, int64_t num_slots, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Decode of a batch whose sequences share a prefix, the prefix computed once
+ * for all (App. C Eq. (C.13)): sequence b attends to the prefix's tokens and
+ * then to its own,
+ *   prefix token j:  cache row prefix_table[j / P] * P + j % P,
+ *                    j < L = clamp(prefix_len[0], 0, max_prefix_pages * P);
+ *   own token j:     as for eg_mla_decode with seq_lens and page_table,
+ * which equals eg_mla_decode over sequences of L + seq_lens[b] tokens whose
+ * first L are the prefix's (up to the rounding of the partial sums).  A
+ * sequence without own tokens attends to the prefix alone, one without any
+ * token gets zeros.
+ *
+ *   prefix_len    [1] int32 on the device;  prefix_table [max_prefix_pages]
+ *   seq_lens [B], page_table [B, max_pages_per_seq] or NULL (contiguous own
+ *   rows: token j of sequence b is row b * max_pages_per_seq * P + j): OWN
+ *   tokens, the prefix not counted.  max_prefix_pages or max_pages_per_seq may
+ *   be 0 (prefix_len and prefix_table, or seq_lens, may then be NULL).
+ *   The other arguments are those of eg_mla_decode.
+ *   workspace  eg_mla_decode_shared_workspace_size(dims, B, max_pages_per_seq,
+ *              max_prefix_pages) bytes, 256-byte aligned, no initialisation
+ *              (a smaller batch or context may ask for more); calls that share
+ *              it must be ordered.
+ * Arithmetic as for eg_mla_decode (any shape and storage type).  batch above
+ * 65535 is EG_MLA_ERR_UNSUPPORTED.
+ * ------------------------------------------------------------------------- */
+size_t eg_mla_decode_shared_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_pages_per_seq,
+                                           int32_t max_prefix_pages);
+
+eg_mla_status eg_mla_decode_shared(const eg_mla_dims* dims, int32_t batch, const void* q, const void* latent_cache,
+                                   const int32_t* token_id_cache, const void* gate_table, const void* w_uk,
+                                   const void* w_uv, const int32_t* prefix_len, const int32_t* prefix_table,
+                                   int32_t max_prefix_pages, const int32_t* seq_lens, const int32_t* page_table,
+                                   int32_t max_pages_per_seq, int64_t num_slots, void* workspace,
+                                   size_t workspace_bytes, void* out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Sparse attention over cache pages, in three calls: the pages' mean keys
+ * (kept beside the cache), the scores of a step's queries, and the choice of
+ * pages, which eg_mla_decode then attends to.
+ *
+ * eg_mla_page_means: for every page of sequence b that holds one of the tokens
+ * first_tokens[b] .. seq_lens[b] - 1 (all pages if first_tokens is NULL),
+ *   page_means[p] = (1/n) sum_i [c_i (.) G[id_i] | k^R_i]
+ * over the n tokens of the sequence that lie on it; p is the page's number in
+ * the cache (page_table[b][j], or b * max_pages_per_seq + j without a table).
+ * Sums are in 64 bits, rounded once to the storage type.  Other rows are left
+ * as they are; page numbers outside the cache are skipped.  A page that two
+ * sequences of a call name is written by both.
+ *   page_means [num_slots / P, d_c + d_r]
+ *
+ * eg_mla_page_scores: for column j < ceil(seq_lens[b] / P) of sequence b
+ *   scores[b, j] = max_h tau (q_lat[b,h] . mean_c + q^R[b,h] . mean_r)
+ * with mean = page_means[p] of its page (clamped into the cache) and
+ * q_lat[h] = W_UK[h]^T q^C[h]; -inf behind.  fp32 (bf16 storage: the absorbed
+ * query enters the matrix products as three bf16 parts, which hold all of it).
+ *   q [B, H, d_h + d_r];  scores [B, max_pages_per_seq] fp32
+ *   workspace  eg_mla_page_scores_workspace_size(dims, B) bytes, 256-byte aligned
+ *
+ * eg_mla_select_pages: of the n = ceil(seq_lens[b] / P) pages of sequence b
+ * the first keep_first, the last keep_last (at least 1: the last page may be
+ * partly filled) and, up to `keep` in all, those of the highest score (equal
+ * scores: the first ones; a NaN counts as -inf), in the sequence's order:
+ *   sel_pages[b, :]  their page numbers, -1 behind the last
+ *   sel_lens[b]      their tokens
+ *   sel_index[b, :]  their columns in the sequence, -1 behind (or NULL)
+ * so that eg_mla_decode over sel_lens and sel_pages with max_pages_per_seq =
+ * keep attends to them.  n <= keep: every page.  Scores are read for the
+ * other pages only.  keep >= keep_first + keep_last.
+ *
+ * Lengths are clamped to the capacity, 0 gives no pages.  Of a page table only
+ * the entries of a sequence's pages are read.
+ * ------------------------------------------------------------------------- */
+eg_mla_status eg_mla_page_means(const eg_mla_dims* dims, int32_t batch, const void* latent_cache,
+                                const int32_t* token_id_cache, const void* gate_table, const int32_t* first_tokens,
+                                const int32_t* seq_lens, const int32_t* page_table, int32_t max_pages_per_seq,
+                                int64_t num_slots, void* page_means, void* stream);
+
+size_t eg_mla_page_scores_workspace_size(const eg_mla_dims* dims, int32_t batch);
+
+eg_mla_status eg_mla_page_scores(const eg_mla_dims* dims, int32_t batch, const void* q, const void* w_uk,
+                                 const void* page_means, const int32_t* seq_lens, const int32_t* page_table,
+                                 int32_t max_pages_per_seq, int64_t num_slots, void* workspace,
+                                 size_t workspace_bytes, float* scores, void* stream);
+
+eg_mla_status eg_mla_select_pages(const eg_mla_dims* dims, int32_t batch, const float* scores,
+                                  const int32_t* seq_lens, const int32_t* page_table, int32_t max_pages_per_seq,
+                                  int32_t keep, int32_t keep_first, int32_t keep_last, int32_t* sel_pages,
+                                  int32_t* sel_lens, int32_t* sel_index, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,9 @@ EXPORTS = ["eg_mla_status_string", "eg_mla_check_dims", "eg_mla_append", "eg_mla
            "eg_mla_prefill_ref", "eg_mla_prefill_varlen_workspace_size", "eg_mla_prefill_varlen",
            "eg_mla_decode_literal_workspace_size", "eg_mla_decode_literal", "eg_mla_decode_noalloc",
            "eg_mla_append_workspace_size", "eg_mla_append_ws", "eg_mla_gate_table_marks_size",
-           "eg_mla_gate_table"]
+           "eg_mla_gate_table", "eg_mla_page_plan", "eg_mla_page_release", "eg_mla_qk_norm_rope",
+           "eg_mla_decode_shared_workspace_size", "eg_mla_decode_shared", "eg_mla_page_means",
+           "eg_mla_page_scores_workspace_size", "eg_mla_page_scores", "eg_mla_select_pages"]
 NOALLOC_SCRATCH_BYTES = 32 << 20  # EG_MLA_NOALLOC_SCRATCH_BYTES
 LITERAL_NO_LN, LITERAL_ADD = 1, 2
 
@@ -102,6 +104,25 @@ def lib() -> ctypes.CDLL:
     L.eg_mla_decode_literal.restype = ctypes.c_int
     L.eg_mla_decode_literal.argtypes = [pd, i32, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_uint32, vp, vp, i32, i64,
                                         vp, sz, vp, vp]
+    L.eg_mla_page_plan.restype = ctypes.c_int
+    L.eg_mla_page_plan.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    L.eg_mla_page_release.restype = ctypes.c_int
+    L.eg_mla_page_release.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    L.eg_mla_qk_norm_rope.restype = ctypes.c_int
+    L.eg_mla_qk_norm_rope.argtypes = [pd, i32, vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, i64,
+                                      vp]
+    L.eg_mla_decode_shared_workspace_size.restype = sz
+    L.eg_mla_decode_shared_workspace_size.argtypes = [pd, i32, i32, i32]
+    L.eg_mla_decode_shared.restype = ctypes.c_int
+    L.eg_mla_decode_shared.argtypes = [pd, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, i64, vp, sz, vp, vp]
+    L.eg_mla_page_means.restype = ctypes.c_int
+    L.eg_mla_page_means.argtypes = [pd, i32, vp, vp, vp, vp, vp, vp, i32, i64, vp, vp]
+    L.eg_mla_page_scores_workspace_size.restype = sz
+    L.eg_mla_page_scores_workspace_size.argtypes = [pd, i32]
+    L.eg_mla_page_scores.restype = ctypes.c_int
+    L.eg_mla_page_scores.argtypes = [pd, i32, vp, vp, vp, vp, vp, i32, i64, vp, sz, vp, vp]
+    L.eg_mla_select_pages.restype = ctypes.c_int
+    L.eg_mla_select_pages.argtypes = [pd, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -256,6 +277,182 @@ def prefill_ref(dims: Dims, q, latent, token_ids, gate_table, w_uk, w_uv, worksp
                                     _ptr(gate_table), _ptr(w_uk), _ptr(w_uv), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _ptr(out), _stream(stream)),
            "eg_mla_prefill_ref")
+
+
+# ---------------------------------------------------------------------------
+# around the decode of a paged server: page tables, query and key rows, a
+# shared prefix, sparse attention over pages
+# ---------------------------------------------------------------------------
+def _expect(name: str, *specs) -> None:
+    """Refuses tensors that the C entry would misread.  A spec is (key, tensor or None, type or None, shape or None);
+    every tensor has that type and shape, is contiguous and lies on the current GPU."""
+    import torch
+    here = None
+    for key, t, dtype, shape in specs:
+        if t is None:
+            continue
+        dev = t.get_device()
+        if here is None:
+            here = torch.cuda.current_device() if dev >= 0 else 0
+        if (dtype is None or t.dtype is dtype) and dev == here and t.is_contiguous() and (shape is None or t.shape == shape):
+            continue
+        raise ValueError(f"{name}: {key} is {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}; expected "
+                         f"contiguous{'' if dtype is None else f' {dtype}'}{'' if shape is None else f' {tuple(shape)}'} "
+                         "on the current GPU")
+
+
+def _storage(dims: Dims):
+    import torch
+    return torch.bfloat16 if dims.dtype == BF16 else torch.float32
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def page_plan(page_size: int, cached_lens, new_lens, page_table, free_pages, free_count, seq_lens, cu_seqlens, positions,
+              slots, free_count_out, position_base=None, stream=None) -> None:
+    """eg_mla_page_plan over int32 device tensors: page_table [B, max_pages] is updated, seq_lens, cu_seqlens,
+    positions, slots and free_count_out are written."""
+    from torch import int32 as i
+    b, width, n, free = cached_lens.shape[0], page_table.shape[1], slots.shape[0], free_pages.shape[0]
+    name = "eg_mla_page_plan"
+    _expect(name, ("cached_lens", cached_lens, i, (b,)), ("new_lens", new_lens, i, (b,)),
+            ("page_table", page_table, i, (b, width)), ("free_pages", free_pages, i, (free,)),
+            ("free_count", free_count, i, (1,)), ("seq_lens", seq_lens, i, (b,)), ("cu_seqlens", cu_seqlens, i, (b + 1,)),
+            ("positions", positions, i, (n,)), ("slots", slots, i, (n,)), ("free_count_out", free_count_out, i, (1,)),
+            ("position_base", position_base, i, (b,)))
+    _check(lib().eg_mla_page_plan(b, page_size, width, n, _ptr(cached_lens), _ptr(new_lens), _ptr(position_base),
+                                  _ptr(page_table), _ptr(free_pages), _ptr(free_count), free, _ptr(seq_lens),
+                                  _ptr(cu_seqlens), _ptr(positions), _ptr(slots), _ptr(free_count_out),
+                                  _stream(stream)), name)
+
+
+def page_release(page_size: int, seq_lens, ended, page_table, free_pages, free_count, seq_lens_out, free_count_out,
+                 stream=None) -> None:
+    """eg_mla_page_release over int32 device tensors: free_pages is updated, seq_lens_out and free_count_out written."""
+    from torch import int32 as i
+    b, width, free = seq_lens.shape[0], page_table.shape[1], free_pages.shape[0]
+    name = "eg_mla_page_release"
+    _expect(name, ("seq_lens", seq_lens, i, (b,)), ("ended", ended, i, (b,)), ("page_table", page_table, i, (b, width)),
+            ("free_pages", free_pages, i, (free,)), ("free_count", free_count, i, (1,)),
+            ("seq_lens_out", seq_lens_out, i, (b,)), ("free_count_out", free_count_out, i, (1,)))
+    _check(lib().eg_mla_page_release(b, page_size, width, _ptr(seq_lens), _ptr(ended), _ptr(page_table),
+                                     _ptr(free_pages), _ptr(free_count), free, _ptr(seq_lens_out),
+                                     _ptr(free_count_out), _stream(stream)), name)
+
+
+def _row_stride(name: str, key: str, t, n: int, row: int) -> int:
+    """Elements between the rows of a [n, row] or [n, heads, d] tensor or view whose rows are contiguous."""
+    if t.shape[0] != n or t.numel() != n * row or (n and not t[0].is_contiguous()):
+        raise ValueError(f"{name}: {key} is {tuple(t.shape)} with strides {t.stride()}, not {n} contiguous rows of {row}")
+    return t.stride(0) if n > 1 else row
+
+
+def qk_norm_rope(dims: Dims, q, q_out, kv, latent_cache, token_id_cache, token_ids, positions, slots, q_norm_w=None,
+                 kv_norm_w=None, k_norm_w=None, rope_theta: float = 10000.0, stream=None) -> None:
+    """eg_mla_qk_norm_rope over device tensors: q [n, H, d_h + d_r] or [n, H (d_h + d_r)] and kv [n, d_c + d_r], or
+    views with a stride between their rows; q (with q_out) or kv (with the cache arguments) may be None."""
+    from torch import int32 as i
+    name, dt = "eg_mla_qk_norm_rope", _storage(dims)
+    if q is None and kv is None:
+        raise ValueError(f"{name}: neither q nor kv")
+    n = (kv if q is None else q).shape[0]
+    dq, row = dims.head_dim + dims.rope_dim, dims.latent_dim + dims.rope_dim
+    specs = [("positions", positions, i, (n,))]
+    qs = ks = num_slots = 0
+    if q is not None:
+        qs = _row_stride(name, "q", q, n, dims.num_heads * dq)
+        if q_out is None or q_out.numel() != q.numel():
+            raise ValueError(f"{name}: q_out does not hold {n} rows of {dims.num_heads} heads of {dq} values")
+        specs += [("q", q[:0], dt, None), ("q_out", q_out, dt, None), ("q_norm_w", q_norm_w, dt, (dq,))]
+    if kv is not None:
+        ks = _row_stride(name, "kv", kv, n, row)
+        num_slots = latent_cache.shape[0]
+        specs += [("kv", kv[:0], dt, None), ("latent_cache", latent_cache, dt, (num_slots, row)),
+                  ("token_id_cache", token_id_cache, i, (num_slots,)), ("token_ids", token_ids, i, (n,)),
+                  ("slots", slots, i, (n,)), ("kv_norm_w", kv_norm_w, dt, (dims.latent_dim,)),
+                  ("k_norm_w", k_norm_w, dt, (dims.rope_dim,))]
+    _expect(name, *specs)
+    _check(lib().eg_mla_qk_norm_rope(ctypes.byref(dims), n, _ptr(q), qs, _ptr(q_norm_w), _ptr(q_out), _ptr(kv), ks,
+                                     _ptr(kv_norm_w), _ptr(k_norm_w), _ptr(token_ids), _ptr(positions), _ptr(slots),
+                                     rope_theta, _ptr(latent_cache), _ptr(token_id_cache), num_slots, _stream(stream)),
+           name)
+
+
+def decode_shared_workspace_size(dims: Dims, batch: int, max_pages_per_seq: int, max_prefix_pages: int) -> int:
+    return lib().eg_mla_decode_shared_workspace_size(ctypes.byref(dims), batch, max_pages_per_seq, max_prefix_pages)
+
+
+def decode_shared(dims: Dims, q, latent_cache, token_id_cache, gate_table, w_uk, w_uv, prefix_len, prefix_table,
+                  seq_lens, page_table, max_pages_per_seq: int, workspace, out, stream=None) -> None:
+    """eg_mla_decode_shared over device tensors: prefix_len [1] and prefix_table [pages] (or None: no prefix) name the
+    shared tokens, seq_lens and page_table each sequence's own."""
+    from torch import int32 as i
+    name, dt = "eg_mla_decode_shared", _storage(dims)
+    b, slots, h = q.shape[0], latent_cache.shape[0], dims.num_heads
+    dh, dv, dc, dr = dims.head_dim, dims.v_head_dim, dims.latent_dim, dims.rope_dim
+    pages = 0 if prefix_table is None else prefix_table.shape[0]
+    _expect(name, ("q", q, dt, (b, h, dh + dr)), ("latent_cache", latent_cache, dt, (slots, dc + dr)),
+            ("token_id_cache", token_id_cache, i, (slots,)), ("gate_table", gate_table, dt, (dims.vocab_size, dc)),
+            ("w_uk", w_uk, dt, (h, dh, dc)), ("w_uv", w_uv, dt, (h, dv, dc)), ("prefix_len", prefix_len, i, (1,)),
+            ("prefix_table", prefix_table, i, (pages,)), ("seq_lens", seq_lens, i, (b,)),
+            ("page_table", page_table, i, (b, max_pages_per_seq)), ("out", out, dt, (b, h, dv)),
+            ("workspace", workspace, None, None))
+    _check(lib().eg_mla_decode_shared(ctypes.byref(dims), b, _ptr(q), _ptr(latent_cache), _ptr(token_id_cache),
+                                      _ptr(gate_table), _ptr(w_uk), _ptr(w_uv), _ptr(prefix_len), _ptr(prefix_table),
+                                      pages, _ptr(seq_lens), _ptr(page_table), max_pages_per_seq, slots,
+                                      _ptr(workspace), _bytes(workspace), _ptr(out), _stream(stream)), name)
+
+
+def page_means(dims: Dims, latent_cache, token_id_cache, gate_table, first_tokens, seq_lens, page_table,
+               max_pages_per_seq: int, means, stream=None) -> None:
+    """eg_mla_page_means over device tensors: means [num_slots / P, d_c + d_r] is updated."""
+    from torch import int32 as i
+    name, dt = "eg_mla_page_means", _storage(dims)
+    b, slots, row = seq_lens.shape[0], latent_cache.shape[0], dims.latent_dim + dims.rope_dim
+    _expect(name, ("latent_cache", latent_cache, dt, (slots, row)), ("token_id_cache", token_id_cache, i, (slots,)),
+            ("gate_table", gate_table, dt, (dims.vocab_size, dims.latent_dim)),
+            ("first_tokens", first_tokens, i, (b,)), ("seq_lens", seq_lens, i, (b,)),
+            ("page_table", page_table, i, (b, max_pages_per_seq)), ("means", means, dt, (slots // dims.page_size, row)))
+    _check(lib().eg_mla_page_means(ctypes.byref(dims), b, _ptr(latent_cache), _ptr(token_id_cache), _ptr(gate_table),
+                                   _ptr(first_tokens), _ptr(seq_lens), _ptr(page_table), max_pages_per_seq, slots,
+                                   _ptr(means), _stream(stream)), name)
+
+
+def page_scores_workspace_size(dims: Dims, batch: int) -> int:
+    return lib().eg_mla_page_scores_workspace_size(ctypes.byref(dims), batch)
+
+
+def page_scores(dims: Dims, q, w_uk, means, seq_lens, page_table, max_pages_per_seq: int, workspace, scores,
+                stream=None) -> None:
+    """eg_mla_page_scores over device tensors: scores [B, max_pages_per_seq] fp32 is written."""
+    from torch import float32, int32 as i
+    name, dt = "eg_mla_page_scores", _storage(dims)
+    b, pages, dr = q.shape[0], means.shape[0], dims.rope_dim
+    _expect(name, ("q", q, dt, (b, dims.num_heads, dims.head_dim + dr)),
+            ("w_uk", w_uk, dt, (dims.num_heads, dims.head_dim, dims.latent_dim)),
+            ("means", means, dt, (pages, dims.latent_dim + dr)), ("seq_lens", seq_lens, i, (b,)),
+            ("page_table", page_table, i, (b, max_pages_per_seq)), ("scores", scores, float32, (b, max_pages_per_seq)),
+            ("workspace", workspace, None, None))
+    _check(lib().eg_mla_page_scores(ctypes.byref(dims), b, _ptr(q), _ptr(w_uk), _ptr(means), _ptr(seq_lens),
+                                    _ptr(page_table), max_pages_per_seq, pages * dims.page_size, _ptr(workspace),
+                                    _bytes(workspace), _ptr(scores), _stream(stream)), name)
+
+
+def select_pages(dims: Dims, scores, seq_lens, page_table, max_pages_per_seq: int, sel_pages, sel_lens,
+                 keep_first: int = 0, keep_last: int = 1, sel_index=None, stream=None) -> None:
+    """eg_mla_select_pages over device tensors: sel_pages [B, keep], sel_lens [B] and sel_index [B, keep] (or None) are
+    written; decode(..., sel_lens, sel_pages, keep, ...) attends to the chosen pages."""
+    from torch import float32, int32 as i
+    name = "eg_mla_select_pages"
+    b, keep = sel_pages.shape
+    _expect(name, ("scores", scores, float32, (b, max_pages_per_seq)), ("seq_lens", seq_lens, i, (b,)),
+            ("page_table", page_table, i, (b, max_pages_per_seq)), ("sel_pages", sel_pages, i, (b, keep)),
+            ("sel_lens", sel_lens, i, (b,)), ("sel_index", sel_index, i, (b, keep)))
+    _check(lib().eg_mla_select_pages(ctypes.byref(dims), b, _ptr(scores), _ptr(seq_lens), _ptr(page_table),
+                                     max_pages_per_seq, keep, keep_first, keep_last, _ptr(sel_pages), _ptr(sel_lens),
+                                     _ptr(sel_index), _stream(stream)), name)
 
 
 # ---------------------------------------------------------------------------

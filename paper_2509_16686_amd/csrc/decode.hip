@@ -22,6 +22,7 @@
 #include <cmath>
 #include <mutex>
 
+#include "absorb.h"
 #include "device_common.h"
 #include "eg_mla.h"
 #include "host_plan.h"
@@ -523,7 +524,7 @@ hipError_t launch_split(const eg_mla_dims& d, const DecodePlan& p, const SplitAr
       if (static_cast<int64_t>(nblocks) * p.slices > 0x7fffffff) return hipErrorInvalidValue;
       return launch_slice<128, 64>(a, p.slices, p.pieces, nblocks, stream, ev0, ev1);
     }
-    if (heads_kernel_shape(d)) return launch_wide(a, wide_groups(a.groups), stream, ev0, ev1);
+    if (p.balanced) return launch_wide(a, wide_groups(a.groups), stream, ev0, ev1);
     if (rows_kernel_shape(d)) {
       hipExtLaunchKernelGGL((split_rows_kernel<320, 64, 4>), dim3(nblocks), dim3(256), 0, stream, ev0, ev1, 0, a);
       return hipGetLastError();
@@ -562,6 +563,72 @@ hipError_t launch_split(const eg_mla_dims& d, const DecodePlan& p, const SplitAr
 namespace egmla {
 namespace {
 
+// Grid of the MFMA absorption.  A W_UK of a few MB is read once per block of
+// sequences: group blocks so it is read about once; a small one is cheap to
+// re-read, and one block per work-group spreads the work over more compute
+// units.  A small grid takes narrower column slices: more work-groups, each
+// with less of W_UK to load (measured faster for B32 H16, slower for B256).
+struct AbsorbGrid {
+  bool grouped, narrow;
+  dim3 grid;
+};
+AbsorbGrid absorb_grid(const eg_mla_dims& d, int32_t batch, bool wide_rows) {
+  const size_t wuk_bytes = static_cast<size_t>(d.num_heads) * d.head_dim * d.latent_dim * 2;
+  const bool grouped = wide_rows || (d.head_dim == 128 && wuk_bytes >= (size_t{4} << 20));
+  const int rows = kAbsRows * (grouped ? kAbsBlocks : 1);
+  const int row_blocks = (batch + rows - 1) / rows;
+  const bool narrow = !grouped && d.num_heads * row_blocks < kAbsMinWorkGroups;
+  const int cols = narrow ? kAbsColsNarrow : kAbsCols;
+  return {grouped, narrow, dim3(d.num_heads, row_blocks, (d.latent_dim + cols - 1) / cols)};
+}
+
+// Absorption with a balanced schedule (bf16, d_h 128): one more column of
+// work-groups, the first of which writes the schedule.  The wide kernel takes
+// the query as fp16 rows (q^R in bf16), the d_c 128 kernel as fp32 rows.
+hipError_t launch_absorb_sched(const eg_mla_dims& d, const DecodePlan& p, int32_t batch, const void* q,
+                               const void* w_uk, float* qfull, const SchedArgs& sched, hipStream_t stream) {
+  const uint16_t* q16 = static_cast<const uint16_t*>(q);
+  const uint16_t* wuk16 = static_cast<const uint16_t*>(w_uk);
+  const AbsorbGrid ag = absorb_grid(d, batch, p.balanced);
+  const dim3 grid(ag.grid.x + 1, ag.grid.y, ag.grid.z);
+  auto kern = p.balanced  ? absorb_mfma_kernel<128, kAbsBlocks, kAbsCols, true>
+              : ag.grouped ? absorb_mfma_kernel<128, kAbsBlocks, kAbsCols, false, true>
+              : ag.narrow  ? absorb_mfma_kernel<128, 1, kAbsColsNarrow, false, true>
+                           : absorb_mfma_kernel<128, 1, kAbsCols, false, true>;
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, q16, wuk16, qfull, batch, d.num_heads, d.latent_dim, d.rope_dim,
+                     sched);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* qfull,
+                         hipStream_t stream) {
+  const bool bf = d.dtype == EG_MLA_BF16;
+  if (bf && (d.head_dim == 128 || d.head_dim == 64)) {
+    const AbsorbGrid ag = absorb_grid(d, batch, false);
+    auto kern = d.head_dim == 64 ? (ag.narrow ? absorb_mfma_kernel<64, 1, kAbsColsNarrow>
+                                              : absorb_mfma_kernel<64, 1, kAbsCols>)
+                : ag.grouped ? absorb_mfma_kernel<128, kAbsBlocks, kAbsCols>
+                : ag.narrow  ? absorb_mfma_kernel<128, 1, kAbsColsNarrow>
+                             : absorb_mfma_kernel<128, 1, kAbsCols>;
+    hipLaunchKernelGGL(kern, ag.grid, dim3(256), 0, stream, static_cast<const uint16_t*>(q),
+                       static_cast<const uint16_t*>(w_uk), qfull, batch, d.num_heads, d.latent_dim, d.rope_dim,
+                       SchedArgs{});
+    return hipGetLastError();
+  }
+  const dim3 grid(d.num_heads, (d.latent_dim + kAbsorbCols - 1) / kAbsorbCols, (batch + kAbsorbRows - 1) / kAbsorbRows);
+  const size_t lds = sizeof(float) * (kAbsorbRows * d.head_dim + 4 * kAbsorbRows * kAbsorbCols);
+  auto kern = bf ? absorb_kernel<true> : absorb_kernel<false>;
+  hipError_t e = set_lds(kern, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, grid, dim3(256), lds, stream, q, w_uk, qfull, batch, d.num_heads, d.head_dim, d.latent_dim,
+                     d.rope_dim);
+  return hipGetLastError();
+}
+
+namespace {
+
 // Enqueues one decode call whose arguments validate_decode has accepted, with
 // its workspace at `workspace` laid out by the plan p.
 eg_mla_status run_decode(const eg_mla_dims& d, const DecodePlan& p, int32_t batch, const void* q,
@@ -595,64 +662,11 @@ eg_mla_status run_decode(const eg_mla_dims& d, const DecodePlan& p, int32_t batc
                       p.fused_absorb ? batch * p.head_groups * p.s_max : 0};
   // 1. absorption (or inside the split kernel)
   if (!p.fused_absorb && !p.one_launch) {
-    dim3 grid(d.num_heads, (d.latent_dim + kAbsorbCols - 1) / kAbsorbCols, (batch + kAbsorbRows - 1) / kAbsorbRows);
-    const size_t lds = sizeof(float) * (kAbsorbRows * d.head_dim + 4 * kAbsorbRows * kAbsorbCols);
-    if (bf && (d.head_dim == 128 || d.head_dim == 64)) {
-      // A W_UK of a few MB is read once per block of sequences: group blocks so
-      // it is read about once; a small one is cheap to re-read, and one block
-      // per work-group spreads the work over more compute units.
-      const size_t wuk_bytes = static_cast<size_t>(d.num_heads) * d.head_dim * d.latent_dim * 2;
-      const bool grouped = p.balanced || (d.head_dim == 128 && wuk_bytes >= (size_t{4} << 20));
-      const int rows = kAbsRows * (grouped ? kAbsBlocks : 1);
-      const int row_blocks = (batch + rows - 1) / rows;
-      // a small grid takes narrower column slices: more work-groups, each
-      // with less of W_UK to load (measured faster for B32 H16, slower for B256)
-      const bool narrow = !grouped && d.num_heads * row_blocks < kAbsMinWorkGroups;
-      const int cols = narrow ? kAbsColsNarrow : kAbsCols;
-      dim3 ga(d.num_heads, row_blocks, (d.latent_dim + cols - 1) / cols);
-      const uint16_t* q16 = static_cast<const uint16_t*>(q);
-      const uint16_t* wuk16 = static_cast<const uint16_t*>(w_uk);
-      if (p.balanced)  // the wide kernel takes the query as fp16 rows (q^R in bf16); one more column: its schedule
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, kAbsBlocks, kAbsCols, true>), dim3(ga.x + 1, ga.y, ga.z),
-                           dim3(256), 0, stream, q16, wuk16, qfull, batch, d.num_heads, d.latent_dim, d.rope_dim,
-                           sched);
-      else if (p.tok_balanced && grouped)
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, kAbsBlocks, kAbsCols, false, true>), dim3(ga.x + 1, ga.y, ga.z),
-                           dim3(256), 0, stream, q16, wuk16, qfull, batch, d.num_heads, d.latent_dim, d.rope_dim,
-                           sched);
-      else if (p.tok_balanced && narrow)
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, 1, kAbsColsNarrow, false, true>), dim3(ga.x + 1, ga.y, ga.z),
-                           dim3(256), 0, stream, q16, wuk16, qfull, batch, d.num_heads, d.latent_dim, d.rope_dim,
-                           sched);
-      else if (p.tok_balanced)
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, 1, kAbsCols, false, true>), dim3(ga.x + 1, ga.y, ga.z), dim3(256),
-                           0, stream, q16, wuk16, qfull, batch, d.num_heads, d.latent_dim, d.rope_dim, sched);
-      else if (d.head_dim == 64) {
-        if (narrow)
-          hipLaunchKernelGGL((absorb_mfma_kernel<64, 1, kAbsColsNarrow>), ga, dim3(256), 0, stream, q16, wuk16, qfull,
-                             batch, d.num_heads, d.latent_dim, d.rope_dim, sched);
-        else
-          hipLaunchKernelGGL((absorb_mfma_kernel<64, 1, kAbsCols>), ga, dim3(256), 0, stream, q16, wuk16, qfull,
-                             batch, d.num_heads, d.latent_dim, d.rope_dim, sched);
-      } else if (grouped)
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, kAbsBlocks, kAbsCols>), ga, dim3(256), 0, stream, q16, wuk16,
-                           qfull, batch, d.num_heads, d.latent_dim, d.rope_dim, sched);
-      else if (narrow)
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, 1, kAbsColsNarrow>), ga, dim3(256), 0, stream, q16, wuk16, qfull,
-                           batch, d.num_heads, d.latent_dim, d.rope_dim, sched);
-      else
-        hipLaunchKernelGGL((absorb_mfma_kernel<128, 1, kAbsCols>), ga, dim3(256), 0, stream, q16, wuk16, qfull, batch,
-                           d.num_heads, d.latent_dim, d.rope_dim, sched);
-    } else if (bf) {
-      if (set_lds(absorb_kernel<true>, lds) != hipSuccess) return EG_MLA_ERR_HIP;
-      hipLaunchKernelGGL(absorb_kernel<true>, grid, dim3(256), lds, stream, q, w_uk, qfull, batch, d.num_heads,
-                         d.head_dim, d.latent_dim, d.rope_dim);
-    } else {
-      if (set_lds(absorb_kernel<false>, lds) != hipSuccess) return EG_MLA_ERR_HIP;
-      hipLaunchKernelGGL(absorb_kernel<false>, grid, dim3(256), lds, stream, q, w_uk, qfull, batch, d.num_heads,
-                         d.head_dim, d.latent_dim, d.rope_dim);
+    if (p.balanced || p.tok_balanced) {
+      if (launch_absorb_sched(d, p, batch, q, w_uk, qfull, sched, stream) != hipSuccess) return EG_MLA_ERR_HIP;
+    } else if (launch_absorb(d, batch, q, w_uk, qfull, stream) != hipSuccess) {
+      return EG_MLA_ERR_HIP;
     }
-    if (hipGetLastError() != hipSuccess) return EG_MLA_ERR_HIP;
   }
   // 2. split kernel (skipped when the cache has no capacity: every length clamps to 0)
   if (p.capacity > 0) {
@@ -825,3 +839,5 @@ extern "C" eg_mla_status eg_mla_decode(const eg_mla_dims* dims, int32_t batch, c
                                page_table, max_pages_per_seq, num_slots, workspace, workspace_bytes, out, stream,
                                nullptr);
 }
+
+#include "decode_shared.h"

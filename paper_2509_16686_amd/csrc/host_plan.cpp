@@ -2,6 +2,7 @@
 #include "host_plan.h"
 
 #include <algorithm>
+#include <initializer_list>
 
 namespace egmla {
 
@@ -477,6 +478,263 @@ eg_mla_status validate_literal(const eg_mla_dims* d, int32_t batch, const void* 
     return EG_MLA_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < literal_workspace_bytes(*d, batch, max_pages_per_seq))
     return EG_MLA_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
+  return EG_MLA_OK;
+}
+
+namespace {
+
+// Arrays of a call that must not overlap (a null one takes no room).
+struct Span {
+  const void* p;
+  int64_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+  if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+}
+// Whether any of the outputs overlaps another output or an input.
+bool outputs_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span* q = o + 1; q != outs.end(); ++q)
+      if (overlap(*o, *q)) return true;
+    for (const Span& i : ins)
+      if (overlap(*o, i)) return true;
+  }
+  return false;
+}
+
+constexpr int64_t kMaxCapacity = int64_t{1} << 30;  // tokens of a sequence's row of the page table, array lengths
+
+// The cache and page table of a call over `batch` sequences of max_pages pages.
+eg_mla_status check_pages(const eg_mla_dims& d, int32_t batch, int32_t max_pages, int64_t num_slots, bool paged) {
+  if (batch < 0 || max_pages < 0 || num_slots < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (num_slots >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
+  const int64_t cap = static_cast<int64_t>(max_pages) * d.page_size;
+  if (cap > kMaxCapacity) return EG_MLA_ERR_INVALID_ARG;
+  if (batch == 0 || max_pages == 0) return EG_MLA_OK;
+  if (!paged && cap > num_slots / batch) return EG_MLA_ERR_INVALID_ARG;  // contiguous rows must fit in the cache
+  return num_slots < d.page_size ? EG_MLA_ERR_INVALID_ARG : EG_MLA_OK;
+}
+
+}  // namespace
+
+eg_mla_status validate_page_plan(int32_t batch, int32_t page_size, int32_t max_pages_per_seq, int32_t max_tokens,
+                                 const int32_t* cached_lens, const int32_t* new_lens, const int32_t* position_base,
+                                 const int32_t* page_table, const int32_t* free_pages, const int32_t* free_count,
+                                 int32_t free_capacity, const int32_t* seq_lens, const int32_t* cu_seqlens,
+                                 const int32_t* positions, const int32_t* slots, const int32_t* free_count_out) {
+  if (batch < 0 || page_size < 1 || max_pages_per_seq < 0 || max_tokens < 0 || free_capacity < 0)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(max_pages_per_seq) * page_size > kMaxCapacity || max_tokens > kMaxCapacity ||
+      free_capacity > kMaxCapacity)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (batch > kPageMaxBatch) return EG_MLA_ERR_UNSUPPORTED;
+  if (batch == 0) return EG_MLA_OK;
+  if (!cached_lens || !new_lens || !free_count || !seq_lens || !cu_seqlens || !free_count_out)
+    return EG_MLA_ERR_INVALID_ARG;
+  if ((max_pages_per_seq > 0 && !page_table) || (free_capacity > 0 && !free_pages) ||
+      (max_tokens > 0 && (!positions || !slots)))
+    return EG_MLA_ERR_INVALID_ARG;
+  // every work-group reads the inputs for itself while others write
+  const int64_t n = 4 * static_cast<int64_t>(batch), t = 4 * static_cast<int64_t>(max_tokens);
+  if (outputs_overlap({{seq_lens, n}, {cu_seqlens, n + 4}, {positions, t}, {slots, t}, {free_count_out, 4},
+                       {page_table, n * max_pages_per_seq}},
+                      {{cached_lens, n}, {new_lens, n}, {position_base, n}, {free_count, 4},
+                       {free_pages, 4 * static_cast<int64_t>(free_capacity)}}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_page_release(int32_t batch, int32_t page_size, int32_t max_pages_per_seq,
+                                    const int32_t* seq_lens, const int32_t* ended, const int32_t* page_table,
+                                    const int32_t* free_pages, const int32_t* free_count, int32_t free_capacity,
+                                    const int32_t* seq_lens_out, const int32_t* free_count_out) {
+  if (batch < 0 || page_size < 1 || max_pages_per_seq < 0 || free_capacity < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(max_pages_per_seq) * page_size > kMaxCapacity || free_capacity > kMaxCapacity)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (batch > kPageMaxBatch) return EG_MLA_ERR_UNSUPPORTED;
+  if (batch == 0) return EG_MLA_OK;
+  if (!seq_lens || !ended || !free_count || !seq_lens_out || !free_count_out) return EG_MLA_ERR_INVALID_ARG;
+  if ((max_pages_per_seq > 0 && !page_table) || (free_capacity > 0 && !free_pages)) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t n = 4 * static_cast<int64_t>(batch);
+  if (outputs_overlap({{seq_lens_out, n}, {free_count_out, 4}, {free_pages, 4 * static_cast<int64_t>(free_capacity)}},
+                      {{seq_lens, n}, {ended, n}, {free_count, 4}, {page_table, n * max_pages_per_seq}}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_qk(const eg_mla_dims* d, int32_t n_tokens, const void* q, int64_t q_stride,
+                          const void* q_norm_w, const void* q_out, const void* kv, int64_t kv_stride,
+                          const void* kv_norm_w, const void* k_norm_w, const int32_t* token_ids,
+                          const int32_t* positions, const int32_t* slots, float rope_theta, const void* latent_cache,
+                          const int32_t* token_id_cache, int64_t num_slots) {
+  const eg_mla_status st = check_dims(d);
+  if (st != EG_MLA_OK) return st;
+  if (n_tokens < 0 || num_slots < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (rope_theta > 3.4e38f) return EG_MLA_ERR_INVALID_ARG;  // infinite
+  if (n_tokens == 0) return EG_MLA_OK;
+  if (!q && !kv) return EG_MLA_ERR_INVALID_ARG;
+  if (d->rope_dim > 0 && !positions) return EG_MLA_ERR_INVALID_ARG;
+  const int eb = elem_bytes(*d), vec = 16 / eb;
+  const int64_t row = d->latent_dim + d->rope_dim, n = n_tokens;
+  const int64_t q_row = static_cast<int64_t>(d->num_heads) * (d->head_dim + d->rope_dim);
+  constexpr int64_t kMaxStride = int64_t{1} << 32;
+  if (q) {
+    if (!q_out || q_stride < q_row || q_stride % vec != 0 || q_stride > kMaxStride) return EG_MLA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(q_out) || !aligned16(q_norm_w)) return EG_MLA_ERR_INVALID_ARG;
+  }
+  if (kv) {
+    if (!latent_cache || !token_id_cache || !token_ids || !slots) return EG_MLA_ERR_INVALID_ARG;
+    if (kv_stride < row || kv_stride % vec != 0 || kv_stride > kMaxStride) return EG_MLA_ERR_INVALID_ARG;
+    if (!aligned16(kv) || !aligned16(kv_norm_w) || !aligned16(k_norm_w) || !aligned16(latent_cache))
+      return EG_MLA_ERR_INVALID_ARG;
+  }
+  // the rotated query may take its source's place where the rows are the same; nothing else may overlap
+  const Span qs{q, ((n - 1) * q_stride + q_row) * eb}, ks{kv, ((n - 1) * kv_stride + row) * eb};
+  const Span qo{q ? q_out : nullptr, n * q_row * eb}, cache{kv ? latent_cache : nullptr, num_slots * row * eb};
+  const bool in_place = q && q == q_out && q_stride == q_row;
+  if ((!in_place && overlap(qs, qo)) || outputs_overlap({qo, cache}, {ks}) || overlap(cache, qs))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+size_t page_scores_workspace_bytes(const eg_mla_dims& d, int32_t batch) {
+  return std::max<size_t>(align_up(static_cast<size_t>(std::max(batch, 0)) * d.num_heads *
+                                   static_cast<size_t>(d.latent_dim + d.rope_dim) * sizeof(float)),
+                          kAlign);
+}
+
+eg_mla_status validate_page_means(const eg_mla_dims* d, int32_t batch, const void* latent_cache,
+                                  const int32_t* token_id_cache, const void* gate_table, const int32_t* seq_lens,
+                                  const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                  const void* page_means) {
+  eg_mla_status st = check_dims(d);
+  if (st != EG_MLA_OK) return st;
+  st = check_pages(*d, batch, max_pages_per_seq, num_slots, page_table != nullptr);
+  if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
+  if (!latent_cache || !token_id_cache || !gate_table || !seq_lens || !page_means) return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned16(latent_cache) || !aligned16(gate_table) || !aligned16(page_means)) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t row = static_cast<int64_t>(d->latent_dim + d->rope_dim) * elem_bytes(*d);
+  if (overlap({page_means, num_slots / d->page_size * row}, {latent_cache, num_slots * row}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_page_scores(const eg_mla_dims* d, int32_t batch, const void* q, const void* w_uk,
+                                   const void* page_means, const int32_t* seq_lens, const int32_t* page_table,
+                                   int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
+                                   size_t workspace_bytes, const float* scores) {
+  eg_mla_status st = check_dims(d);
+  if (st != EG_MLA_OK) return st;
+  st = check_pages(*d, batch, max_pages_per_seq, num_slots, page_table != nullptr);
+  if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
+  if (!q || !w_uk || !page_means || !seq_lens || !scores) return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(w_uk) || !aligned16(page_means)) return EG_MLA_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < page_scores_workspace_bytes(*d, batch)) return EG_MLA_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const float* scores, const int32_t* seq_lens,
+                                    const int32_t* page_table, int32_t max_pages_per_seq, int32_t keep,
+                                    int32_t keep_first, int32_t keep_last, const int32_t* sel_pages,
+                                    const int32_t* sel_lens, const int32_t* sel_index) {
+  const eg_mla_status st = check_dims(d);
+  if (st != EG_MLA_OK) return st;
+  if (batch < 0 || max_pages_per_seq < 0 || keep_first < 0 || keep_last < 1 ||
+      static_cast<int64_t>(keep_first) + keep_last > keep)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(max_pages_per_seq) * d->page_size > kMaxCapacity) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t entries = static_cast<int64_t>(batch) * max_pages_per_seq;
+  if (!page_table && entries > 0x7fffffff) return EG_MLA_ERR_INVALID_ARG;  // page numbers are 32-bit
+  if (batch == 0) return EG_MLA_OK;
+  if (!seq_lens || !sel_pages || !sel_lens || (max_pages_per_seq > 0 && !scores)) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t n = 4 * static_cast<int64_t>(batch);
+  if (outputs_overlap({{sel_pages, n * keep}, {sel_lens, n}, {sel_index, n * keep}},
+                      {{seq_lens, n}, {page_table, 4 * entries}, {scores, 4 * entries}}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+namespace {
+
+// The split kernel of one part of a shared decode: the decode's plan without
+// its absorption, schedules and single-launch form (the call absorbs once for
+// both parts and merges them itself).
+eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages, DecodePlan* p) {
+  const eg_mla_status st = make_decode_plan(d, batch, max_pages, nullptr, p);
+  if (st != EG_MLA_OK) return st;
+  p->fused_absorb = p->one_launch = p->tok_balanced = false;
+  p->pieces = 0;
+  if (p->balanced) {
+    p->balanced = false;
+    p->heads_per_group = 16;
+    p->head_groups = ceil_div(d.num_heads, 16);
+    const int64_t s = ceil_div(static_cast<int64_t>(batch) * std::max(p->capacity, 1) * p->head_groups, kTargetWorkItems);
+    p->split_tokens = static_cast<int>(std::min<int64_t>(std::max<int64_t>((s + kTile - 1) / kTile * kTile, 256), kMaxSplitTokens));
+    p->s_max = ceil_div(std::max(p->capacity, 1), p->split_tokens);
+  }
+  if (p->path == EG_MLA_PATH_VALU && !p->f32_mfma) {
+    // the vector kernel's queries and probabilities of a group of heads lie in LDS
+    while (p->heads_per_group > 1 &&
+           4 * static_cast<int64_t>(p->heads_per_group) * (d.latent_dim + d.rope_dim + kTile + 1) > 64 * 1024)
+      p->heads_per_group /= 2;
+    p->head_groups = ceil_div(d.num_heads, p->heads_per_group);
+  }
+  if (p->capacity > 0 && static_cast<int64_t>(batch) * p->s_max * p->head_groups > 0x7fffffff)
+    return EG_MLA_ERR_UNSUPPORTED;
+  return EG_MLA_OK;
+}
+
+}  // namespace
+
+eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,
+                               int32_t max_prefix_pages, SharedPlan* out) {
+  SharedPlan p;
+  // all heads of all sequences are the prefix's heads; merge grid
+  if (static_cast<int64_t>(batch) * d.num_heads > (1 << 30) || batch > 65535) return EG_MLA_ERR_UNSUPPORTED;
+  eg_mla_dims all = d;
+  all.num_heads = std::max(1, batch * d.num_heads);
+  eg_mla_status st = shared_part_plan(all, 1, max_prefix_pages, &p.pre);
+  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, max_pages_per_seq, &p.own);
+  if (st != EG_MLA_OK) return st;
+  const size_t rows = static_cast<size_t>(batch) * d.num_heads;
+  size_t off = align_up(rows * static_cast<size_t>(d.latent_dim + d.rope_dim) * 4);
+  for (DecodePlan* s : {&p.pre, &p.own}) {
+    const size_t n = s->capacity > 0 ? rows * static_cast<size_t>(s->s_max) : 0;
+    s->off_ml = off;
+    off = align_up(off + n * 8);
+    s->off_o = off;
+    off = align_up(off + n * static_cast<size_t>(d.latent_dim) * 4);
+  }
+  p.bytes = std::max<size_t>(off, kAlign);
+  *out = p;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_decode_shared(const eg_mla_dims* d, int32_t batch, const void* q, const void* latent_cache,
+                                     const int32_t* token_id_cache, const void* gate_table, const void* w_uk,
+                                     const void* w_uv, const int32_t* prefix_len, const int32_t* prefix_table,
+                                     int32_t max_prefix_pages, const int32_t* seq_lens, const int32_t* page_table,
+                                     int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
+                                     size_t workspace_bytes, const void* out, SharedPlan* p) {
+  eg_mla_status st = check_dims(d);
+  if (st != EG_MLA_OK) return st;
+  st = check_pages(*d, batch, max_pages_per_seq, num_slots, page_table != nullptr);
+  if (st == EG_MLA_OK) st = check_pages(*d, std::min(batch, 1), max_prefix_pages, num_slots, true);
+  if (st != EG_MLA_OK) return st;
+  st = make_shared_plan(*d, batch, max_pages_per_seq, max_prefix_pages, p);
+  if (st != EG_MLA_OK || batch == 0) return st;
+  if (!q || !gate_table || !w_uk || !w_uv || !out) return EG_MLA_ERR_INVALID_ARG;
+  if (max_prefix_pages > 0 && (!prefix_len || !prefix_table)) return EG_MLA_ERR_INVALID_ARG;
+  if (max_pages_per_seq > 0 && !seq_lens) return EG_MLA_ERR_INVALID_ARG;
+  if ((max_prefix_pages > 0 || max_pages_per_seq > 0) && (!latent_cache || !token_id_cache))
+    return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(latent_cache) || !aligned16(gate_table) || !aligned16(w_uk) || !aligned16(w_uv))
+    return EG_MLA_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < p->bytes) return EG_MLA_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
   return EG_MLA_OK;
 }

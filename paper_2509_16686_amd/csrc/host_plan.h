@@ -152,6 +152,58 @@ eg_mla_status validate_literal(const eg_mla_dims* d, int32_t batch, const void* 
                                const int32_t* seq_lens, const int32_t* page_table, int32_t max_pages_per_seq,
                                int64_t num_slots, const void* workspace, size_t workspace_bytes, const void* out);
 
+// Page tables and positions from request lengths (pages.hip): a batch's two
+// running sums lie in LDS.
+constexpr int kPageMaxBatch = 4096;
+eg_mla_status validate_page_plan(int32_t batch, int32_t page_size, int32_t max_pages_per_seq, int32_t max_tokens,
+                                 const int32_t* cached_lens, const int32_t* new_lens, const int32_t* position_base,
+                                 const int32_t* page_table, const int32_t* free_pages, const int32_t* free_count,
+                                 int32_t free_capacity, const int32_t* seq_lens, const int32_t* cu_seqlens,
+                                 const int32_t* positions, const int32_t* slots, const int32_t* free_count_out);
+eg_mla_status validate_page_release(int32_t batch, int32_t page_size, int32_t max_pages_per_seq,
+                                    const int32_t* seq_lens, const int32_t* ended, const int32_t* page_table,
+                                    const int32_t* free_pages, const int32_t* free_count, int32_t free_capacity,
+                                    const int32_t* seq_lens_out, const int32_t* free_count_out);
+
+// Norms and rotation of queries and keys (qk_rope.hip).
+eg_mla_status validate_qk(const eg_mla_dims* d, int32_t n_tokens, const void* q, int64_t q_stride,
+                          const void* q_norm_w, const void* q_out, const void* kv, int64_t kv_stride,
+                          const void* kv_norm_w, const void* k_norm_w, const int32_t* token_ids,
+                          const int32_t* positions, const int32_t* slots, float rope_theta, const void* latent_cache,
+                          const int32_t* token_id_cache, int64_t num_slots);
+
+// Page means, scores and selection (page_select.hip).
+size_t page_scores_workspace_bytes(const eg_mla_dims& d, int32_t batch);  // absorbed queries, fp32 [B, H, d_c + d_r]
+eg_mla_status validate_page_means(const eg_mla_dims* d, int32_t batch, const void* latent_cache,
+                                  const int32_t* token_id_cache, const void* gate_table, const int32_t* seq_lens,
+                                  const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                  const void* page_means);
+eg_mla_status validate_page_scores(const eg_mla_dims* d, int32_t batch, const void* q, const void* w_uk,
+                                   const void* page_means, const int32_t* seq_lens, const int32_t* page_table,
+                                   int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
+                                   size_t workspace_bytes, const float* scores);
+eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const float* scores, const int32_t* seq_lens,
+                                    const int32_t* page_table, int32_t max_pages_per_seq, int32_t keep,
+                                    int32_t keep_first, int32_t keep_last, const int32_t* sel_pages,
+                                    const int32_t* sel_lens, const int32_t* sel_index);
+
+// Decode with a shared prefix (decode_shared.h): `pre` is the decode of one
+// sequence of B H heads over the prefix, `own` that of the batch over its own
+// tokens; their off_ml and off_o are offsets into the call's one workspace.
+struct SharedPlan {
+  DecodePlan pre, own;
+  size_t off_q = 0;  // fp32 [B, H, d_c + d_r]
+  size_t bytes = 0;
+};
+eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,
+                               int32_t max_prefix_pages, SharedPlan* out);
+eg_mla_status validate_decode_shared(const eg_mla_dims* d, int32_t batch, const void* q, const void* latent_cache,
+                                     const int32_t* token_id_cache, const void* gate_table, const void* w_uk,
+                                     const void* w_uv, const int32_t* prefix_len, const int32_t* prefix_table,
+                                     int32_t max_prefix_pages, const int32_t* seq_lens, const int32_t* page_table,
+                                     int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
+                                     size_t workspace_bytes, const void* out, SharedPlan* p);
+
 inline float softmax_scale(const eg_mla_dims& d) {
   if (d.softmax_scale > 0.f) return d.softmax_scale;
   return 1.0f / __builtin_sqrtf(static_cast<float>(d.head_dim + d.rope_dim));

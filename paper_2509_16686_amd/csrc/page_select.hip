@@ -1,0 +1,337 @@
+// Sparse attention over cache pages (gfx950): the mean key of each page, a
+// query's score of every page from it, and the pages that a query attends to.
+// The decode over the chosen pages is eg_mla_decode on the table that
+// eg_mla_select_pages writes.
+//
+//   mean[p]     = (1/n) sum_i [c_i (.) G[id_i] | k^R_i]      over the page's n cached tokens
+//   score[b,j]  = max_h tau (q_lat[b,h] . mean_c + q^R[b,h] . mean_r)   of page j of sequence b
+//
+// With the gate in the latent space a page's mean key is one vector for all
+// heads (the mean of c~ commutes with W_UK[h]), of the cache row's size.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "absorb.h"
+#include "device_common.h"
+#include "eg_mla.h"
+#include "host_plan.h"
+
+namespace egmla {
+
+// ---------------------------------------------------------------------------
+// Page means.  A work-group takes whole pages of one sequence: thread (r, c)
+// adds piece c (16 bytes) of the page's rows r, r + rows, ...; the row lanes
+// meet in LDS.  Sums are in 64 bits: the products of two bf16 values are exact
+// there and a sum of up to 2^20 of them is off by far less than the last bit
+// of its rounding, so that a mean does not depend on the order of its tokens
+// (a page whose means are formed again from the same rows keeps its bits).
+// Bound by the latency of length, table entry, id and row for a step's pages,
+// by HBM for a prompt's.
+// ---------------------------------------------------------------------------
+constexpr int kMeanThreads = 256;
+constexpr int kMeanGroups = 1024;  // work-groups, about: four per compute unit
+
+struct MeansArgs {
+  const void* cache;
+  const int32_t* ids;
+  const void* gate;
+  const int32_t* first;  // or null
+  const int32_t* lens;
+  const int32_t* table;  // or null
+  void* means;
+  int64_t num_slots;
+  int32_t DC, DR, P, W, V, cap;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void load_piece(const void* p, int64_t i, float (&v)[BF16 ? 8 : 4]) {
+  if constexpr (BF16) {
+    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = bf16_lo(w[e]);
+      v[2 * e + 1] = bf16_hi(w[e]);
+    }
+  } else {
+    const f32x4_t w = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = w[e];
+  }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kMeanThreads) void page_means_kernel(MeansArgs a) {
+  constexpr int N = BF16 ? 8 : 4;
+  __shared__ double red[kMeanThreads * N];
+  const int b = blockIdx.x;
+  const int DQ = a.DC + a.DR, np = DQ / N;  // np <= 160 pieces
+  const int rows = kMeanThreads / np;
+  const int tid = threadIdx.x, c = tid % np, r = tid / np;
+  const int L = clamp_len(a.lens[b], a.cap);
+  const int first = a.first ? max(a.first[b], 0) : 0;
+  if (first >= L) return;
+  const int64_t npages = a.num_slots / a.P;
+  for (int pg = first / a.P + blockIdx.y; static_cast<int64_t>(pg) * a.P < L; pg += gridDim.y) {
+    const int n = min(a.P, L - pg * a.P);
+    const int64_t page = a.table ? a.table[static_cast<int64_t>(b) * a.W + pg] : static_cast<int64_t>(b) * a.W + pg;
+    if (page < 0 || page >= npages) continue;  // uniform: no such page of the cache
+    double acc[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = 0.0;
+    if (r < rows) {
+      for (int i = r; i < n; i += rows) {
+        const int64_t slot = page * a.P + i;
+        float x[N];
+        load_piece<BF16>(a.cache, slot * DQ + c * N, x);
+        if (c * N < a.DC) {
+          float g[N];
+          load_piece<BF16>(a.gate, static_cast<int64_t>(clamp_id(a.ids[slot], a.V)) * a.DC + c * N, g);
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[e] += static_cast<double>(x[e]) * static_cast<double>(g[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[e] += static_cast<double>(x[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) red[e * kMeanThreads + tid] = acc[e];
+    __syncthreads();
+    for (int i = tid; i < DQ; i += kMeanThreads) {
+      double s = 0.0;
+      for (int k = 0; k < rows; ++k) s += red[(i % N) * kMeanThreads + k * np + i / N];
+      st<BF16>(a.means, page * DQ + i, static_cast<float>(s / n));
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Page scores.  q rows are [q_lat | q^R] in fp32, from the absorption.
+// ---------------------------------------------------------------------------
+struct ScoreArgs {
+  const float* qfull;  // [B, H, DC + DR]
+  const void* means;
+  const int32_t* lens;
+  const int32_t* table;  // or null
+  float* scores;         // [B, W]
+  int64_t num_slots;
+  int32_t H, DQ, P, W, cap;
+  float scale;
+};
+
+// The page of column j of sequence b, clamped into the cache.
+__device__ __forceinline__ int64_t score_page(const ScoreArgs& a, int b, int j) {
+  const int64_t npages = a.num_slots / a.P;
+  int64_t page = a.table ? a.table[static_cast<int64_t>(b) * a.W + j] : static_cast<int64_t>(b) * a.W + j;
+  page = page < 0 ? 0 : page;
+  return page < npages ? page : npages - 1;
+}
+
+// Any shape, fp32 arithmetic: one wave per page, lanes along the row.
+template <bool BF16>
+__global__ __launch_bounds__(256) void page_scores_kernel(ScoreArgs a) {
+  const int b = blockIdx.x, lane = threadIdx.x & 63;
+  const int pages = (clamp_len(a.lens[b], a.cap) + a.P - 1) / a.P;
+  for (int j = blockIdx.y * 4 + (threadIdx.x >> 6); j < a.W; j += gridDim.y * 4) {
+    float best = -INFINITY;
+    if (j < pages) {
+      const int64_t row = score_page(a, b, j) * a.DQ;
+      float m[10];  // d_c + d_r <= 640
+#pragma unroll
+      for (int i = 0; i < 10; ++i) m[i] = lane + 64 * i < a.DQ ? ld<BF16>(a.means, row + lane + 64 * i) : 0.f;
+      for (int h = 0; h < a.H; ++h) {
+        const float* q = a.qfull + (static_cast<int64_t>(b) * a.H + h) * a.DQ;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 10; ++i)
+          if (lane + 64 * i < a.DQ) s = fmaf(q[lane + 64 * i], m[i], s);
+        best = fmaxf(best, wave_sum(s) * a.scale);
+      }
+    }
+    if (lane == 0) a.scores[static_cast<int64_t>(b) * a.W + j] = best;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Page selection: one work-group per sequence.  A page's key is its score as
+// an unsigned number of the same order (a NaN counts as -inf, -0 as 0; pages
+// that are always kept come first); the K-th largest key is found by four
+// passes over 8 bits each (a histogram in LDS), then every key above it and
+// the first ones equal to it are written in the order of the sequence.
+// ---------------------------------------------------------------------------
+constexpr int kSelThreads = 1024;
+
+struct SelectArgs {
+  const float* scores;
+  const int32_t* lens;
+  const int32_t* table;  // or null
+  int32_t* sel;
+  int32_t* sel_lens;
+  int32_t* sel_index;  // or null
+  int32_t W, P, K, cap, keep_first, keep_last;
+};
+
+__device__ __forceinline__ uint32_t score_key(float s) {
+  if (s != s) s = -INFINITY;
+  const uint32_t u = __float_as_uint(s + 0.f);  // -0 + 0 is +0
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(kSelThreads) void select_pages_kernel(SelectArgs a) {
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t state[2];  // prefix of the K-th key, keys still to take among those with it
+  __shared__ uint32_t above_w[kSelThreads / 64], equal_w[kSelThreads / 64];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int L = clamp_len(a.lens[b], a.cap);
+  const int n = (L + a.P - 1) / a.P;
+  int32_t* sel = a.sel + static_cast<int64_t>(b) * a.K;
+  int32_t* index = a.sel_index ? a.sel_index + static_cast<int64_t>(b) * a.K : nullptr;
+  auto page_of = [&](int j) { return a.table ? a.table[static_cast<int64_t>(b) * a.W + j] : b * a.W + j; };
+  if (tid == 0) a.sel_lens[b] = n <= a.K ? L : L - (n - a.K) * a.P;
+  if (n <= a.K) {  // every page
+    for (int j = tid; j < a.K; j += kSelThreads) {
+      sel[j] = j < n ? page_of(j) : -1;
+      if (index) index[j] = j < n ? j : -1;
+    }
+    return;
+  }
+  const float* score = a.scores + static_cast<int64_t>(b) * a.W;
+  auto key_of = [&](int j) {
+    return j < a.keep_first || j >= n - a.keep_last ? 0xffffffffu : score_key(score[j]);
+  };
+  uint32_t prefix = 0, want = a.K;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += kSelThreads) {
+      const uint32_t k = key_of(j);
+      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    if (w == 0) {  // the digit whose keys hold the `want`-th from the top: lane l looks at digits 255 - 4 l ...
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        c[e] = hist[255 - 4 * lane - e];
+        sum += c[e];
+      }
+      uint32_t incl = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += u;
+      }
+      uint32_t before = incl - sum;
+      if (before < want && want <= incl) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (before < want && want <= before + c[e]) {
+            state[0] = (prefix << 8) | static_cast<uint32_t>(255 - 4 * lane - e);
+            state[1] = want - before;
+          }
+          before += c[e];
+        }
+      }
+    }
+    __syncthreads();
+    prefix = state[0];
+    want = state[1];
+  }
+  // keys above `prefix`, and the first `want` equal to it, in order
+  uint32_t above = 0, equal = 0;
+  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
+    const int j = j0 + tid;
+    const uint32_t k = j < n ? key_of(j) : 0u;
+    const bool is_above = j < n && k > prefix, is_equal = j < n && k == prefix;
+    const uint64_t ma = __ballot(is_above), me = __ballot(is_equal);
+    __syncthreads();
+    if (lane == 0) {
+      above_w[w] = __popcll(ma);
+      equal_w[w] = __popcll(me);
+    }
+    __syncthreads();
+    uint32_t ra = above, re = equal;
+    for (int i = 0; i < kSelThreads / 64; ++i) {
+      if (i < w) {
+        ra += above_w[i];
+        re += equal_w[i];
+      }
+      above += above_w[i];
+      equal += equal_w[i];
+    }
+    const uint64_t low = (uint64_t{1} << lane) - 1;
+    ra += __popcll(ma & low);
+    re += __popcll(me & low);
+    if (is_above || (is_equal && re < want)) {
+      const uint32_t at = ra + min(re, want);
+      sel[at] = page_of(j);
+      if (index) index[at] = j;
+    }
+  }
+}
+
+}  // namespace egmla
+
+using namespace egmla;
+
+extern "C" eg_mla_status eg_mla_page_means(const eg_mla_dims* dims, int32_t batch, const void* latent_cache,
+                                           const int32_t* token_id_cache, const void* gate_table,
+                                           const int32_t* first_tokens, const int32_t* seq_lens,
+                                           const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                           void* page_means, void* stream_) {
+  const eg_mla_status st = validate_page_means(dims, batch, latent_cache, token_id_cache, gate_table, seq_lens,
+                                               page_table, max_pages_per_seq, num_slots, page_means);
+  if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
+  const eg_mla_dims& d = *dims;
+  MeansArgs a{latent_cache, token_id_cache, gate_table, first_tokens, seq_lens, page_table, page_means, num_slots,
+              d.latent_dim, d.rope_dim, d.page_size, max_pages_per_seq, d.vocab_size, max_pages_per_seq * d.page_size};
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  (void)hipGetLastError();
+  const dim3 grid(batch, std::min(max_pages_per_seq, std::max(1, kMeanGroups / batch)));
+  if (d.dtype == EG_MLA_BF16) hipLaunchKernelGGL(page_means_kernel<true>, grid, dim3(kMeanThreads), 0, stream, a);
+  else hipLaunchKernelGGL(page_means_kernel<false>, grid, dim3(kMeanThreads), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
+}
+
+extern "C" size_t eg_mla_page_scores_workspace_size(const eg_mla_dims* dims, int32_t batch) {
+  if (check_dims(dims) != EG_MLA_OK || batch < 0) return 0;
+  return page_scores_workspace_bytes(*dims, batch);
+}
+
+extern "C" eg_mla_status eg_mla_page_scores(const eg_mla_dims* dims, int32_t batch, const void* q, const void* w_uk,
+                                            const void* page_means, const int32_t* seq_lens,
+                                            const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                            void* workspace, size_t workspace_bytes, float* scores, void* stream_) {
+  const eg_mla_status st = validate_page_scores(dims, batch, q, w_uk, page_means, seq_lens, page_table,
+                                                max_pages_per_seq, num_slots, workspace, workspace_bytes, scores);
+  if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
+  const eg_mla_dims& d = *dims;
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  (void)hipGetLastError();
+  if (launch_absorb(d, batch, q, w_uk, static_cast<float*>(workspace), stream) != hipSuccess) return EG_MLA_ERR_HIP;
+  ScoreArgs a{static_cast<const float*>(workspace), page_means, seq_lens, page_table, scores, num_slots, d.num_heads,
+              d.latent_dim + d.rope_dim, d.page_size, max_pages_per_seq, max_pages_per_seq * d.page_size,
+              softmax_scale(d)};
+  const dim3 grid(batch, std::min((max_pages_per_seq + 3) / 4, std::max(1, 2048 / batch)));
+  if (d.dtype == EG_MLA_BF16) hipLaunchKernelGGL(page_scores_kernel<true>, grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(page_scores_kernel<false>, grid, dim3(256), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
+}
+
+extern "C" eg_mla_status eg_mla_select_pages(const eg_mla_dims* dims, int32_t batch, const float* scores,
+                                             const int32_t* seq_lens, const int32_t* page_table,
+                                             int32_t max_pages_per_seq, int32_t keep, int32_t keep_first,
+                                             int32_t keep_last, int32_t* sel_pages, int32_t* sel_lens,
+                                             int32_t* sel_index, void* stream_) {
+  const eg_mla_status st = validate_select_pages(dims, batch, scores, seq_lens, page_table, max_pages_per_seq, keep,
+                                                 keep_first, keep_last, sel_pages, sel_lens, sel_index);
+  if (st != EG_MLA_OK || batch == 0) return st;
+  SelectArgs a{scores, seq_lens, page_table, sel_pages, sel_lens, sel_index, max_pages_per_seq, dims->page_size, keep,
+               max_pages_per_seq * dims->page_size, keep_first, keep_last};
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(select_pages_kernel, dim3(batch), dim3(kSelThreads), 0, static_cast<hipStream_t>(stream_), a);
+  return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
+}
