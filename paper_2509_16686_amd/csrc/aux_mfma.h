@@ -31,35 +31,25 @@ constexpr int kAbsColsNarrow = 32;
 // Below this many work-groups the absorption takes the narrow column slices.
 constexpr int kAbsMinWorkGroups = 128;
 
-// HALF: instead of fp32 rows [B, H, DC + DR], write 16-bit rows [B, H, DC + DR]
-// = [q_lat in fp16 (one rounding) | q^R in bf16 (copied)], the operands of the
-// wide kernel's fp16 latent product and exact bf16 RoPE product.
-// SCHED: the grid has one more column of work-groups (blockIdx.x == H), the
-// first of which computes the balanced schedule from the lengths (sa).
-// (HALF: the wide kernel's schedule, otherwise the d_c 128 kernel's)
-template <int DH, int BLOCKS, int COLS, bool HALF = false, bool SCHED = HALF>
-__global__ __launch_bounds__(256) void absorb_mfma_kernel(const uint16_t* __restrict__ q,
-                                                          const uint16_t* __restrict__ w_uk,
-                                                          float* __restrict__ qfull, int B, int H, int DC, int DR,
-                                                          SchedArgs sa) {
+// Rows written: fp32 [B, H, DC + DR], or 16-bit [B, H, DC + DR] = [q_lat in
+// fp16 (one rounding) | q^R in bf16 (copied)], the operands of fp16 latent
+// products and exact bf16 RoPE products, or both.
+enum class AbsorbRows { kFloat, kHalf, kBoth };
+
+// Tile (h, by, bz) of the absorption: head h, row block by, column slice bz.
+template <int DH, int BLOCKS, int COLS, AbsorbRows ROWS_OUT>
+__device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, const uint16_t* __restrict__ w_uk,
+                                            float* __restrict__ qfull, uint16_t* __restrict__ qhalf, int B, int H,
+                                            int DC, int DR, int h, int by, int bz) {
   static_assert(BLOCKS >= 1 && BLOCKS <= kAbsBlocks, "row blocks per work-group");
-  if constexpr (SCHED) {
-    if (blockIdx.x == H) {
-      if (blockIdx.y == 0 && blockIdx.z == 0) {
-        if constexpr (HALF) wide_schedule<256>(sa.wide, B);
-        else tok_schedule<256>(sa.tok, B);
-      }
-      return;
-    }
-  }
+  constexpr bool FLOAT = ROWS_OUT != AbsorbRows::kHalf, HALF = ROWS_OUT != AbsorbRows::kFloat;
   static_assert(COLS % 16 == 0 && COLS <= 128, "latent columns per work-group");
   constexpr int RS = COLS + 8;  // padded LDS row (bf16 elements)
   constexpr int NK = DH / 32;
   __shared__ __attribute__((aligned(16))) uint16_t wrm[DH * RS];  // [k][c], row-major
   constexpr int ROWS = kAbsRows * BLOCKS;  // sequences of this work-group
-  const int h = blockIdx.x;
-  const int b0 = blockIdx.y * ROWS;
-  const int c0 = blockIdx.z * COLS;
+  const int b0 = by * ROWS;
+  const int c0 = bz * COLS;
   const int nc = min(COLS, DC - c0);
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
   const int DQin = DH + DR, DQ = DC + DR;
@@ -89,7 +79,7 @@ __global__ __launch_bounds__(256) void absorb_mfma_kernel(const uint16_t* __rest
   // and at most 64, thread t loads 4 consecutive values of row t / (d_r / 4)
   // of each row block (8-byte loads, rows clamped so the loads are
   // unconditional); other shapes copy element by element after the product.
-  const bool rope_vec = blockIdx.z == 0 && DR > 0 && DR % 4 == 0 && DR <= 64;
+  const bool rope_vec = bz == 0 && DR > 0 && DR % 4 == 0 && DR <= 64;
   const int rq_row = rope_vec ? tid / (DR / 4) : 0;  // row within a block
   const int rq_col = rope_vec ? 4 * (tid % (DR / 4)) : 0;
   uint2 rq[BLOCKS];
@@ -134,12 +124,10 @@ __global__ __launch_bounds__(256) void absorb_mfma_kernel(const uint16_t* __rest
       for (int r = 0; r < 4; ++r) {
         const int b = b0 + rb * kAbsRows + 4 * g + r;
         if (b < B && c < DC) {
-          if constexpr (HALF) {
-            reinterpret_cast<_Float16*>(qfull)[(static_cast<int64_t>(b) * H + h) * DQ + c] =
+          if constexpr (HALF)
+            reinterpret_cast<_Float16*>(qhalf)[(static_cast<int64_t>(b) * H + h) * DQ + c] =
                 static_cast<_Float16>(acc[rb][r]);
-          } else {
-            qfull[(static_cast<int64_t>(b) * H + h) * DQ + c] = acc[rb][r];
-          }
+          if constexpr (FLOAT) qfull[(static_cast<int64_t>(b) * H + h) * DQ + c] = acc[rb][r];
         }
       }
     }
@@ -150,25 +138,42 @@ __global__ __launch_bounds__(256) void absorb_mfma_kernel(const uint16_t* __rest
       const int b = b0 + rb * kAbsRows + rq_row;
       if (rq_row < kAbsRows && b < B) {
         if constexpr (HALF)
-          *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(qfull) + (static_cast<int64_t>(b) * H + h) * DQ + DC +
-                                    rq_col) = rq[rb];
-        else
+          *reinterpret_cast<uint2*>(qhalf + (static_cast<int64_t>(b) * H + h) * DQ + DC + rq_col) = rq[rb];
+        if constexpr (FLOAT)
           *reinterpret_cast<float4*>(qfull + (static_cast<int64_t>(b) * H + h) * DQ + DC + rq_col) =
               make_float4(bf16_lo(rq[rb].x), bf16_hi(rq[rb].x), bf16_lo(rq[rb].y), bf16_hi(rq[rb].y));
       }
     }
-  } else if (blockIdx.z == 0) {
+  } else if (bz == 0) {
     for (int i = tid; i < ROWS * DR; i += 256) {
       const int bb = i / DR, r = i % DR;
       if (b0 + bb < B) {
         const uint16_t v = q[(static_cast<int64_t>(b0 + bb) * H + h) * DQin + DH + r];
-        if constexpr (HALF)
-          reinterpret_cast<uint16_t*>(qfull)[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r] = v;
-        else
+        if constexpr (HALF) qhalf[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r] = v;
+        if constexpr (FLOAT)
           qfull[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r] = bf16_to_f32(v);
       }
     }
   }
+}
+
+// HALF: 16-bit rows instead of fp32 ones (the wide kernel's), at the same place.
+template <int DH, int BLOCKS, int COLS, bool HALF = false, bool SCHED = HALF>
+__global__ __launch_bounds__(256) void absorb_mfma_kernel(const uint16_t* __restrict__ q,
+                                                          const uint16_t* __restrict__ w_uk,
+                                                          float* __restrict__ qfull, int B, int H, int DC, int DR,
+                                                          SchedArgs sa) {
+  if constexpr (SCHED) {
+    if (blockIdx.x == H) {
+      if (blockIdx.y == 0 && blockIdx.z == 0) {
+        if constexpr (HALF) wide_schedule<256>(sa.wide, B);
+        else tok_schedule<256>(sa.tok, B);
+      }
+      return;
+    }
+  }
+  absorb_tile<DH, BLOCKS, COLS, HALF ? AbsorbRows::kHalf : AbsorbRows::kFloat>(
+      q, w_uk, qfull, reinterpret_cast<uint16_t*>(qfull), B, H, DC, DR, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 // ---------------------------------------------------------------------------

@@ -10,6 +10,8 @@
 //   out[b,h] = W_UV[h] o.
 #pragma once
 
+#include "shared_prefix.h"
+
 namespace egmla {
 
 // Partial rows of one part: row (s, i) of query row i is at s * stride + i * step.
@@ -73,55 +75,165 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedPart pre, Sha
 
 namespace {
 
-eg_mla_status run_decode_shared(const eg_mla_dims& d, const SharedPlan& p, int32_t batch, const void* q,
-                                const void* latent_cache, const int32_t* token_id_cache, const void* gate_table,
-                                const void* w_uk, const void* w_uv, const int32_t* prefix_len,
-                                const int32_t* prefix_table, int32_t max_prefix_pages, const int32_t* seq_lens,
-                                const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
-                                void* workspace, void* out, hipStream_t stream) {
-  (void)hipGetLastError();
-  unsigned char* ws = static_cast<unsigned char*>(workspace);
-  float* qfull = reinterpret_cast<float*>(ws + p.off_q);
-  if (launch_absorb(d, batch, q, w_uk, qfull, stream) != hipSuccess) return EG_MLA_ERR_HIP;
+// Everything a shared decode's launches read.
+struct SharedCall {
+  const eg_mla_dims& d;
+  const SharedPlan& p;
+  int32_t batch;
+  const void *q, *cache;
+  const int32_t* ids;
+  const void *gate, *w_uk, *w_uv;
+  const int32_t *prefix_len, *prefix_table;
+  int32_t max_prefix_pages;
+  const int32_t *seq_lens, *page_table;
+  int32_t max_pages;
+  int64_t num_slots;
+  unsigned char* ws;
+  void* out;
+  hipStream_t stream;
+};
+
+// Sequences of a merge work-group: 16, or fewer while that leaves under one work-group per compute unit.
+constexpr int kSharedMergeGroups = 256;
+
+// Split kernel of the prefix (part 0, as one sequence of B H heads) or of the own tokens (part 1).
+hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {
+  const DecodePlan& s = part ? c.p.own : c.p.pre;
+  eg_mla_dims ds = c.d;
+  if (part == 0) ds.num_heads = c.batch * c.d.num_heads;
   SplitArgs a{};
   a.qfull = qfull;
-  a.cache = latent_cache;
-  a.ids = token_id_cache;
-  a.gate = gate_table;
-  a.num_slots = num_slots;
-  a.DC = d.latent_dim;
-  a.DR = d.rope_dim;
-  a.P = d.page_size;
-  a.V = d.vocab_size;
-  a.scale_log2 = softmax_scale(d) * kLog2e;
-  a.DH = d.head_dim;
-  // the prefix: one sequence of B H heads; then each sequence's own tokens
-  SharedPart parts[2] = {};
-  for (int part = 0; part < 2; ++part) {
-    const DecodePlan& s = part ? p.own : p.pre;
-    if (s.capacity == 0) continue;
-    eg_mla_dims ds = d;
-    if (part == 0) ds.num_heads = batch * d.num_heads;
-    a.B = part ? batch : 1;
-    a.H = ds.num_heads;
-    a.seq_lens = part ? seq_lens : prefix_len;
-    a.page_table = part ? page_table : prefix_table;
-    a.max_pages = part ? max_pages_per_seq : max_prefix_pages;
-    a.cap = s.capacity;
-    a.split = s.split_tokens;
-    a.s_max = s.s_max;
-    a.groups = s.head_groups;
-    a.hpg = s.heads_per_group;
-    a.part_ml = reinterpret_cast<float*>(ws + s.off_ml);
-    a.part_o = reinterpret_cast<float*>(ws + s.off_o);
-    const OneArgs one{q, w_uk, w_uv, out, d.v_head_dim, 1, 1};
-    if (launch_split(ds, s, a, one, stream, nullptr, nullptr) != hipSuccess) return EG_MLA_ERR_HIP;
-    parts[part] = {a.part_ml, a.part_o, a.seq_lens, s.capacity, s.split_tokens, s.s_max};
+  a.cache = c.cache;
+  a.ids = c.ids;
+  a.gate = c.gate;
+  a.num_slots = c.num_slots;
+  a.DC = c.d.latent_dim;
+  a.DR = c.d.rope_dim;
+  a.P = c.d.page_size;
+  a.V = c.d.vocab_size;
+  a.scale_log2 = softmax_scale(c.d) * kLog2e;
+  a.DH = c.d.head_dim;
+  a.B = part ? c.batch : 1;
+  a.H = ds.num_heads;
+  a.seq_lens = part ? c.seq_lens : c.prefix_len;
+  a.page_table = part ? c.page_table : c.prefix_table;
+  a.max_pages = part ? c.max_pages : c.max_prefix_pages;
+  a.cap = s.capacity;
+  a.split = s.split_tokens;
+  a.s_max = s.s_max;
+  a.groups = s.head_groups;
+  a.hpg = s.heads_per_group;
+  a.part_ml = reinterpret_cast<float*>(c.ws + s.off_ml);
+  a.part_o = reinterpret_cast<float*>(c.ws + s.off_o);
+  if (s.balanced) {
+    a.sched_hdr = reinterpret_cast<const int64_t*>(c.ws + s.off_sched);
+    a.wg_start = reinterpret_cast<const int2*>(c.ws + s.off_sched + 16);
   }
-  const size_t lds = sizeof(float) * static_cast<size_t>(d.latent_dim);
+  *rows = {a.part_ml, a.part_o, a.seq_lens, s.capacity, s.split_tokens, s.s_max};
+  const OneArgs one{c.q, c.w_uk, c.w_uv, c.out, c.d.v_head_dim, 1, 1};
+  return launch_split(ds, s, a, one, c.stream, nullptr, nullptr);
+}
+
+template <int DC>
+hipError_t launch_tiled(const SharedCall& c) {
+  const eg_mla_dims& d = c.d;
+  const SharedPlan& p = c.p;
+  const bool wide = p.own.balanced && p.own.capacity > 0;
+  int2* seq_rows = reinterpret_cast<int2*>(c.ws + p.own.off_sched + 16 + kWideMaxGroups * 8);
+  PrefixPrepArgs pa{};
+  pa.q = static_cast<const uint16_t*>(c.q);
+  pa.w_uk = static_cast<const uint16_t*>(c.w_uk);
+  pa.qfull = reinterpret_cast<float*>(c.ws + p.off_q);
+  pa.qhalf = reinterpret_cast<uint16_t*>(c.ws + p.off_half);
+  pa.cache = static_cast<const uint16_t*>(c.cache);
+  pa.ids = c.ids;
+  pa.gate = static_cast<const uint16_t*>(c.gate);
+  pa.len = c.prefix_len;
+  pa.table = c.prefix_table;
+  pa.tiles = c.ws + p.off_tiles;
+  pa.num_slots = c.num_slots;
+  if (wide)
+    pa.sched = {c.seq_lens, p.own.capacity, wide_groups(p.own.head_groups),
+                reinterpret_cast<int64_t*>(c.ws + p.own.off_sched),
+                reinterpret_cast<int2*>(c.ws + p.own.off_sched + 16), seq_rows};
+  pa.B = c.batch;
+  pa.H = d.num_heads;
+  pa.DC = DC;
+  pa.V = d.vocab_size;
+  pa.P = d.page_size;
+  pa.cap = p.pre.capacity;
+  pa.gate_wgs = std::min((p.pre.capacity + kPrepTokens - 1) / kPrepTokens, kPrepGroups);
+  const AbsorbGrid ag = absorb_grid(d, c.batch, p.own.balanced);
+  pa.row_blocks = ag.grid.y;
+  auto prep = p.own.balanced ? shared_prep_kernel<AbsorbRows::kHalf, kAbsBlocks, kAbsCols>
+              : ag.grouped   ? shared_prep_kernel<AbsorbRows::kBoth, kAbsBlocks, kAbsCols>
+              : ag.narrow    ? shared_prep_kernel<AbsorbRows::kBoth, 1, kAbsColsNarrow>
+                             : shared_prep_kernel<AbsorbRows::kBoth, 1, kAbsCols>;
+  const int64_t prep_wgs = 1 + pa.gate_wgs + static_cast<int64_t>(ag.grid.x) * ag.grid.y * ag.grid.z;
+  if (prep_wgs > 0x7fffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(prep, dim3(static_cast<unsigned>(prep_wgs)), dim3(256), 0, c.stream, pa);
+
+  PrefixArgs a{};
+  a.qhalf = pa.qhalf;
+  a.tiles = pa.tiles;
+  a.len = c.prefix_len;
+  a.part_ml = reinterpret_cast<float*>(c.ws + p.pre.off_ml);
+  a.part_o = reinterpret_cast<uint16_t*>(c.ws + p.pre.off_o);
+  a.cap = p.pre.capacity;
+  a.rows = c.batch * d.num_heads;
+  a.row_blocks = p.row_blocks;
+  a.s_max = p.splits;
+  a.scale_log2 = softmax_scale(d) * kLog2e;
+  hipLaunchKernelGGL(shared_prefix_kernel<DC>, dim3(p.row_blocks * p.splits), dim3(kPrefixThreads), 0, c.stream, a);
+
+  SharedPart own{};
+  if (p.own.capacity > 0) {
+    const hipError_t e = launch_shared_part(c, 1, wide ? reinterpret_cast<const float*>(pa.qhalf) : pa.qfull, &own);
+    if (e != hipSuccess) return e;
+  }
+  SharedMergeArgs m{};
+  m.pre_ml = a.part_ml;
+  m.pre_o = a.part_o;
+  m.pre_len = c.prefix_len;
+  m.own_ml = own.ml;
+  m.own_o = own.o;
+  m.own_lens = own.lens;
+  m.own_rows = seq_rows;
+  m.w_uv = static_cast<const uint16_t*>(c.w_uv);
+  m.out = static_cast<uint16_t*>(c.out);
+  m.B = c.batch;
+  m.H = d.num_heads;
+  m.pre_cap = p.pre.capacity;
+  m.pre_s_max = p.splits;
+  m.own_cap = own.cap;
+  m.own_split = own.split;
+  m.own_s_max = own.s_max;
+  m.spw = kSharedMergeSeq;
+  while (m.spw > 1 && static_cast<int64_t>(d.num_heads) * ((c.batch + m.spw - 1) / m.spw) < kSharedMergeGroups) m.spw /= 2;
+  auto merge = shared_merge_kernel<DC, false>;
+  if constexpr (DC == 512) merge = wide ? shared_merge_kernel<DC, true> : merge;
+  hipLaunchKernelGGL(merge, dim3(d.num_heads, (c.batch + m.spw - 1) / m.spw), dim3(kSharedMergeWaves * 64), 0, c.stream, m);
+  return hipGetLastError();
+}
+
+eg_mla_status run_decode_shared(const SharedCall& c) {
+  const eg_mla_dims& d = c.d;
+  (void)hipGetLastError();
+  if (c.p.tiled) {
+    const hipError_t e = d.latent_dim == 128   ? launch_tiled<128>(c)
+                         : d.latent_dim == 320 ? launch_tiled<320>(c)
+                                               : launch_tiled<512>(c);
+    return e == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
+  }
+  float* qfull = reinterpret_cast<float*>(c.ws + c.p.off_q);
+  if (launch_absorb(d, c.batch, c.q, c.w_uk, qfull, c.stream) != hipSuccess) return EG_MLA_ERR_HIP;
+  SharedPart parts[2] = {};
+  for (int part = 0; part < 2; ++part)
+    if ((part ? c.p.own : c.p.pre).capacity > 0 && launch_shared_part(c, part, qfull, &parts[part]) != hipSuccess)
+      return EG_MLA_ERR_HIP;
   auto kern = d.dtype == EG_MLA_BF16 ? shared_combine_kernel<true> : shared_combine_kernel<false>;
-  hipLaunchKernelGGL(kern, dim3(d.num_heads, batch), dim3(256), lds, stream, parts[0], parts[1], w_uv, out, batch,
-                     d.num_heads, d.latent_dim, d.v_head_dim);
+  hipLaunchKernelGGL(kern, dim3(d.num_heads, c.batch), dim3(256), sizeof(float) * d.latent_dim, c.stream, parts[0],
+                     parts[1], c.w_uv, c.out, c.batch, d.num_heads, d.latent_dim, d.v_head_dim);
   return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
 }
 
@@ -148,7 +260,7 @@ extern "C" eg_mla_status eg_mla_decode_shared(const eg_mla_dims* dims, int32_t b
       dims, batch, q, latent_cache, token_id_cache, gate_table, w_uk, w_uv, prefix_len, prefix_table, max_prefix_pages,
       seq_lens, page_table, max_pages_per_seq, num_slots, workspace, workspace_bytes, out, &p);
   if (st != EG_MLA_OK || batch == 0) return st;
-  return egmla::run_decode_shared(*dims, p, batch, q, latent_cache, token_id_cache, gate_table, w_uk, w_uv, prefix_len,
-                                  prefix_table, max_prefix_pages, seq_lens, page_table, max_pages_per_seq, num_slots,
-                                  workspace, out, static_cast<hipStream_t>(stream));
+  return egmla::run_decode_shared({*dims, p, batch, q, latent_cache, token_id_cache, gate_table, w_uk, w_uv, prefix_len,
+                                   prefix_table, max_prefix_pages, seq_lens, page_table, max_pages_per_seq, num_slots,
+                                   static_cast<unsigned char*>(workspace), out, static_cast<hipStream_t>(stream)});
 }

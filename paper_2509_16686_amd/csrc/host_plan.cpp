@@ -662,13 +662,14 @@ namespace {
 
 // The split kernel of one part of a shared decode: the decode's plan without
 // its absorption, schedules and single-launch form (the call absorbs once for
-// both parts and merges them itself).
-eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages, DecodePlan* p) {
+// both parts and merges them itself).  The wide kernel, with its schedule,
+// stays where the tiled prefix kernel prepares both (`wide`).
+eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages, bool wide, DecodePlan* p) {
   const eg_mla_status st = make_decode_plan(d, batch, max_pages, nullptr, p);
   if (st != EG_MLA_OK) return st;
   p->fused_absorb = p->one_launch = p->tok_balanced = false;
   p->pieces = 0;
-  if (p->balanced) {
+  if (p->balanced && !wide) {
     p->balanced = false;
     p->heads_per_group = 16;
     p->head_groups = ceil_div(d.num_heads, 16);
@@ -688,26 +689,59 @@ eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
   return EG_MLA_OK;
 }
 
+// Query rows from which the prefix runs on the tiled kernel.
+constexpr int64_t kPrefixMinRows = 64;
+// Its work-groups: two per compute unit where their registers and tiles allow (d_c 128).
+int prefix_groups(const eg_mla_dims& d) { return d.latent_dim == 128 ? 512 : 256; }
+
+bool prefix_tiled(const eg_mla_dims& d, int64_t rows) {
+  return d.dtype == EG_MLA_BF16 && d.head_dim == 128 && d.v_head_dim == 128 && d.rope_dim == 64 &&
+         (d.latent_dim == 128 || d.latent_dim == 320 || d.latent_dim == 512) && rows >= kPrefixMinRows;
+}
+
 }  // namespace
 
 eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,
                                int32_t max_prefix_pages, SharedPlan* out) {
   SharedPlan p;
   // all heads of all sequences are the prefix's heads; merge grid
-  if (static_cast<int64_t>(batch) * d.num_heads > (1 << 30) || batch > 65535) return EG_MLA_ERR_UNSUPPORTED;
+  const int64_t rows64 = static_cast<int64_t>(batch) * d.num_heads;
+  if (rows64 > (1 << 30) || batch > 65535) return EG_MLA_ERR_UNSUPPORTED;
   eg_mla_dims all = d;
   all.num_heads = std::max(1, batch * d.num_heads);
-  eg_mla_status st = shared_part_plan(all, 1, max_prefix_pages, &p.pre);
-  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, max_pages_per_seq, &p.own);
+  eg_mla_status st = shared_part_plan(all, 1, max_prefix_pages, false, &p.pre);
+  p.tiled = p.pre.capacity > 0 && prefix_tiled(d, rows64);
+  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, max_pages_per_seq, p.tiled, &p.own);
   if (st != EG_MLA_OK) return st;
-  const size_t rows = static_cast<size_t>(batch) * d.num_heads;
-  size_t off = align_up(rows * static_cast<size_t>(d.latent_dim + d.rope_dim) * 4);
-  for (DecodePlan* s : {&p.pre, &p.own}) {
-    const size_t n = s->capacity > 0 ? rows * static_cast<size_t>(s->s_max) : 0;
-    s->off_ml = off;
-    off = align_up(off + n * 8);
-    s->off_o = off;
-    off = align_up(off + n * static_cast<size_t>(d.latent_dim) * 4);
+  const size_t rows = static_cast<size_t>(rows64), dc = static_cast<size_t>(d.latent_dim), dq = dc + d.rope_dim;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes);
+    return at;
+  };
+  if (p.tiled) {
+    const int tiles = ceil_div(p.pre.capacity, kPrefixKeys);
+    p.row_blocks = ceil_div(rows64, kPrefixRows);
+    p.splits = std::max(1, std::min(prefix_groups(d) / p.row_blocks, tiles));
+    if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x7fffffff) return EG_MLA_ERR_UNSUPPORTED;
+    p.off_half = take(rows * dq * 2);
+    if (!p.own.balanced) p.off_q = take(rows * dq * 4);
+    p.off_tiles = take(static_cast<size_t>(tiles) * kPrefixKeys * (prefix_latent_row(d.latent_dim) + 128));
+    p.pre.off_ml = take(rows * p.splits * 8);
+    p.pre.off_o = take(rows * p.splits * dc * 2);
+  } else {
+    p.off_q = take(rows * dq * 4);
+    const size_t n = p.pre.capacity > 0 ? rows * static_cast<size_t>(p.pre.s_max) : 0;
+    p.pre.off_ml = take(n * 8);
+    p.pre.off_o = take(n * dc * 4);
+  }
+  if (p.own.capacity > 0) {
+    const size_t n = p.own.balanced ? (static_cast<size_t>(kWideMaxGroups) + batch) * d.num_heads
+                                    : rows * static_cast<size_t>(p.own.s_max);
+    p.own.off_ml = take(n * 8);
+    p.own.off_o = take(n * dc * (p.own.balanced ? 2 : 4));
+    if (p.own.balanced) p.own.off_sched = take(16 + kWideMaxGroups * 8 + static_cast<size_t>(batch) * 8);
   }
   p.bytes = std::max<size_t>(off, kAlign);
   *out = p;
@@ -732,7 +766,8 @@ eg_mla_status validate_decode_shared(const eg_mla_dims* d, int32_t batch, const 
   if (max_pages_per_seq > 0 && !seq_lens) return EG_MLA_ERR_INVALID_ARG;
   if ((max_prefix_pages > 0 || max_pages_per_seq > 0) && (!latent_cache || !token_id_cache))
     return EG_MLA_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(latent_cache) || !aligned16(gate_table) || !aligned16(w_uk) || !aligned16(w_uv))
+  if (!aligned16(q) || !aligned16(latent_cache) || !aligned16(gate_table) || !aligned16(w_uk) || !aligned16(w_uv) ||
+      !aligned16(out))
     return EG_MLA_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < p->bytes) return EG_MLA_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;

@@ -189,10 +189,18 @@ eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const f
 
 // Decode with a shared prefix (decode_shared.h): `pre` is the decode of one
 // sequence of B H heads over the prefix, `own` that of the batch over its own
-// tokens; their off_ml and off_o are offsets into the call's one workspace.
+// tokens; their off_ml, off_o and off_sched are offsets into the call's one
+// workspace.
+constexpr int kPrefixKeys = 64;   // keys of a tile of the tiled prefix attention (shared_prefix.h)
+constexpr int kPrefixRows = 128;  // query rows of its work-groups
+constexpr int prefix_latent_row(int dc) { return (2 * dc + 255) / 256 * 256; }  // bytes of a key's latent in a tile
 struct SharedPlan {
   DecodePlan pre, own;
-  size_t off_q = 0;  // fp32 [B, H, d_c + d_r]
+  bool tiled = false;    // the prefix on the tiled kernel, in at most `splits` runs of tiles (pre: capacity and offsets)
+  int row_blocks = 0, splits = 0;
+  size_t off_q = 0;      // fp32 [B, H, d_c + d_r] (not tiled, or own tokens not on the wide kernel)
+  size_t off_half = 0;   // tiled: 16-bit [B, H, d_c + d_r]
+  size_t off_tiles = 0;  // tiled: the gated prefix
   size_t bytes = 0;
 };
 eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,

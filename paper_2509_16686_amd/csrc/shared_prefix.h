@@ -1,0 +1,517 @@
+// Attention of many query rows over one prefix on gfx950 MFMA (bf16 storage,
+// d_h = d_v = 128, d_r = 64, d_c 128, 320 or 512): the prefix part of the
+// shared decode.  Included by decode.hip.
+//
+// With all heads on one latent, the B H query rows of a batch attend to the
+// same keys [c~ | k^R] and values c~: a flash attention with d_c + d_r wide
+// keys and d_c wide values, bound by the matrix cores once a few hundred rows
+// share a key.  Three launches:
+//  1. shared_prep_kernel: the query absorption (16-bit rows [q_lat fp16 | q^R
+//     bf16], and fp32 ones where the own tokens' kernel wants them), the own
+//     tokens' schedule, and, once per prefix token, the gated latent (the exact
+//     fp32 product rounded to fp16) and the RoPE key (bf16), written as tiles of
+//     64 keys that are byte for byte what the attention holds in LDS: page
+//     table, gate and bank swizzle are dealt with once, and a tile is copied
+//     as one run of memory.
+//  2. shared_prefix_kernel: a work-group of 4 waves takes 128 query rows (32
+//     per wave, in registers) and a run of tiles.
+//  3. shared_merge_kernel (after the own tokens' split kernel): joins both
+//     parts' partial rows and applies W_UV.
+//
+// Attention kernel.  Tiles go straight from global memory into the other of
+// two LDS buffers while the current one is computed.  Scores
+// S^T[key][row] on v_mfma_f32_32x32x16 (A: 32 keys from LDS, B: the wave's 32
+// rows), online softmax per row in the log2 domain with lazy rescale, values
+// O^T[dim][row] += C~^T P^T with the probabilities as the B operand as they
+// lie in the score accumulators and transposed LDS reads as the A operand.
+// Each LDS byte read feeds 32 rows.  A partial row is O / l in fp16 (a convex
+// combination of fp16 values) with its maximum and sum in fp32.
+#pragma once
+
+namespace egmla {
+
+template <int DC>
+struct PrefixCfg {
+  static constexpr int KEYS = kPrefixKeys;
+  static constexpr int LROW = prefix_latent_row(DC);   // bytes per key: gated latent, padded to whole 256 bytes
+  static constexpr int RROW = 128;                     // RoPE key
+  static constexpr int ROPE = KEYS * LROW;             // its rows lie behind the latent rows
+  static constexpr int TILE = KEYS * (LROW + RROW);
+  static_assert(DC % 32 == 0 && TILE % 4096 == 0 && 2 * TILE <= 160 * 1024, "two tile buffers, copied by 4 waves");
+};
+constexpr int kPrefixThreads = 256;
+constexpr int kPrefixRsrcWord3 = 0x00020000;  // raw buffer resource: 32-bit data format, the record count in bytes
+static_assert(kPrefixRows == 32 * kPrefixThreads / 64, "32 rows per wave");
+
+// Byte of piece p (16 bytes: dims 8p ..) of a key's latent row, and of its
+// RoPE row: the low bits of the piece are swizzled by the key so that the 16
+// lanes of a 16-byte read cycle (keys) and the 32 lanes of a transposed 8-byte
+// read cycle hit distinct banks.
+__host__ __device__ __forceinline__ int prefix_latent_byte(int key, int p) {
+  return 256 * (p >> 4) + 16 * ((p & 15) ^ (((key & 3) << 2) | ((key >> 2) & 3)));
+}
+__host__ __device__ __forceinline__ int prefix_rope_byte(int key, int p) { return 16 * (p ^ ((key >> 1) & 7)); }
+
+constexpr int kPrepTokens = 32;   // tokens that a work-group gates at a time
+constexpr int kPrepGroups = 2048;  // work-groups that gate, at most
+
+struct PrefixPrepArgs {
+  const uint16_t* q;
+  const uint16_t* w_uk;
+  float* qfull;      // fp32 rows, where written
+  uint16_t* qhalf;   // 16-bit rows
+  const uint16_t* cache;
+  const int32_t* ids;
+  const uint16_t* gate;
+  const int32_t* len;
+  const int32_t* table;
+  unsigned char* tiles;
+  int64_t num_slots;
+  WideSchedArgs sched;  // G = 0: none
+  int32_t B, H, DC, V, P, cap;
+  int32_t gate_wgs, row_blocks;
+};
+
+template <AbsorbRows ROWS_OUT, int BLOCKS, int COLS>
+__global__ __launch_bounds__(256) void shared_prep_kernel(PrefixPrepArgs a) {
+  constexpr int DR = 64;
+  int wg = blockIdx.x;
+  if (wg == 0) {
+    if (a.sched.G > 0) wide_schedule<256>(a.sched, a.B);
+    return;
+  }
+  wg -= 1;
+  if (wg >= a.gate_wgs) {
+    wg -= a.gate_wgs;
+    const int h = wg % a.H, by = (wg / a.H) % a.row_blocks, bz = wg / (a.H * a.row_blocks);
+    absorb_tile<128, BLOCKS, COLS, ROWS_OUT>(a.q, a.w_uk, a.qfull, a.qhalf, a.B, a.H, a.DC, DR, h, by, bz);
+    return;
+  }
+  // pieces of the prefix's tokens, kPrepTokens tokens at a time; those behind the last token, up to the end of its
+  // tile, are zero
+  const int L = clamp_len(a.len[0], a.cap), end = (L + kPrefixKeys - 1) / kPrefixKeys * kPrefixKeys;
+  const int np = a.DC / 8 + DR / 8, lat = a.DC / 8;
+  const int lrow = prefix_latent_row(a.DC), tile_bytes = kPrefixKeys * (lrow + 128);
+  for (int base = wg * kPrepTokens; base < end; base += a.gate_wgs * kPrepTokens) {
+    for (int i = threadIdx.x; i < kPrepTokens * np; i += 256) {
+      const int t = base + i / np, p = i % np, key = t % kPrefixKeys;
+      unsigned char* dst = a.tiles + static_cast<int64_t>(t / kPrefixKeys) * tile_bytes +
+                           (p < lat ? key * lrow + prefix_latent_byte(key, p)
+                                    : kPrefixKeys * lrow + key * 128 + prefix_rope_byte(key, p - lat));
+      u32x4_t v = {0u, 0u, 0u, 0u};
+      if (t < L) {
+        const int64_t slot = paged_slot(a.table[t / a.P], t, a.P, a.num_slots);
+        v = *reinterpret_cast<const u32x4_t*>(a.cache + slot * (a.DC + DR) + 8 * p);
+        if (p < lat)
+          v = gate_chunk_f16(v, *reinterpret_cast<const u32x4_t*>(
+                                    a.gate + static_cast<int64_t>(clamp_id(a.ids[slot], a.V)) * a.DC + 8 * p));
+      }
+      *reinterpret_cast<u32x4_t*>(dst) = v;
+    }
+  }
+}
+
+// Tiles per split of a prefix of L tokens cut into at most s_max splits, and the splits that have any.
+__device__ __forceinline__ int prefix_per_split(int L, int s_max) {
+  const int tiles = (L + kPrefixKeys - 1) / kPrefixKeys;
+  return (tiles + s_max - 1) / s_max;
+}
+__device__ __forceinline__ int prefix_splits(int L, int s_max) {
+  const int tiles = (L + kPrefixKeys - 1) / kPrefixKeys, per = prefix_per_split(L, s_max);
+  return per ? (tiles + per - 1) / per : 0;
+}
+
+struct PrefixArgs {
+  const uint16_t* qhalf;       // [rows][DC + 64]: q_lat fp16 | q^R bf16
+  const unsigned char* tiles;  // PrefixCfg<DC>::TILE bytes each
+  const int32_t* len;
+  float* part_ml;              // [s_max][rows][2]
+  uint16_t* part_o;            // [s_max][rows][DC] fp16: O / l
+  int32_t cap, rows, row_blocks, s_max;
+  float scale_log2;
+};
+
+typedef __attribute__((ext_vector_type(16))) float px_f32x16_t;
+
+// Holds a block of accumulators in accumulation or ordinary registers at this point.
+__device__ __forceinline__ void in_agprs(px_f32x16_t& x) { asm volatile("" : "+a"(x)); }
+__device__ __forceinline__ void in_vgprs(px_f32x16_t& x) { asm volatile("" : "+v"(x)); }
+
+// Maximum and sum of lanes i and i ^ 32, the same value (same order) in both.
+__device__ __forceinline__ float half_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+template <int DC>
+__global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_prefix_kernel(PrefixArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host pass knows neither the copies to LDS nor the register constraints
+  using C = PrefixCfg<DC>;
+  constexpr int DQ = DC + 64, NC = DC / 16, NR = 4, KB = C::KEYS / 32, NDB = DC / 32;
+  __shared__ __attribute__((aligned(16))) unsigned char lds0[C::TILE];  // two tile buffers
+  __shared__ __attribute__((aligned(16))) unsigned char lds1[C::TILE];
+  // consecutive items (the row blocks of a split) share an XCD, whose L2 then serves the split's tiles
+  const int item = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int rb = item % a.row_blocks, split = item / a.row_blocks;
+  const int L = clamp_len(a.len[0], a.cap);
+  const int per = prefix_per_split(L, a.s_max);
+  const int t0 = split * per, t1 = min(t0 + per, (L + C::KEYS - 1) / C::KEYS);
+  if (t0 >= t1) return;
+
+  const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, R1 = (lane >> 4) & 1;
+  // this lane's query row; rows past the last repeat it and are not stored
+  const int row = rb * kPrefixRows + 32 * w + r32;
+  const int64_t qrow = static_cast<int64_t>(min(row, a.rows - 1)) * DQ + 8 * h;
+  f16x8_t qv[NC];   // q_lat
+  bf16x8_t qr[NR];  // q^R
+#pragma unroll
+  for (int c = 0; c < NC; ++c) qv[c] = *reinterpret_cast<const f16x8_t*>(a.qhalf + qrow + 16 * c);
+#pragma unroll
+  for (int c = 0; c < NR; ++c) qr[c] = *reinterpret_cast<const bf16x8_t*>(a.qhalf + qrow + DC + 16 * c);
+
+  auto lds_ptr = [](unsigned char* p) { return (__attribute__((address_space(3))) void*)p; };
+  auto issue_tile = [&](int tile, unsigned char* base) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<unsigned char*>(a.tiles) + static_cast<int64_t>(tile) * C::TILE, 0, C::TILE, kPrefixRsrcWord3);
+#pragma unroll
+    for (int j = 0; j < C::TILE / 4096; ++j) {
+      const int at = 1024 * (C::TILE / 4096 * w + j);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, lds_ptr(base + at), 16, 16 * lane, at, 0, 0);
+    }
+  };
+  // this wave's copies have landed; the barrier after it covers every wave's
+  auto tile_landed = []() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+
+  // per-lane LDS offsets (bytes within a tile buffer): score operands (key row r32 of a block of 32) ...
+  const int swz_l = ((r32 & 3) << 2) | ((r32 >> 2) & 3), swz_r = (r32 >> 1) & 7;
+  const int off_l = r32 * C::LROW, off_r = C::ROPE + r32 * C::RROW;
+  // ... and value operands (transposed reads): rows 16 m + 4 h + r16 / 4 (+ 8); operand row 16 R1 + 4 j + e is
+  // dim 16 R1 + 8 (j % 2) + 4 (j / 2) + e of a block of 32, so that an accumulator lane's outputs are adjacent dims
+  const int off_v = (4 * h + (r16 >> 2)) * C::LROW + 8 * ((r16 & 3) >> 1);
+  const int vlo = 2 * R1 + (r16 & 1);  // low 2 bits of the logical piece
+
+  px_f32x16_t o[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+  float m_run = -1e30f, l_run = 0.f;
+  // With d_c / 2 values a lane, the accumulators and the query fill the register file: the accumulators stay in the
+  // accumulation registers on every path (left to itself the compiler moves them through ordinary ones around the
+  // rescale, at each tile, and spills: 875 registers of d_c 512)
+  constexpr bool ACC = DC > 128;
+  auto hold = [&]() {
+    if constexpr (ACC) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) in_agprs(o[db]);
+    }
+  };
+
+  issue_tile(t0, lds0);
+  tile_landed();
+  __syncthreads();
+  // step i computes tile i from `tb` and copies tile i + 1 into `nb` (last read in step i - 1, which ended in a barrier)
+  auto step = [&](int i, const unsigned char* tb, unsigned char* nb) {
+    if (i + 1 < t1) issue_tile(i + 1, nb);
+    hold();
+    px_f32x16_t s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const f16x8_t av = *reinterpret_cast<const f16x8_t*>(tb + off_l + 32 * kb * C::LROW + 256 * (c >> 3) +
+                                                             16 * ((2 * (c & 7) + h) ^ swz_l));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, qv[c], s[kb], 0, 0, 0);
+      }
+#pragma unroll
+    for (int c = 0; c < NR; ++c)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const bf16x8_t av =
+            *reinterpret_cast<const bf16x8_t*>(tb + off_r + 32 * kb * C::RROW + 16 * ((2 * c + h) ^ swz_r));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qr[c], s[kb], 0, 0, 0);
+      }
+    // issue order: the A operands of a chunk one chunk ahead of its products
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * KB, 0);
+#pragma unroll
+    for (int c = 0; c < NC + NR - 1; ++c) {
+      __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
+    if ((i + 1) * C::KEYS > L) {  // the prefix ends inside this tile
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (i * C::KEYS + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3) >= L) s[kb][r] = -INFINITY;
+    }
+
+    // online softmax (row = lane % 32; keys split between lanes l and l ^ 32); the scale (tau log2 e > 0) commutes with
+    // the maximum and is applied inside the exponent
+    float mt = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[kb][r]);
+    mt = half_max(mt) * a.scale_log2;
+    const float m_new = fmaxf(m_run, mt);
+    const bool grow = m_new > m_run + kLazyRescale;
+    const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
+    m_run = grow ? m_new : m_run;
+    l_run *= alpha;
+    if (__builtin_amdgcn_ballot_w64(grow)) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        if constexpr (ACC) {  // one block at a time through ordinary registers
+          px_f32x16_t f = o[db];
+          in_vgprs(f);
+          f *= alpha;
+          in_agprs(f);
+          o[db] = f;
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          o[db] *= alpha;
+        }
+      }
+    }
+    hold();
+    f16x8_t pb[KB][2];  // [kb][16-key chunk m]: keys 16 m + 8 (e / 4) + 4 h + e % 4 of element e
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][8 * m + e], a.scale_log2, -m_run));
+          l_run += p[e];
+        }
+        pb[kb][m] = __builtin_bit_cast(f16x8_t, u32x4_t{pack_f16x2(p[0], p[1]), pack_f16x2(p[2], p[3]),
+                                                        pack_f16x2(p[4], p[5]), pack_f16x2(p[6], p[7])});
+      }
+
+    // values O^T[dim][row] += C~^T P^T
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const unsigned char* vp = tb + off_v + (32 * kb + 16 * m) * C::LROW;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          // logical piece 4 db + vlo; rows +0 and +8 swizzle with 4 (r16 / 4) + h and + 2
+          const int p0 = 256 * (db >> 2) + 16 * (4 * ((db & 3) ^ (r16 >> 2)) + (vlo ^ h));
+          const int p1 = 256 * (db >> 2) + 16 * (4 * ((db & 3) ^ (r16 >> 2)) + (vlo ^ (h + 2)));
+          const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(vp + p0));
+          const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4_t*)(vp + 8 * C::LROW + p1));
+          const f16x8_t av = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, pb[kb][m], o[db], 0, 0, 0);
+        }
+      }
+    tile_landed();
+    __syncthreads();
+  };
+  for (int i = t0; i < t1; i += 2) {
+    step(i, lds0, lds1);
+    if (i + 1 < t1) step(i + 1, lds1, lds0);
+  }
+
+  // O / l: lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row whose scores all
+  // overflowed to -inf weighs nothing
+  const float l = half_sum(l_run);
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  if (row < a.rows) {
+    const int64_t at = static_cast<int64_t>(split) * a.rows + row;
+    if (h == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(l > 0.f ? m_run : -INFINITY, l);
+    uint16_t* orow = a.part_o + at * DC + 8 * h;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<u32x4_t*>(orow + 32 * db + 16 * j) =
+            u32x4_t{pack_f16x2(o[db][8 * j] * inv, o[db][8 * j + 1] * inv),
+                    pack_f16x2(o[db][8 * j + 2] * inv, o[db][8 * j + 3] * inv),
+                    pack_f16x2(o[db][8 * j + 4] * inv, o[db][8 * j + 5] * inv),
+                    pack_f16x2(o[db][8 * j + 6] * inv, o[db][8 * j + 7] * inv)};
+  }
+#endif
+}
+
+// ---------------------------------------------------------------------------
+// Merge and up-projection: grid (H, ceil(B / spw)), 8 waves, one head and
+// spw = 1, 2, 4, 8 or 16 sequences per work-group.  DC / 8 lanes hold a row (8
+// dims each); with 4 rows to a wave (d_c 128) or one, each group of lanes is a
+// worker, and spw sequences share the work-group's workers in rounds.  A
+// worker folds every W-th partial row of its sequence (the prefix's, then its
+// own tokens') online in fp32, kSharedBatch rows loaded together; the workers
+// of a sequence meet in LDS, and the merged row o / l goes there once more as
+// bf16 hi + lo, the B operands of out^T[v][b] = W_UV[h] o^T on
+// v_mfma_f32_16x16x32_bf16.  Latency-bound: the rows' two round trips, the
+// exchanges, W_UV's rows (loaded at the start).
+// ---------------------------------------------------------------------------
+constexpr int kSharedMergeWaves = 8;
+constexpr int kSharedMergeSeq = 16;
+constexpr int kSharedBatch = 8;
+
+struct SharedMergeArgs {
+  const float* pre_ml;      // [s_max][B H][2]
+  const uint16_t* pre_o;    // [s_max][B H][DC] fp16, normalised
+  const int32_t* pre_len;   // null: no prefix
+  const float* own_ml;
+  const void* own_o;        // fp32 sums, [B][own_s_max][H][DC]; WIDE: fp16, normalised, rows of own_rows
+  const int32_t* own_lens;  // null: no own tokens
+  const int2* own_rows;     // WIDE
+  const uint16_t* w_uv;
+  uint16_t* out;
+  int32_t B, H, pre_cap, pre_s_max, own_cap, own_split, own_s_max, spw;
+};
+
+template <int DC, bool WIDE>
+__global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(SharedMergeArgs a) {
+  constexpr int DV = 128, NKC = DC / 32, OS = DC + 8;
+  constexpr int LPR = DC / 8, GPW = 64 / LPR;       // lanes per row, rows (workers) per wave
+  constexpr int WORKERS = kSharedMergeWaves * GPW;
+  __shared__ __attribute__((aligned(16))) uint16_t o_s[2][kSharedMergeSeq][OS];  // merged rows, hi and lo
+  __shared__ __attribute__((aligned(16))) float part[WORKERS][DC];
+  __shared__ float m_part[WORKERS], l_part[WORKERS];
+  const int h = blockIdx.x, b0 = blockIdx.y * a.spw;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int nseq = min(a.spw, a.B - b0);
+  // W_UV rows 16 w + r16 (columns 32 kc + 8 g ..) of this wave's output tile
+  u32x4_t wa[NKC];
+  auto load_w = [&]() {
+    const uint16_t* wrow = a.w_uv + (static_cast<int64_t>(h) * DV + 16 * w + r16) * DC + 8 * g;
+#pragma unroll
+    for (int kc = 0; kc < NKC; ++kc) wa[kc] = *reinterpret_cast<const u32x4_t*>(wrow + 32 * kc);
+  };
+  if constexpr (DC <= 128) load_w();
+
+  const int pre_n = a.pre_len ? prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max) : 0;
+  const int wps = max(1, WORKERS / a.spw);  // workers per sequence (spw <= WORKERS where GPW > 1, else rounds)
+  const int spr = WORKERS / wps;            // sequences per round
+  const int worker = w * GPW + (GPW > 1 ? lane / LPR : 0);
+  const bool live = GPW > 1 || lane < LPR;  // lanes without a piece of a row
+  const int col = 8 * (lane % LPR);
+  for (int r0 = 0; r0 < a.spw; r0 += spr) {
+    const int k = r0 + worker / wps, me = worker % wps;
+    const int b = b0 + k;
+    float M = -INFINITY, sum = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // rows me, me + wps, ... < n of a part; load(i, ml, v) reads row i
+    auto fold = [&](int n, bool normalised, auto load) {
+      for (int i0 = me; i0 < n; i0 += wps * kSharedBatch) {
+        float2 ml[kSharedBatch];
+        float v[kSharedBatch][8];
+#pragma unroll
+        for (int u = 0; u < kSharedBatch; ++u) load(min(i0 + u * wps, n - 1), ml[u], v[u]);
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < kSharedBatch; ++u) top = fmaxf(top, ml[u].x);  // repeats change no maximum
+        const bool any = top > -INFINITY;  // rows without weight have maximum -inf
+        const float keep = any ? __builtin_amdgcn_exp2f(M - top) : 1.f;
+        sum *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= keep;
+#pragma unroll
+        for (int u = 0; u < kSharedBatch; ++u) {
+          const float x = any && i0 + u * wps < n ? __builtin_amdgcn_exp2f(ml[u].x - top) : 0.f;
+          sum = fmaf(x, ml[u].y, sum);
+          const float y = normalised ? x * ml[u].y : x;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] = fmaf(y, v[u][e], acc[e]);
+        }
+        M = top;
+      }
+    };
+    auto half_row = [&](const uint16_t* p, float (&v)[8]) {
+      const f16x8_t x = *reinterpret_cast<const f16x8_t*>(p + col);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
+    };
+    if (live && k < nseq) {
+      const int64_t rows = static_cast<int64_t>(a.B) * a.H, qrow = static_cast<int64_t>(b) * a.H + h;
+      fold(pre_n, true, [&](int i, float2& ml, float (&v)[8]) {
+        const int64_t at = i * rows + qrow;
+        ml = *reinterpret_cast<const float2*>(a.pre_ml + 2 * at);
+        half_row(a.pre_o + at * DC, v);
+      });
+      if (a.own_lens) {
+        if constexpr (WIDE) {
+          const int2 list = a.own_rows[b];
+          fold(list.y, true, [&](int i, float2& ml, float (&v)[8]) {
+            const int64_t at = static_cast<int64_t>(list.x + i) * a.H + h;
+            ml = *reinterpret_cast<const float2*>(a.own_ml + 2 * at);
+            half_row(static_cast<const uint16_t*>(a.own_o) + at * DC, v);
+          });
+        } else {
+          const int L = clamp_len(a.own_lens[b], a.own_cap);
+          fold(min((L + a.own_split - 1) / a.own_split, a.own_s_max), false, [&](int i, float2& ml, float (&v)[8]) {
+            const int64_t at = (static_cast<int64_t>(b) * a.own_s_max + i) * a.H + h;
+            ml = *reinterpret_cast<const float2*>(a.own_ml + 2 * at);
+            const f32x4_t* p = reinterpret_cast<const f32x4_t*>(static_cast<const float*>(a.own_o) + at * DC + col);
+            const f32x4_t x = p[0], y = p[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = x[e];
+              v[4 + e] = y[e];
+            }
+          });
+        }
+      }
+    }
+    if (r0 > 0) __syncthreads();  // the round before has been read
+    if (live) {
+      *reinterpret_cast<f32x4_t*>(&part[worker][col]) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
+      *reinterpret_cast<f32x4_t*>(&part[worker][col + 4]) = f32x4_t{acc[4], acc[5], acc[6], acc[7]};
+      if (lane % LPR == 0) {
+        m_part[worker] = M;
+        l_part[worker] = sum;
+      }
+    }
+    __syncthreads();
+    // merged rows of the round's sequences (zero without tokens and past the batch)
+    for (int i = tid; i < spr * DC; i += kSharedMergeWaves * 64) {
+      const int kk = i / DC, c = i - kk * DC;
+      float top = -INFINITY, num = 0.f, den = 0.f;
+      for (int p = 0; p < wps; ++p) top = fmaxf(top, m_part[kk * wps + p]);
+      if (top > -INFINITY)
+        for (int p = 0; p < wps; ++p) {
+          const float x = __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top);
+          num = fmaf(x, part[kk * wps + p][c], num);
+          den = fmaf(x, l_part[kk * wps + p], den);
+        }
+      const float v = top > -INFINITY ? num / den : 0.f;
+      const __bf16 hi = static_cast<__bf16>(v);
+      o_s[0][r0 + kk][c] = __builtin_bit_cast(uint16_t, hi);
+      o_s[1][r0 + kk][c] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - static_cast<float>(hi)));
+    }
+  }
+  __syncthreads();
+  if constexpr (DC > 128) load_w();
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  const int rr = min(r16, a.spw - 1);  // columns past spw repeat the last and are not stored
+#pragma unroll
+  for (int kc = 0; kc < NKC; ++kc) {
+    const bf16x8_t av = __builtin_bit_cast(bf16x8_t, wa[kc]);
+    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[0][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[1][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+  }
+  // lane: rows 16 w + 4 g + 0..3 of sequence b0 + r16
+  if (r16 < nseq)
+    *reinterpret_cast<u32x2_t*>(a.out + (static_cast<int64_t>(b0 + r16) * a.H + h) * DV + 16 * w + 4 * g) =
+        u32x2_t{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+}
+
+}  // namespace egmla

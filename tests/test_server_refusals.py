@@ -102,7 +102,7 @@ SHARED = dict(dims=None, batch=4, q=at(0), cache=at(1), ids=at(2), gate=at(3), w
     (dict(gate=None), ARG), (dict(w_uk=None), ARG), (dict(w_uv=None), ARG), (dict(prefix_len=None), ARG),
     (dict(prefix_table=None), ARG), (dict(lens=None), ARG), (dict(out=None), ARG), (dict(ws=None), WS), (dict(ws_bytes=255), WS),
     (dict(ws=at(10, 16)), WS), (dict(q=at(0, 8)), ARG), (dict(cache=at(1, 8)), ARG), (dict(gate=at(3, 8)), ARG),
-    (dict(w_uk=at(4, 8)), ARG), (dict(w_uv=at(5, 8)), ARG),
+    (dict(w_uk=at(4, 8)), ARG), (dict(w_uv=at(5, 8)), ARG), (dict(out=at(11, 8)), ARG),
     (dict(table=None, num_slots=4 * 8 * 64 - 1), ARG),   # contiguous rows that the cache does not hold
 ])
 def test_decode_shared(change, expect):
