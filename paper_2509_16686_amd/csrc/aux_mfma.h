@@ -33,8 +33,9 @@ constexpr int kAbsMinWorkGroups = 128;
 
 // Rows written: fp32 [B, H, DC + DR], or 16-bit [B, H, DC + DR] = [q_lat in
 // fp16 (one rounding) | q^R in bf16 (copied)], the operands of fp16 latent
-// products and exact bf16 RoPE products, or both.
-enum class AbsorbRows { kFloat, kHalf, kBoth };
+// products and exact bf16 RoPE products, or both; or the page scores' operands
+// (three bf16 parts of q_lat, PartsLayout).
+enum class AbsorbRows { kFloat, kHalf, kBoth, kParts };
 
 // Tile (h, by, bz) of the absorption: head h, row block by, column slice bz.
 template <int DH, int BLOCKS, int COLS, AbsorbRows ROWS_OUT>
@@ -42,7 +43,9 @@ __device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, cons
                                             float* __restrict__ qfull, uint16_t* __restrict__ qhalf, int B, int H,
                                             int DC, int DR, int h, int by, int bz) {
   static_assert(BLOCKS >= 1 && BLOCKS <= kAbsBlocks, "row blocks per work-group");
-  constexpr bool FLOAT = ROWS_OUT != AbsorbRows::kHalf, HALF = ROWS_OUT != AbsorbRows::kFloat;
+  constexpr bool PARTS = ROWS_OUT == AbsorbRows::kParts;
+  constexpr bool FLOAT = ROWS_OUT == AbsorbRows::kFloat || ROWS_OUT == AbsorbRows::kBoth;
+  constexpr bool HALF = ROWS_OUT == AbsorbRows::kHalf || ROWS_OUT == AbsorbRows::kBoth;
   static_assert(COLS % 16 == 0 && COLS <= 128, "latent columns per work-group");
   constexpr int RS = COLS + 8;  // padded LDS row (bf16 elements)
   constexpr int NK = DH / 32;
@@ -127,6 +130,16 @@ __device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, cons
           if constexpr (HALF)
             reinterpret_cast<_Float16*>(qhalf)[(static_cast<int64_t>(b) * H + h) * DQ + c] =
                 static_cast<_Float16>(acc[rb][r]);
+          if constexpr (PARTS) {
+            const PartsLayout at(H, DC, DR);
+            const float x = acc[rb][r];
+            const uint16_t p0 = f32_to_bf16(x);
+            const float left = x - bf16_to_f32(p0);  // exact
+            const uint16_t p1 = f32_to_bf16(left);
+            qhalf[at(b, h, 0, c)] = p0;
+            qhalf[at(b, h, 1, c)] = p1;
+            qhalf[at(b, h, 2, c)] = f32_to_bf16(left - bf16_to_f32(p1));
+          }
           if constexpr (FLOAT) qfull[(static_cast<int64_t>(b) * H + h) * DQ + c] = acc[rb][r];
         }
       }
@@ -137,6 +150,7 @@ __device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, cons
     for (int rb = 0; rb < BLOCKS; ++rb) {
       const int b = b0 + rb * kAbsRows + rq_row;
       if (rq_row < kAbsRows && b < B) {
+        if constexpr (PARTS) *reinterpret_cast<uint2*>(qhalf + PartsLayout(H, DC, DR)(b, h, 0, DC + rq_col)) = rq[rb];
         if constexpr (HALF)
           *reinterpret_cast<uint2*>(qhalf + (static_cast<int64_t>(b) * H + h) * DQ + DC + rq_col) = rq[rb];
         if constexpr (FLOAT)
@@ -149,6 +163,7 @@ __device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, cons
       const int bb = i / DR, r = i % DR;
       if (b0 + bb < B) {
         const uint16_t v = q[(static_cast<int64_t>(b0 + bb) * H + h) * DQin + DH + r];
+        if constexpr (PARTS) qhalf[PartsLayout(H, DC, DR)(b0 + bb, h, 0, DC + r)] = v;
         if constexpr (HALF) qhalf[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r] = v;
         if constexpr (FLOAT)
           qfull[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r] = bf16_to_f32(v);
@@ -174,6 +189,15 @@ __global__ __launch_bounds__(256) void absorb_mfma_kernel(const uint16_t* __rest
   }
   absorb_tile<DH, BLOCKS, COLS, HALF ? AbsorbRows::kHalf : AbsorbRows::kFloat>(
       q, w_uk, qfull, reinterpret_cast<uint16_t*>(qfull), B, H, DC, DR, blockIdx.x, blockIdx.y, blockIdx.z);
+}
+
+// The absorbed query in three bf16 parts (page scores).
+template <int DH, int BLOCKS, int COLS>
+__global__ __launch_bounds__(256) void absorb_parts_kernel(const uint16_t* __restrict__ q,
+                                                           const uint16_t* __restrict__ w_uk,
+                                                           uint16_t* __restrict__ parts, int B, int H, int DC, int DR) {
+  absorb_tile<DH, BLOCKS, COLS, AbsorbRows::kParts>(q, w_uk, nullptr, parts, B, H, DC, DR, blockIdx.x, blockIdx.y,
+                                                    blockIdx.z);
 }
 
 // ---------------------------------------------------------------------------

@@ -602,6 +602,19 @@ hipError_t launch_absorb_sched(const eg_mla_dims& d, const DecodePlan& p, int32_
 
 }  // namespace
 
+hipError_t launch_absorb_parts(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, uint16_t* parts,
+                               hipStream_t stream) {
+  const AbsorbGrid ag = absorb_grid(d, batch, false);
+  auto kern = d.head_dim == 64 ? (ag.narrow ? absorb_parts_kernel<64, 1, kAbsColsNarrow>
+                                            : absorb_parts_kernel<64, 1, kAbsCols>)
+              : ag.grouped ? absorb_parts_kernel<128, kAbsBlocks, kAbsCols>
+              : ag.narrow  ? absorb_parts_kernel<128, 1, kAbsColsNarrow>
+                           : absorb_parts_kernel<128, 1, kAbsCols>;
+  hipLaunchKernelGGL(kern, ag.grid, dim3(256), 0, stream, static_cast<const uint16_t*>(q),
+                     static_cast<const uint16_t*>(w_uk), parts, batch, d.num_heads, d.latent_dim, d.rope_dim);
+  return hipGetLastError();
+}
+
 hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* qfull,
                          hipStream_t stream) {
   const bool bf = d.dtype == EG_MLA_BF16;

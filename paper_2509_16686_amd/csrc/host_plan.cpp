@@ -600,10 +600,15 @@ eg_mla_status validate_qk(const eg_mla_dims* d, int32_t n_tokens, const void* q,
   return EG_MLA_OK;
 }
 
+bool page_scores_mfma(const eg_mla_dims& d) {
+  return d.dtype == EG_MLA_BF16 && (d.head_dim == 64 || d.head_dim == 128);
+}
+
 size_t page_scores_workspace_bytes(const eg_mla_dims& d, int32_t batch) {
-  return std::max<size_t>(align_up(static_cast<size_t>(std::max(batch, 0)) * d.num_heads *
-                                   static_cast<size_t>(d.latent_dim + d.rope_dim) * sizeof(float)),
-                          kAlign);
+  const size_t n = static_cast<size_t>(std::max(batch, 0)), dq = static_cast<size_t>(d.latent_dim + d.rope_dim);
+  const size_t runs = static_cast<size_t>(ceil_div(d.latent_dim + d.rope_dim, 32) + 2 * ceil_div(d.latent_dim, 32));
+  const size_t bytes = page_scores_mfma(d) ? n * ceil_div(d.num_heads, 16) * runs * 1024 : n * d.num_heads * dq * 4;
+  return std::max<size_t>(align_up(bytes), kAlign);
 }
 
 eg_mla_status validate_page_means(const eg_mla_dims* d, int32_t batch, const void* latent_cache,

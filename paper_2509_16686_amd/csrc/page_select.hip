@@ -27,11 +27,14 @@ namespace egmla {
 // there and a sum of up to 2^20 of them is off by far less than the last bit
 // of its rounding, so that a mean does not depend on the order of its tokens
 // (a page whose means are formed again from the same rows keeps its bits).
-// Bound by the latency of length, table entry, id and row for a step's pages,
-// by HBM for a prompt's.
+// Bound by the latency of length, table entry, id, row and gate row for a
+// step's pages (so a page's ids load together, and kMeanBatch rows of a thread
+// at a time: 8 sequences of the 128-head layer, 2 or 3 pages each, 22 us with
+// one row after the other), by HBM for a prompt's.
 // ---------------------------------------------------------------------------
-constexpr int kMeanThreads = 256;
-constexpr int kMeanGroups = 1024;  // work-groups, about: four per compute unit
+constexpr int kMeanThreads = 512;
+constexpr int kMeanGroups = 1024;  // work-groups, about
+constexpr int kMeanBatch = 4;
 
 struct MeansArgs {
   const void* cache;
@@ -65,6 +68,7 @@ template <bool BF16>
 __global__ __launch_bounds__(kMeanThreads) void page_means_kernel(MeansArgs a) {
   constexpr int N = BF16 ? 8 : 4;
   __shared__ double red[kMeanThreads * N];
+  __shared__ int32_t id_s[kMeanThreads];
   const int b = blockIdx.x;
   const int DQ = a.DC + a.DR, np = DQ / N;  // np <= 160 pieces
   const int rows = kMeanThreads / np;
@@ -73,6 +77,7 @@ __global__ __launch_bounds__(kMeanThreads) void page_means_kernel(MeansArgs a) {
   const int first = a.first ? max(a.first[b], 0) : 0;
   if (first >= L) return;
   const int64_t npages = a.num_slots / a.P;
+  const bool gated = c * N < a.DC, adds = r < rows;
   for (int pg = first / a.P + blockIdx.y; static_cast<int64_t>(pg) * a.P < L; pg += gridDim.y) {
     const int n = min(a.P, L - pg * a.P);
     const int64_t page = a.table ? a.table[static_cast<int64_t>(b) * a.W + pg] : static_cast<int64_t>(b) * a.W + pg;
@@ -80,21 +85,33 @@ __global__ __launch_bounds__(kMeanThreads) void page_means_kernel(MeansArgs a) {
     double acc[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.0;
-    if (r < rows) {
-      for (int i = r; i < n; i += rows) {
-        const int64_t slot = page * a.P + i;
-        float x[N];
-        load_piece<BF16>(a.cache, slot * DQ + c * N, x);
-        if (c * N < a.DC) {
-          float g[N];
-          load_piece<BF16>(a.gate, static_cast<int64_t>(clamp_id(a.ids[slot], a.V)) * a.DC + c * N, g);
+    for (int base = 0; base < n; base += kMeanThreads) {  // the ids of up to kMeanThreads tokens at a time
+      const int64_t slot0 = page * a.P + base;
+      const int m = min(n - base, kMeanThreads);
+      const int id = a.ids[slot0 + min(tid, m - 1)];
+      for (int i0 = r, round = 0; round * rows * kMeanBatch < m; ++round, i0 += rows * kMeanBatch) {
+        float x[kMeanBatch][N], g[kMeanBatch][N];
 #pragma unroll
-          for (int e = 0; e < N; ++e) acc[e] += static_cast<double>(x[e]) * static_cast<double>(g[e]);
-        } else {
+        for (int u = 0; u < kMeanBatch; ++u)  // rows past the last repeat it and are not added
+          load_piece<BF16>(a.cache, (slot0 + min(i0 + u * rows, m - 1)) * DQ + c * N, x[u]);
+        if (round == 0) {
+          id_s[tid] = clamp_id(id, a.V);
+          __syncthreads();
+        }
+        if (gated) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) acc[e] += static_cast<double>(x[e]);
+          for (int u = 0; u < kMeanBatch; ++u)
+            load_piece<BF16>(a.gate, static_cast<int64_t>(id_s[min(i0 + u * rows, m - 1)]) * a.DC + c * N, g[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kMeanBatch; ++u) {
+          if (!adds || i0 + u * rows >= m) continue;
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            acc[e] += gated ? static_cast<double>(x[u][e]) * static_cast<double>(g[u][e]) : static_cast<double>(x[u][e]);
         }
       }
+      __syncthreads();  // the ids have been read
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) red[e * kMeanThreads + tid] = acc[e];
@@ -152,6 +169,169 @@ __global__ __launch_bounds__(256) void page_scores_kernel(ScoreArgs a) {
       }
     }
     if (lane == 0) a.scores[static_cast<int64_t>(b) * a.W + j] = best;
+  }
+}
+
+// Matrix cores, bf16 storage: S[head][page] on v_mfma_f32_16x16x32_bf16, 16
+// heads (A: the query's parts) by 16 pages (B: their means), both operands
+// straight from global memory.  The products of bf16 values are exact and the
+// three parts hold all of the fp32 query, so the scores are fp32 ones.  HW
+// waves share a tile of TPW x 16 pages, each with every HW-th block of 16
+// heads, and join their maxima in LDS; the other 8 / HW take the next tiles.
+// Bound by latency for few heads, and by the query's parts through L2 for many
+// (6 d_c + 2 d_r bytes a head, read once per tile of pages).
+constexpr int kScoreWaves = 8;
+
+constexpr int kScoreBatch = 4;
+
+struct ScoreMfmaArgs {
+  const uint16_t* parts;  // PartsLayout
+  const uint16_t* means;
+  ScoreArgs s;
+  int32_t B, DC, groups;  // work-groups per sequence
+};
+
+// NC > 0: d_c = 32 NC and d_r = 64; 0: any.
+template <int HW, int TPW, int NC>
+__global__ __launch_bounds__(kScoreWaves * 64) void page_scores_mfma_kernel(ScoreMfmaArgs a) {
+  __shared__ float best_s[kScoreWaves][TPW * 16];
+  constexpr int PW = kScoreWaves / HW;
+  // means that several waves take lie in LDS, rows padded by 16 bytes (the 16 rows of an operand read on distinct banks)
+  constexpr bool STAGE = HW > 1 && NC > 0;
+  constexpr int MROW = 32 * NC + 64 + 8;
+  __shared__ __attribute__((aligned(16))) uint16_t mean_s[STAGE ? PW * TPW * 16 * MROW : 8];
+  const int item = xcd_logical_block(blockIdx.x, gridDim.x);  // a sequence's work-groups share its query in an XCD's L2
+  const int b = item / a.groups, lane = threadIdx.x & 63, w = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+  const int DC = NC ? 32 * NC : a.DC, DQ = NC ? DC + 64 : a.s.DQ, H = a.s.H;
+  const int pages = (clamp_len(a.s.lens[b], a.s.cap) + a.s.P - 1) / a.s.P;
+  const int p0 = ((item - b * a.groups) * PW + w / HW) * TPW * 16;  // this wave's first page
+  float best[TPW];
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) best[t] = -INFINITY;
+  if constexpr (STAGE) {
+    constexpr int PIECES = 4 * NC + 8, ALL = PW * TPW * 16 * PIECES, THREADS = kScoreWaves * 64;
+    constexpr int PER = (ALL + THREADS - 1) / THREADS;
+    const int wg0 = (item - b * a.groups) * PW * TPW * 16;
+    if (wg0 < pages) {
+      u32x4_t v[PER];
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {  // rows past the last page repeat it
+        const int i = min(static_cast<int>(threadIdx.x) + k * THREADS, ALL - 1), row = i / PIECES, c = i % PIECES;
+        v[k] = *reinterpret_cast<const u32x4_t*>(a.means + score_page(a.s, b, min(wg0 + row, pages - 1)) * DQ + 8 * c);
+      }
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const int i = threadIdx.x + k * THREADS, row = i / PIECES, c = i % PIECES;
+        if (i < ALL) *reinterpret_cast<u32x4_t*>(mean_s + row * MROW + 8 * c) = v[k];
+      }
+    }
+    __syncthreads();
+  }
+  if (p0 < pages) {
+    const uint16_t* mrow[TPW];  // columns past the last page repeat it
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+      if constexpr (STAGE) mrow[t] = mean_s + (w / HW * TPW * 16 + 16 * t + r16) * MROW + 8 * g;
+      else mrow[t] = a.means + score_page(a.s, b, min(p0 + 16 * t + r16, pages - 1)) * DQ + 8 * g;
+    }
+    const PartsLayout layout(H, DC, DQ - DC);
+    for (int h0 = 16 * (w % HW); h0 < H; h0 += 16 * HW) {
+      // A operand of 32 values: this lane's 16 bytes of a run
+      const uint16_t* q0 = a.parts + layout(b, h0, 0, 0) + 8 * lane;
+      const uint16_t* q1 = a.parts + layout(b, h0, 1, 0) + 8 * lane;
+      const uint16_t* q2 = a.parts + layout(b, h0, 2, 0) + 8 * lane;
+      f32x4_t acc[TPW];
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const u32x4_t zero = {0u, 0u, 0u, 0u};
+      // values k + 8g .. of a mean's row, and of the query's part; zeros past the row's end
+      auto mean = [&](const uint16_t* p, int k) {
+        return __builtin_bit_cast(bf16x8_t, NC || k + 8 * g < DQ ? *reinterpret_cast<const u32x4_t*>(p + k) : zero);
+      };
+      auto query = [&](const uint16_t* p, int k, int end) {
+        return __builtin_bit_cast(bf16x8_t, NC || k + 8 * g < end ? *reinterpret_cast<const u32x4_t*>(p + 16 * k) : zero);
+      };
+      if constexpr (NC > 0) {
+        // batches of kScoreBatch runs, the next one's loads in flight while one is multiplied; the RoPE runs (the
+        // first part holds all of q^R) go out first and are multiplied last
+        constexpr int NB = (NC + kScoreBatch - 1) / kScoreBatch;
+        bf16x8_t xr[2], mr[2][TPW], x[2][kScoreBatch][3], m[2][kScoreBatch][TPW];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          xr[c] = query(q0, 32 * (NC + c), DQ);
+#pragma unroll
+          for (int t = 0; t < TPW; ++t) mr[c][t] = mean(mrow[t], 32 * (NC + c));
+        }
+        auto load = [&](int n) {
+#pragma unroll
+          for (int j = 0; j < kScoreBatch; ++j) {
+            const int c = n * kScoreBatch + j;
+            if (c >= NC) continue;
+            x[n & 1][j][0] = query(q0, 32 * c, DQ);
+            x[n & 1][j][1] = query(q1, 32 * c, DC);
+            x[n & 1][j][2] = query(q2, 32 * c, DC);
+#pragma unroll
+            for (int t = 0; t < TPW; ++t) m[n & 1][j][t] = mean(mrow[t], 32 * c);
+          }
+        };
+        load(0);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          if (n + 1 < NB) load(n + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < kScoreBatch; ++j) {
+            if (n * kScoreBatch + j >= NC) continue;
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+#pragma unroll
+              for (int t = 0; t < TPW; ++t)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[n & 1][j][i], m[n & 1][j][t], acc[t], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int t = 0; t < TPW; ++t)
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xr[c], mr[c][t], acc[t], 0, 0, 0);
+      } else {
+        for (int k = 0; k < DQ; k += 32) {
+          bf16x8_t m[TPW];
+#pragma unroll
+          for (int t = 0; t < TPW; ++t) m[t] = mean(mrow[t], k);
+          const bf16x8_t x[3] = {query(q0, k, DQ), query(q1, k, DC), query(q2, k, DC)};
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+#pragma unroll
+            for (int t = 0; t < TPW; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], m[t], acc[t], 0, 0, 0);
+        }
+      }
+      // lane: heads h0 + 4 g + 0..3 of page r16
+#pragma unroll
+      for (int t = 0; t < TPW; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (h0 + 4 * g + r < H) best[t] = fmaxf(best[t], acc[t][r]);
+    }
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) best[t] = max_over_row_groups(best[t]) * a.s.scale;
+  }
+  if constexpr (HW > 1) {
+    if (g == 0) {
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) best_s[w][16 * t + r16] = best[t];
+    }
+    __syncthreads();
+    if (w % HW) return;
+#pragma unroll
+    for (int t = 0; t < TPW; ++t)
+      for (int k = 1; k < HW; ++k) best[t] = fmaxf(best[t], best_s[w + k][16 * t + r16]);
+  }
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) {
+    const int j = p0 + 16 * t + r16;
+    if (g == 0 && j < a.s.W) a.s.scores[static_cast<int64_t>(b) * a.s.W + j] = j < pages ? best[t] : -INFINITY;
   }
 }
 
@@ -277,6 +457,28 @@ __global__ __launch_bounds__(kSelThreads) void select_pages_kernel(SelectArgs a)
 
 using namespace egmla;
 
+namespace {
+
+// The instance of a layer's width for HW waves along the heads and TPW tiles of 16 pages a wave.
+template <int HW, int TPW>
+hipError_t launch_scores(const eg_mla_dims& d, int32_t batch, const uint16_t* parts, const ScoreArgs& a,
+                         hipStream_t stream) {
+  constexpr int per = kScoreWaves / HW * TPW * 16;  // pages of a work-group
+  const int groups = (a.W + per - 1) / per;
+  if (static_cast<int64_t>(batch) * groups > 0x7fffffff) return hipErrorInvalidValue;
+  const ScoreMfmaArgs m{parts, static_cast<const uint16_t*>(a.means), a, batch, d.latent_dim, groups};
+  auto kern = d.rope_dim != 64        ? page_scores_mfma_kernel<HW, TPW, 0>
+              : d.latent_dim == 64    ? page_scores_mfma_kernel<HW, TPW, 2>
+              : d.latent_dim == 128   ? page_scores_mfma_kernel<HW, TPW, 4>
+              : d.latent_dim == 320   ? page_scores_mfma_kernel<HW, TPW, 10>
+              : d.latent_dim == 512   ? page_scores_mfma_kernel<HW, TPW, 16>
+                                      : page_scores_mfma_kernel<HW, TPW, 0>;
+  hipLaunchKernelGGL(kern, dim3(batch * groups), dim3(kScoreWaves * 64), 0, stream, m);
+  return hipGetLastError();
+}
+
+}  // namespace
+
 extern "C" eg_mla_status eg_mla_page_means(const eg_mla_dims* dims, int32_t batch, const void* latent_cache,
                                            const int32_t* token_id_cache, const void* gate_table,
                                            const int32_t* first_tokens, const int32_t* seq_lens,
@@ -311,10 +513,19 @@ extern "C" eg_mla_status eg_mla_page_scores(const eg_mla_dims* dims, int32_t bat
   const eg_mla_dims& d = *dims;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   (void)hipGetLastError();
-  if (launch_absorb(d, batch, q, w_uk, static_cast<float*>(workspace), stream) != hipSuccess) return EG_MLA_ERR_HIP;
   ScoreArgs a{static_cast<const float*>(workspace), page_means, seq_lens, page_table, scores, num_slots, d.num_heads,
               d.latent_dim + d.rope_dim, d.page_size, max_pages_per_seq, max_pages_per_seq * d.page_size,
               softmax_scale(d)};
+  if (page_scores_mfma(d)) {
+    uint16_t* parts = static_cast<uint16_t*>(workspace);
+    if (launch_absorb_parts(d, batch, q, w_uk, parts, stream) != hipSuccess) return EG_MLA_ERR_HIP;
+    const int blocks = (d.num_heads + 15) / 16;
+    const hipError_t e = blocks == 1 ? launch_scores<1, 1>(d, batch, parts, a, stream)
+                         : blocks <= 4 ? launch_scores<4, 1>(d, batch, parts, a, stream)
+                                       : launch_scores<8, 2>(d, batch, parts, a, stream);
+    return e == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
+  }
+  if (launch_absorb(d, batch, q, w_uk, static_cast<float*>(workspace), stream) != hipSuccess) return EG_MLA_ERR_HIP;
   const dim3 grid(batch, std::min((max_pages_per_seq + 3) / 4, std::max(1, 2048 / batch)));
   if (d.dtype == EG_MLA_BF16) hipLaunchKernelGGL(page_scores_kernel<true>, grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL(page_scores_kernel<false>, grid, dim3(256), 0, stream, a);

@@ -120,8 +120,8 @@ class Layer:
 
     def rows(self, pages, n):
         """[c (.) G[id] | k^R] of the first n tokens of a list of pages."""
-        at = np.asarray([int(p) * self.page + o for p in pages for o in range(self.page)], dtype=np.int64)[:n]
-        x = self.f64(self.cache)[at]
+        at = (np.asarray([int(p) for p in pages], dtype=np.int64)[:, None] * self.page + np.arange(self.page)).reshape(-1)[:n]
+        x = self.f64(self.cache[torch.from_numpy(at).cuda()])
         ids = self.ids.cpu().numpy()[at].clip(0, self.gate.shape[0] - 1)
         x[:, : self.dc] *= self.f64(self.gate)[ids]
         return x
