@@ -149,7 +149,10 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        try:  # the handle alone: 0.3 us instead of 2.8 for a Stream object
+            return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        except AttributeError:
+            return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -322,9 +325,9 @@ def page_plan(page_size: int, cached_lens, new_lens, page_table, free_pages, fre
             ("free_count", free_count, i, (1,)), ("seq_lens", seq_lens, i, (b,)), ("cu_seqlens", cu_seqlens, i, (b + 1,)),
             ("positions", positions, i, (n,)), ("slots", slots, i, (n,)), ("free_count_out", free_count_out, i, (1,)),
             ("position_base", position_base, i, (b,)))
-    _check(lib().eg_mla_page_plan(b, page_size, width, n, _ptr(cached_lens), _ptr(new_lens), _ptr(position_base),
-                                  _ptr(page_table), _ptr(free_pages), _ptr(free_count), free, _ptr(seq_lens),
-                                  _ptr(cu_seqlens), _ptr(positions), _ptr(slots), _ptr(free_count_out),
+    _check(lib().eg_mla_page_plan(b, page_size, width, n, cached_lens.data_ptr(), new_lens.data_ptr(), _ptr(position_base),
+                                  page_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), free, seq_lens.data_ptr(),
+                                  cu_seqlens.data_ptr(), positions.data_ptr(), slots.data_ptr(), free_count_out.data_ptr(),
                                   _stream(stream)), name)
 
 
@@ -337,16 +340,27 @@ def page_release(page_size: int, seq_lens, ended, page_table, free_pages, free_c
     _expect(name, ("seq_lens", seq_lens, i, (b,)), ("ended", ended, i, (b,)), ("page_table", page_table, i, (b, width)),
             ("free_pages", free_pages, i, (free,)), ("free_count", free_count, i, (1,)),
             ("seq_lens_out", seq_lens_out, i, (b,)), ("free_count_out", free_count_out, i, (1,)))
-    _check(lib().eg_mla_page_release(b, page_size, width, _ptr(seq_lens), _ptr(ended), _ptr(page_table),
-                                     _ptr(free_pages), _ptr(free_count), free, _ptr(seq_lens_out),
-                                     _ptr(free_count_out), _stream(stream)), name)
+    _check(lib().eg_mla_page_release(b, page_size, width, seq_lens.data_ptr(), ended.data_ptr(), page_table.data_ptr(),
+                                     free_pages.data_ptr(), free_count.data_ptr(), free, seq_lens_out.data_ptr(),
+                                     free_count_out.data_ptr(), _stream(stream)), name)
 
 
-def _row_stride(name: str, key: str, t, n: int, row: int) -> int:
-    """Elements between the rows of a [n, row] or [n, heads, d] tensor or view whose rows are contiguous."""
-    if t.shape[0] != n or t.numel() != n * row or (n and not t[0].is_contiguous()):
-        raise ValueError(f"{name}: {key} is {tuple(t.shape)} with strides {t.stride()}, not {n} contiguous rows of {row}")
-    return t.stride(0) if n > 1 else row
+def _row_stride(name: str, key: str, t, n: int, row: int, dtype) -> int:
+    """Elements between the rows of a [n, row] or [n, heads, d] tensor, or a view, whose rows are contiguous."""
+    import torch
+    shape, strides = t.shape, t.stride()
+    inner = 1
+    for size, step in zip(shape[:0:-1], strides[:0:-1]):
+        if size != 1 and step != inner:
+            inner = -1
+            break
+        inner *= size
+    if shape[0] != n or (n and inner != row):
+        raise ValueError(f"{name}: {key} is {tuple(shape)} with strides {strides}, not {n} contiguous rows of {row}")
+    dev = t.get_device()
+    if t.dtype is not dtype or dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{name}: {key} is {t.dtype} on {t.device}; expected {dtype} on the current GPU")
+    return strides[0] if n > 1 else row
 
 
 def qk_norm_rope(dims: Dims, q, q_out, kv, latent_cache, token_id_cache, token_ids, positions, slots, q_norm_w=None,
@@ -362,17 +376,17 @@ def qk_norm_rope(dims: Dims, q, q_out, kv, latent_cache, token_id_cache, token_i
     specs = [("positions", positions, i, (n,))]
     qs = ks = num_slots = 0
     if q is not None:
-        qs = _row_stride(name, "q", q, n, dims.num_heads * dq)
-        if q_out is None or q_out.numel() != q.numel():
+        if q_out is None or q_out.shape[0] != n or q_out.numel() != n * dims.num_heads * dq:
             raise ValueError(f"{name}: q_out does not hold {n} rows of {dims.num_heads} heads of {dq} values")
-        specs += [("q", q[:0], dt, None), ("q_out", q_out, dt, None), ("q_norm_w", q_norm_w, dt, (dq,))]
+        qs = _row_stride(name, "q", q, n, dims.num_heads * dq, dt)
+        specs += (("q_out", q_out, dt, None), ("q_norm_w", q_norm_w, dt, (dq,)))
     if kv is not None:
-        ks = _row_stride(name, "kv", kv, n, row)
+        ks = _row_stride(name, "kv", kv, n, row, dt)
         num_slots = latent_cache.shape[0]
-        specs += [("kv", kv[:0], dt, None), ("latent_cache", latent_cache, dt, (num_slots, row)),
+        specs += (("latent_cache", latent_cache, dt, (num_slots, row)),
                   ("token_id_cache", token_id_cache, i, (num_slots,)), ("token_ids", token_ids, i, (n,)),
                   ("slots", slots, i, (n,)), ("kv_norm_w", kv_norm_w, dt, (dims.latent_dim,)),
-                  ("k_norm_w", k_norm_w, dt, (dims.rope_dim,))]
+                  ("k_norm_w", k_norm_w, dt, (dims.rope_dim,)))
     _expect(name, *specs)
     _check(lib().eg_mla_qk_norm_rope(ctypes.byref(dims), n, _ptr(q), qs, _ptr(q_norm_w), _ptr(q_out), _ptr(kv), ks,
                                      _ptr(kv_norm_w), _ptr(k_norm_w), _ptr(token_ids), _ptr(positions), _ptr(slots),
@@ -400,9 +414,9 @@ def decode_shared(dims: Dims, q, latent_cache, token_id_cache, gate_table, w_uk,
             ("page_table", page_table, i, (b, max_pages_per_seq)), ("out", out, dt, (b, h, dv)),
             ("workspace", workspace, None, None))
     _check(lib().eg_mla_decode_shared(ctypes.byref(dims), b, _ptr(q), _ptr(latent_cache), _ptr(token_id_cache),
-                                      _ptr(gate_table), _ptr(w_uk), _ptr(w_uv), _ptr(prefix_len), _ptr(prefix_table),
+                                      gate_table.data_ptr(), w_uk.data_ptr(), w_uv.data_ptr(), _ptr(prefix_len), _ptr(prefix_table),
                                       pages, _ptr(seq_lens), _ptr(page_table), max_pages_per_seq, slots,
-                                      _ptr(workspace), _bytes(workspace), _ptr(out), _stream(stream)), name)
+                                      _ptr(workspace), _bytes(workspace), out.data_ptr(), _stream(stream)), name)
 
 
 def page_means(dims: Dims, latent_cache, token_id_cache, gate_table, first_tokens, seq_lens, page_table,
@@ -415,9 +429,9 @@ def page_means(dims: Dims, latent_cache, token_id_cache, gate_table, first_token
             ("gate_table", gate_table, dt, (dims.vocab_size, dims.latent_dim)),
             ("first_tokens", first_tokens, i, (b,)), ("seq_lens", seq_lens, i, (b,)),
             ("page_table", page_table, i, (b, max_pages_per_seq)), ("means", means, dt, (slots // dims.page_size, row)))
-    _check(lib().eg_mla_page_means(ctypes.byref(dims), b, _ptr(latent_cache), _ptr(token_id_cache), _ptr(gate_table),
+    _check(lib().eg_mla_page_means(ctypes.byref(dims), b, _ptr(latent_cache), _ptr(token_id_cache), gate_table.data_ptr(),
                                    _ptr(first_tokens), _ptr(seq_lens), _ptr(page_table), max_pages_per_seq, slots,
-                                   _ptr(means), _stream(stream)), name)
+                                   means.data_ptr(), _stream(stream)), name)
 
 
 def page_scores_workspace_size(dims: Dims, batch: int) -> int:
@@ -435,9 +449,9 @@ def page_scores(dims: Dims, q, w_uk, means, seq_lens, page_table, max_pages_per_
             ("means", means, dt, (pages, dims.latent_dim + dr)), ("seq_lens", seq_lens, i, (b,)),
             ("page_table", page_table, i, (b, max_pages_per_seq)), ("scores", scores, float32, (b, max_pages_per_seq)),
             ("workspace", workspace, None, None))
-    _check(lib().eg_mla_page_scores(ctypes.byref(dims), b, _ptr(q), _ptr(w_uk), _ptr(means), _ptr(seq_lens),
+    _check(lib().eg_mla_page_scores(ctypes.byref(dims), b, _ptr(q), w_uk.data_ptr(), means.data_ptr(), _ptr(seq_lens),
                                     _ptr(page_table), max_pages_per_seq, pages * dims.page_size, _ptr(workspace),
-                                    _bytes(workspace), _ptr(scores), _stream(stream)), name)
+                                    _bytes(workspace), scores.data_ptr(), _stream(stream)), name)
 
 
 def select_pages(dims: Dims, scores, seq_lens, page_table, max_pages_per_seq: int, sel_pages, sel_lens,
@@ -450,8 +464,8 @@ def select_pages(dims: Dims, scores, seq_lens, page_table, max_pages_per_seq: in
     _expect(name, ("scores", scores, float32, (b, max_pages_per_seq)), ("seq_lens", seq_lens, i, (b,)),
             ("page_table", page_table, i, (b, max_pages_per_seq)), ("sel_pages", sel_pages, i, (b, keep)),
             ("sel_lens", sel_lens, i, (b,)), ("sel_index", sel_index, i, (b, keep)))
-    _check(lib().eg_mla_select_pages(ctypes.byref(dims), b, _ptr(scores), _ptr(seq_lens), _ptr(page_table),
-                                     max_pages_per_seq, keep, keep_first, keep_last, _ptr(sel_pages), _ptr(sel_lens),
+    _check(lib().eg_mla_select_pages(ctypes.byref(dims), b, scores.data_ptr(), _ptr(seq_lens), _ptr(page_table),
+                                     max_pages_per_seq, keep, keep_first, keep_last, sel_pages.data_ptr(), sel_lens.data_ptr(),
                                      _ptr(sel_index), _stream(stream)), name)
 
 

@@ -18,7 +18,7 @@
 // Angles: position times frequency in turns, in 64-bit fixed point modulo one
 // turn (the frequencies, scaled by 2^64 / 2 pi, come from the host in extended
 // precision), so that far positions keep full accuracy: an error below
-// 2^-33 turns for any 32-bit position.  Sine and cosine of the remainder are
+// 2^-30 turns for any 32-bit position.  Sine and cosine of the remainder are
 // fp32.  Sums of squares and every product are fp32; the result is rounded
 // once to the storage type.
 #include <hip/hip_runtime.h>
@@ -293,7 +293,7 @@ extern "C" eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_
   const long double step = d.rope_dim ? powl(theta, -2.0L / d.rope_dim) : 0.0L;
   long double f = 1.0L / 6.283185307179586476925286766559005768L;
   for (int m = 0; m < d.rope_dim / 2; ++m, f *= step)
-    a.freq[m] = static_cast<uint64_t>(fmodl(f, 1.0L) * 18446744073709551616.0L);
+    a.freq[m] = static_cast<uint64_t>((f < 1.0L ? f : fmodl(f, 1.0L)) * 18446744073709551616.0L);  // whole turns drop out
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   (void)hipGetLastError();
   const dim3 grid(static_cast<unsigned>(wgs));
