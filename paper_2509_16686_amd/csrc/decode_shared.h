@@ -138,7 +138,8 @@ template <int DC>
 hipError_t launch_tiled(const SharedCall& c) {
   const eg_mla_dims& d = c.d;
   const SharedPlan& p = c.p;
-  const bool wide = p.own.balanced && p.own.capacity > 0;
+  const bool own_tokens = p.own.capacity > 0;
+  const bool wide = p.own.balanced && own_tokens && !p.fused;
   int2* seq_rows = reinterpret_cast<int2*>(c.ws + p.own.off_sched + 16 + kWideMaxGroups * 8);
   PrefixPrepArgs pa{};
   pa.q = static_cast<const uint16_t*>(c.q);
@@ -169,9 +170,11 @@ hipError_t launch_tiled(const SharedCall& c) {
               : ag.grouped   ? shared_prep_kernel<AbsorbRows::kBoth, kAbsBlocks, kAbsCols>
               : ag.narrow    ? shared_prep_kernel<AbsorbRows::kBoth, 1, kAbsColsNarrow>
                              : shared_prep_kernel<AbsorbRows::kBoth, 1, kAbsCols>;
-  const int64_t prep_wgs = 1 + pa.gate_wgs + static_cast<int64_t>(ag.grid.x) * ag.grid.y * ag.grid.z;
-  if (prep_wgs > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(prep, dim3(static_cast<unsigned>(prep_wgs)), dim3(256), 0, c.stream, pa);
+  const int64_t absorb_wgs = static_cast<int64_t>(ag.grid.x) * ag.grid.y * ag.grid.z;
+  if (absorb_wgs > (1 << 30)) return hipErrorInvalidValue;
+  pa.absorb_wgs = static_cast<int32_t>(absorb_wgs);
+  const unsigned prep_wgs = 1 + pa.absorb_wgs + pa.gate_wgs;
+  hipLaunchKernelGGL(prep, dim3(prep_wgs), dim3(256), 0, c.stream, pa);
 
   PrefixArgs a{};
   a.qhalf = pa.qhalf;
@@ -184,10 +187,27 @@ hipError_t launch_tiled(const SharedCall& c) {
   a.row_blocks = p.row_blocks;
   a.s_max = p.splits;
   a.scale_log2 = softmax_scale(d) * kLog2e;
-  hipLaunchKernelGGL(shared_prefix_kernel<DC>, dim3(p.row_blocks * p.splits), dim3(kPrefixThreads), 0, c.stream, a);
+  auto attend = shared_prefix_kernel<DC, false>;
+  if constexpr (DC == 512) {
+    if (p.fused) {
+      attend = shared_prefix_kernel<DC, true>;
+      a.cache = pa.cache;
+      a.ids = c.ids;
+      a.gate = pa.gate;
+      a.own_lens = own_tokens ? c.seq_lens : nullptr;
+      a.own_table = c.page_table;
+      a.num_slots = c.num_slots;
+      a.own_cap = p.own.capacity;
+      a.own_pages = c.max_pages;
+      a.blocks_per_seq = d.num_heads / kPrefixRows;
+      a.P = d.page_size;
+      a.V = d.vocab_size;
+    }
+  }
+  hipLaunchKernelGGL(attend, dim3(p.row_blocks * p.splits), dim3(kPrefixThreads), 0, c.stream, a);
 
   SharedPart own{};
-  if (p.own.capacity > 0) {
+  if (own_tokens && !p.fused) {
     const hipError_t e = launch_shared_part(c, 1, wide ? reinterpret_cast<const float*>(pa.qhalf) : pa.qfull, &own);
     if (e != hipSuccess) return e;
   }
@@ -208,6 +228,7 @@ hipError_t launch_tiled(const SharedCall& c) {
   m.own_cap = own.cap;
   m.own_split = own.split;
   m.own_s_max = own.s_max;
+  m.every_split = p.fused;
   m.spw = kSharedMergeSeq;
   while (m.spw > 1 && static_cast<int64_t>(d.num_heads) * ((c.batch + m.spw - 1) / m.spw) < kSharedMergeGroups) m.spw /= 2;
   auto merge = shared_merge_kernel<DC, false>;

@@ -726,13 +726,14 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     return at;
   };
   if (p.tiled) {
-    const int tiles = ceil_div(p.pre.capacity, kPrefixKeys);
+    const int keys = prefix_keys(d.latent_dim), tiles = ceil_div(p.pre.capacity, keys);
     p.row_blocks = ceil_div(rows64, kPrefixRows);
     p.splits = std::max(1, std::min(prefix_groups(d) / p.row_blocks, tiles));
     if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x7fffffff) return EG_MLA_ERR_UNSUPPORTED;
+    p.fused = d.latent_dim == 512 && d.num_heads % kPrefixRows == 0;  // a row block within a sequence
     p.off_half = take(rows * dq * 2);
     if (!p.own.balanced) p.off_q = take(rows * dq * 4);
-    p.off_tiles = take(static_cast<size_t>(tiles) * kPrefixKeys * (prefix_latent_row(d.latent_dim) + 128));
+    p.off_tiles = take(static_cast<size_t>(tiles) * keys * (prefix_latent_row(d.latent_dim) + 128));
     p.pre.off_ml = take(rows * p.splits * 8);
     p.pre.off_o = take(rows * p.splits * dc * 2);
   } else {
@@ -741,7 +742,7 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     p.pre.off_ml = take(n * 8);
     p.pre.off_o = take(n * dc * 4);
   }
-  if (p.own.capacity > 0) {
+  if (p.own.capacity > 0 && !p.fused) {
     const size_t n = p.own.balanced ? (static_cast<size_t>(kWideMaxGroups) + batch) * d.num_heads
                                     : rows * static_cast<size_t>(p.own.s_max);
     p.own.off_ml = take(n * 8);

@@ -10,7 +10,7 @@
 //     bf16], and fp32 ones where the own tokens' kernel wants them), the own
 //     tokens' schedule, and, once per prefix token, the gated latent (the exact
 //     fp32 product rounded to fp16) and the RoPE key (bf16), written as tiles of
-//     64 keys that are byte for byte what the attention holds in LDS: page
+//     64 (or 32) keys that are byte for byte what the attention holds in LDS: page
 //     table, gate and bank swizzle are dealt with once, and a tile is copied
 //     as one run of memory.
 //  2. shared_prefix_kernel: a work-group of 4 waves takes 128 query rows (32
@@ -32,7 +32,7 @@ namespace egmla {
 
 template <int DC>
 struct PrefixCfg {
-  static constexpr int KEYS = kPrefixKeys;
+  static constexpr int KEYS = prefix_keys(DC);
   static constexpr int LROW = prefix_latent_row(DC);   // bytes per key: gated latent, padded to whole 256 bytes
   static constexpr int RROW = 128;                     // RoPE key
   static constexpr int ROPE = KEYS * LROW;             // its rows lie behind the latent rows
@@ -52,8 +52,9 @@ __host__ __device__ __forceinline__ int prefix_latent_byte(int key, int p) {
 }
 __host__ __device__ __forceinline__ int prefix_rope_byte(int key, int p) { return 16 * (p ^ ((key >> 1) & 7)); }
 
-constexpr int kPrepTokens = 32;   // tokens that a work-group gates at a time
+constexpr int kPrepTokens = 16;    // tokens that a work-group gates at a time
 constexpr int kPrepGroups = 2048;  // work-groups that gate, at most
+constexpr int kPrepBatch = 5;      // pieces of a thread in flight (d_c 512: 72 a token)
 
 struct PrefixPrepArgs {
   const uint16_t* q;
@@ -69,7 +70,7 @@ struct PrefixPrepArgs {
   int64_t num_slots;
   WideSchedArgs sched;  // G = 0: none
   int32_t B, H, DC, V, P, cap;
-  int32_t gate_wgs, row_blocks;
+  int32_t absorb_wgs, gate_wgs, row_blocks;
 };
 
 template <AbsorbRows ROWS_OUT, int BLOCKS, int COLS>
@@ -81,43 +82,63 @@ __global__ __launch_bounds__(256) void shared_prep_kernel(PrefixPrepArgs a) {
     return;
   }
   wg -= 1;
-  if (wg >= a.gate_wgs) {
-    wg -= a.gate_wgs;
+  if (wg < a.absorb_wgs) {
     const int h = wg % a.H, by = (wg / a.H) % a.row_blocks, bz = wg / (a.H * a.row_blocks);
     absorb_tile<128, BLOCKS, COLS, ROWS_OUT>(a.q, a.w_uk, a.qfull, a.qhalf, a.B, a.H, a.DC, DR, h, by, bz);
     return;
   }
+  wg -= a.absorb_wgs;
   // pieces of the prefix's tokens, kPrepTokens tokens at a time; those behind the last token, up to the end of its
   // tile, are zero
-  const int L = clamp_len(a.len[0], a.cap), end = (L + kPrefixKeys - 1) / kPrefixKeys * kPrefixKeys;
+  const int keys = prefix_keys(a.DC);
+  const int L = clamp_len(a.len[0], a.cap), end = (L + keys - 1) / keys * keys;
   const int np = a.DC / 8 + DR / 8, lat = a.DC / 8;
-  const int lrow = prefix_latent_row(a.DC), tile_bytes = kPrefixKeys * (lrow + 128);
+  const int lrow = prefix_latent_row(a.DC), tile_bytes = keys * (lrow + 128);
+  __shared__ int2 tok_s[kPrepTokens];  // (cache row, id); row -1: behind the last token
   for (int base = wg * kPrepTokens; base < end; base += a.gate_wgs * kPrepTokens) {
-    for (int i = threadIdx.x; i < kPrepTokens * np; i += 256) {
-      const int t = base + i / np, p = i % np, key = t % kPrefixKeys;
-      unsigned char* dst = a.tiles + static_cast<int64_t>(t / kPrefixKeys) * tile_bytes +
-                           (p < lat ? key * lrow + prefix_latent_byte(key, p)
-                                    : kPrefixKeys * lrow + key * 128 + prefix_rope_byte(key, p - lat));
-      u32x4_t v = {0u, 0u, 0u, 0u};
+    if (threadIdx.x < kPrepTokens) {
+      const int t = base + static_cast<int>(threadIdx.x);
+      int2 e = make_int2(-1, 0);
       if (t < L) {
-        const int64_t slot = paged_slot(a.table[t / a.P], t, a.P, a.num_slots);
-        v = *reinterpret_cast<const u32x4_t*>(a.cache + slot * (a.DC + DR) + 8 * p);
-        if (p < lat)
-          v = gate_chunk_f16(v, *reinterpret_cast<const u32x4_t*>(
-                                    a.gate + static_cast<int64_t>(clamp_id(a.ids[slot], a.V)) * a.DC + 8 * p));
+        e.x = static_cast<int>(paged_slot(a.table[t / a.P], t, a.P, a.num_slots));
+        e.y = clamp_id(a.ids[e.x], a.V);
       }
-      *reinterpret_cast<u32x4_t*>(dst) = v;
+      tok_s[threadIdx.x] = e;
     }
+    __syncthreads();
+    for (int i0 = threadIdx.x; i0 < kPrepTokens * np; i0 += 256 * kPrepBatch) {
+      u32x4_t v[kPrepBatch], gv[kPrepBatch];
+#pragma unroll
+      for (int u = 0; u < kPrepBatch; ++u) {
+        const int i = i0 + 256 * u, k = min(i / np, kPrepTokens - 1), p = i % np;
+        const int2 e = tok_s[k];
+        v[u] = gv[u] = u32x4_t{0u, 0u, 0u, 0u};
+        if (i < kPrepTokens * np && e.x >= 0) {
+          v[u] = *reinterpret_cast<const u32x4_t*>(a.cache + static_cast<int64_t>(e.x) * (a.DC + DR) + 8 * p);
+          if (p < lat) gv[u] = *reinterpret_cast<const u32x4_t*>(a.gate + static_cast<int64_t>(e.y) * a.DC + 8 * p);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kPrepBatch; ++u) {
+        const int i = i0 + 256 * u, k = i / np, p = i % np, t = base + k, key = t % keys;
+        if (i >= kPrepTokens * np) continue;
+        unsigned char* dst = a.tiles + static_cast<int64_t>(t / keys) * tile_bytes +
+                             (p < lat ? key * lrow + prefix_latent_byte(key, p)
+                                      : keys * lrow + key * 128 + prefix_rope_byte(key, p - lat));
+        *reinterpret_cast<u32x4_t*>(dst) = p < lat ? gate_chunk_f16(v[u], gv[u]) : v[u];
+      }
+    }
+    __syncthreads();  // the list has been read
   }
 }
 
 // Tiles per split of a prefix of L tokens cut into at most s_max splits, and the splits that have any.
-__device__ __forceinline__ int prefix_per_split(int L, int s_max) {
-  const int tiles = (L + kPrefixKeys - 1) / kPrefixKeys;
+__device__ __forceinline__ int prefix_per_split(int L, int s_max, int keys) {
+  const int tiles = (L + keys - 1) / keys;
   return (tiles + s_max - 1) / s_max;
 }
-__device__ __forceinline__ int prefix_splits(int L, int s_max) {
-  const int tiles = (L + kPrefixKeys - 1) / kPrefixKeys, per = prefix_per_split(L, s_max);
+__device__ __forceinline__ int prefix_splits(int L, int s_max, int keys) {
+  const int tiles = (L + keys - 1) / keys, per = prefix_per_split(L, s_max, keys);
   return per ? (tiles + per - 1) / per : 0;
 }
 
@@ -129,6 +150,14 @@ struct PrefixArgs {
   uint16_t* part_o;            // [s_max][rows][DC] fp16: O / l
   int32_t cap, rows, row_blocks, s_max;
   float scale_log2;
+  // OWN: each sequence's own tokens
+  const uint16_t* cache;       // [num_slots][DC + 64]
+  const int32_t* ids;
+  const uint16_t* gate;        // [V][DC]
+  const int32_t* own_lens;     // null: none
+  const int32_t* own_table;    // or null
+  int64_t num_slots;
+  int32_t own_cap, own_pages, blocks_per_seq, P, V;
 };
 
 typedef __attribute__((ext_vector_type(16))) float px_f32x16_t;
@@ -149,20 +178,29 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
-template <int DC>
+// OWN (heads a multiple of 128, so that a row block lies within a sequence): after its run of the prefix a work-group
+// takes its share of the sequence's own tokens into the same accumulators.  Their raw rows and gate rows are copied to
+// LDS a tile ahead, and gated from there into the tile.
+constexpr int kOwnList = 512;  // own tokens listed at a time
+
+template <int DC, bool OWN>
 __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_prefix_kernel(PrefixArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass knows neither the copies to LDS nor the register constraints
   using C = PrefixCfg<DC>;
   constexpr int DQ = DC + 64, NC = DC / 16, NR = 4, KB = C::KEYS / 32, NDB = DC / 32;
+  // How far the LDS reads run ahead of the products: with two waves per SIMD (d_c 128) the other wave covers their
+  // latency, with one (d_c 512: 161 us, prefix 8000 x 64 x 128 heads) they have to (184 one chunk ahead and the values
+  // in the compiler's order; 175 six or eight value products ahead).
+  constexpr int QA = DC == 512 ? 3 : 1, PA = DC == 128 ? 0 : 4;
   __shared__ __attribute__((aligned(16))) unsigned char lds0[C::TILE];  // two tile buffers
   __shared__ __attribute__((aligned(16))) unsigned char lds1[C::TILE];
   // consecutive items (the row blocks of a split) share an XCD, whose L2 then serves the split's tiles
   const int item = xcd_logical_block(blockIdx.x, gridDim.x);
   const int rb = item % a.row_blocks, split = item / a.row_blocks;
-  const int L = clamp_len(a.len[0], a.cap);
-  const int per = prefix_per_split(L, a.s_max);
+  const int L = a.len ? clamp_len(a.len[0], a.cap) : 0;
+  const int per = prefix_per_split(L, a.s_max, C::KEYS);
   const int t0 = split * per, t1 = min(t0 + per, (L + C::KEYS - 1) / C::KEYS);
-  if (t0 >= t1) return;
+  if (!OWN && t0 >= t1) return;
 
   const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -176,6 +214,14 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
   for (int c = 0; c < NC; ++c) qv[c] = *reinterpret_cast<const f16x8_t*>(a.qhalf + qrow + 16 * c);
 #pragma unroll
   for (int c = 0; c < NR; ++c) qr[c] = *reinterpret_cast<const bf16x8_t*>(a.qhalf + qrow + DC + 16 * c);
+  // d_c 512: q^R waits in LDS, each lane's own operands (with its 16 registers the value operands could not run ahead:
+  // prefix 8000 x 64 x 128 heads with own tokens 198 us, 163 so)
+  constexpr bool QLDS = DC == 512;
+  __shared__ __attribute__((aligned(16))) bf16x8_t qr_s[QLDS ? NR * kPrefixThreads : 1];
+  if constexpr (QLDS) {
+#pragma unroll
+    for (int c = 0; c < NR; ++c) qr_s[c * kPrefixThreads + tid] = qr[c];
+  }
 
   auto lds_ptr = [](unsigned char* p) { return (__attribute__((address_space(3))) void*)p; };
   auto issue_tile = [&](int tile, unsigned char* base) {
@@ -215,26 +261,18 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
     }
   };
 
-  issue_tile(t0, lds0);
-  tile_landed();
-  __syncthreads();
-  // step i computes tile i from `tb` and copies tile i + 1 into `nb` (last read in step i - 1, which ended in a barrier)
-  auto step = [&](int i, const unsigned char* tb, unsigned char* nb) {
-    if (i + 1 < t1) issue_tile(i + 1, nb);
+  // attends to the `valid` first keys of the tile in `tb`
+  auto attend = [&](const unsigned char* tb, int valid) __attribute__((always_inline)) {
     hold();
     px_f32x16_t s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+    if constexpr (QLDS) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const f16x8_t av = *reinterpret_cast<const f16x8_t*>(tb + off_l + 32 * kb * C::LROW + 256 * (c >> 3) +
-                                                             16 * ((2 * (c & 7) + h) ^ swz_l));
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, qv[c], s[kb], 0, 0, 0);
-      }
+      for (int c = 0; c < NR; ++c) qr[c] = qr_s[c * kPrefixThreads + tid];
+    }
 #pragma unroll
     for (int c = 0; c < NR; ++c)
 #pragma unroll
@@ -243,20 +281,28 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
             *reinterpret_cast<const bf16x8_t*>(tb + off_r + 32 * kb * C::RROW + 16 * ((2 * c + h) ^ swz_r));
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qr[c], s[kb], 0, 0, 0);
       }
-    // issue order: the A operands of a chunk one chunk ahead of its products
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * KB, 0);
 #pragma unroll
-    for (int c = 0; c < NC + NR - 1; ++c) {
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const f16x8_t av = *reinterpret_cast<const f16x8_t*>(tb + off_l + 32 * kb * C::LROW + 256 * (c >> 3) +
+                                                             16 * ((2 * (c & 7) + h) ^ swz_l));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, qv[c], s[kb], 0, 0, 0);
+      }
+    // issue order: the A operands QA chunks ahead of their products
+    __builtin_amdgcn_sched_group_barrier(0x100, (QA + 1) * KB + (QLDS ? NR : 0), 0);
+#pragma unroll
+    for (int c = 0; c < NC + NR - QA; ++c) {
       __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
-    if ((i + 1) * C::KEYS > L) {  // the prefix ends inside this tile
+    __builtin_amdgcn_sched_group_barrier(0x008, QA * KB, 0);
+    if (valid < C::KEYS) {  // the tokens end inside this tile
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (i * C::KEYS + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3) >= L) s[kb][r] = -INFINITY;
+          if (32 * kb + 8 * (r >> 2) + 4 * h + (r & 3) >= valid) s[kb][r] = -INFINITY;
     }
 
     // online softmax (row = lane % 32; keys split between lanes l and l ^ 32); the scale (tau log2 e > 0) commutes with
@@ -321,6 +367,26 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, pb[kb][m], o[db], 0, 0, 0);
         }
       }
+    if constexpr (PA > 0) {  // operands PA products ahead
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * PA, 1);
+#pragma unroll
+      for (int c = 0; c < KB * 2 * NDB - PA; ++c) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, PA, 1);
+    }
+  };
+
+  if (t0 < t1) {
+    issue_tile(t0, lds0);
+    tile_landed();
+    __syncthreads();
+  }
+  // step i computes tile i from `tb` and copies tile i + 1 into `nb` (last read in step i - 1, which ended in a barrier)
+  auto step = [&](int i, const unsigned char* tb, unsigned char* nb) __attribute__((always_inline)) {
+    if (i + 1 < t1) issue_tile(i + 1, nb);
+    attend(tb, L - i * C::KEYS);
     tile_landed();
     __syncthreads();
   };
@@ -329,8 +395,79 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
     if (i + 1 < t1) step(i + 1, lds1, lds0);
   }
 
+  if constexpr (OWN) {
+    // own tokens: raw rows of the next tile in `lds1`, its gate rows in `gate_s`, the tile in `lds0`
+    static_assert(C::KEYS == 32 && C::TILE == 32 * DQ * 2, "a tile buffer holds 32 raw rows");
+    constexpr int RP = DQ / 8, GP = DC / 8;  // 16-byte pieces of a raw and of a gate row
+    __shared__ __attribute__((aligned(16))) unsigned char gate_s[32 * DC * 2];
+    __shared__ int2 list[kOwnList];  // (cache row, id)
+    const int b = rb / a.blocks_per_seq;
+    const int own = a.own_lens ? clamp_len(a.own_lens[b], a.own_cap) : 0;
+    const int own_tiles = (own + 31) / 32, own_per = (own_tiles + a.s_max - 1) / a.s_max;
+    const int k0 = min(32 * split * own_per, own), k1 = min(k0 + 32 * own_per, own);  // this work-group's tokens
+    auto fill_list = [&](int base) __attribute__((always_inline)) {  // tokens base .. of this work-group
+#pragma unroll
+      for (int e = 0; e < kOwnList / kPrefixThreads; ++e) {
+        const int t = base + tid + e * kPrefixThreads;
+        if (t < k1) {
+          const int slot = static_cast<int>(cache_slot(a.own_table, b, t, a.P, a.own_pages, a.num_slots));
+          list[t - base] = make_int2(slot, clamp_id(a.ids[slot], a.V));
+        }
+      }
+    };
+    auto issue_raw = [&](int t, int base) __attribute__((always_inline)) {  // tokens past the last repeat it and are masked
+      int lane = threadIdx.x & 63;  // (not known to be the same each time: the addresses are not kept over `attend`)
+      asm volatile("" : "+v"(lane));
+#pragma unroll
+      for (int j = 0; j < RP / 8; ++j) {
+        const int i = 64 * (RP / 8 * w + j) + lane, k = i / RP, p = i % RP;
+        const int slot = list[min(t + k, k1 - 1) - base].x;
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(a.cache + static_cast<int64_t>(slot) * DQ + 8 * p),
+            lds_ptr(lds1 + 1024 * (RP / 8 * w + j)), 16, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < GP / 8; ++j) {
+        const int i = 64 * (GP / 8 * w + j) + lane, k = i / GP, p = i % GP;
+        const int id = list[min(t + k, k1 - 1) - base].y;
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(a.gate + static_cast<int64_t>(id) * DC + 8 * p),
+            lds_ptr(gate_s + 1024 * (GP / 8 * w + j)), 16, 0, 0);
+      }
+    };
+    auto gate_tile = [&]() __attribute__((always_inline)) {  // raw rows and gate rows into the tile
+      int tid = threadIdx.x;
+      asm volatile("" : "+v"(tid));
+#pragma unroll 4
+      for (int j = 0; j < 32 * GP / kPrefixThreads; ++j) {
+        const int i = tid + j * kPrefixThreads, k = i / GP, p = i % GP;
+        *reinterpret_cast<u32x4_t*>(lds0 + k * C::LROW + prefix_latent_byte(k, p)) =
+            gate_chunk_f16(*reinterpret_cast<const u32x4_t*>(lds1 + k * DQ * 2 + 16 * p),
+                           *reinterpret_cast<const u32x4_t*>(gate_s + 16 * i));
+      }
+      const int k = tid / 8, p = tid % 8;
+      *reinterpret_cast<u32x4_t*>(lds0 + C::ROPE + k * C::RROW + prefix_rope_byte(k, p)) =
+          *reinterpret_cast<const u32x4_t*>(lds1 + k * DQ * 2 + DC * 2 + 16 * p);
+    };
+    for (int base = k0; base < k1; base += kOwnList) {
+      fill_list(base);
+      __syncthreads();
+      const int end = min(base + kOwnList, k1);
+      issue_raw(base, base);
+      for (int t = base; t < end; t += 32) {
+        tile_landed();
+        __syncthreads();  // the raw rows are here, and the tile's last reader is done
+        gate_tile();
+        __syncthreads();
+        if (t + 32 < end) issue_raw(t + 32, base);
+        attend(lds0, k1 - t);
+      }
+      __syncthreads();  // the list has been read
+    }
+  }
+
   // O / l: lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row whose scores all
-  // overflowed to -inf weighs nothing
+  // overflowed to -inf (or that had no token) weighs nothing
   const float l = half_sum(l_run);
   const float inv = l > 0.f ? 1.0f / l : 0.f;
   if (row < a.rows) {
@@ -356,7 +493,7 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
 // dims each); with 4 rows to a wave (d_c 128) or one, each group of lanes is a
 // worker, and spw sequences share the work-group's workers in rounds.  A
 // worker folds every W-th partial row of its sequence (the prefix's, then its
-// own tokens') online in fp32, kSharedBatch rows loaded together; the workers
+// own tokens') online in fp32, 2, 4 or 8 rows loaded together; the workers
 // of a sequence meet in LDS, and the merged row o / l goes there once more as
 // bf16 hi + lo, the B operands of out^T[v][b] = W_UV[h] o^T on
 // v_mfma_f32_16x16x32_bf16.  Latency-bound: the rows' two round trips, the
@@ -364,7 +501,10 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
 // ---------------------------------------------------------------------------
 constexpr int kSharedMergeWaves = 8;
 constexpr int kSharedMergeSeq = 16;
-constexpr int kSharedBatch = 8;
+template <int N>
+struct Batch {
+  static constexpr int value = N;
+};
 
 struct SharedMergeArgs {
   const float* pre_ml;      // [s_max][B H][2]
@@ -377,6 +517,7 @@ struct SharedMergeArgs {
   const uint16_t* w_uv;
   uint16_t* out;
   int32_t B, H, pre_cap, pre_s_max, own_cap, own_split, own_s_max, spw;
+  bool every_split;         // the prefix kernel took the own tokens too and left a row in every split
 };
 
 template <int DC, bool WIDE>
@@ -399,7 +540,9 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
   };
   if constexpr (DC <= 128) load_w();
 
-  const int pre_n = a.pre_len ? prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max) : 0;
+  const int pre_n = a.every_split ? a.pre_s_max
+                    : a.pre_len   ? prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max, prefix_keys(DC))
+                                  : 0;
   const int wps = max(1, WORKERS / a.spw);  // workers per sequence (spw <= WORKERS where GPW > 1, else rounds)
   const int spr = WORKERS / wps;            // sequences per round
   const int worker = w * GPW + (GPW > 1 ? lane / LPR : 0);
@@ -409,23 +552,24 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
     const int k = r0 + worker / wps, me = worker % wps;
     const int b = b0 + k;
     float M = -INFINITY, sum = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    // rows me, me + wps, ... < n of a part; load(i, ml, v) reads row i
-    auto fold = [&](int n, bool normalised, auto load) {
-      for (int i0 = me; i0 < n; i0 += wps * kSharedBatch) {
-        float2 ml[kSharedBatch];
-        float v[kSharedBatch][8];
+    // rows me, me + wps, ... < n of a part, U at a time; load(i, ml, v) reads row i
+    auto fold_by = [&](auto batch, int n, bool normalised, auto load) {
+      constexpr int U = decltype(batch)::value;
+      for (int i0 = me; i0 < n; i0 += wps * U) {
+        float2 ml[U];
+        float v[U][8];
 #pragma unroll
-        for (int u = 0; u < kSharedBatch; ++u) load(min(i0 + u * wps, n - 1), ml[u], v[u]);
+        for (int u = 0; u < U; ++u) load(min(i0 + u * wps, n - 1), ml[u], v[u]);
         float top = M;
 #pragma unroll
-        for (int u = 0; u < kSharedBatch; ++u) top = fmaxf(top, ml[u].x);  // repeats change no maximum
+        for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);  // repeats change no maximum
         const bool any = top > -INFINITY;  // rows without weight have maximum -inf
         const float keep = any ? __builtin_amdgcn_exp2f(M - top) : 1.f;
         sum *= keep;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] *= keep;
 #pragma unroll
-        for (int u = 0; u < kSharedBatch; ++u) {
+        for (int u = 0; u < U; ++u) {
           const float x = any && i0 + u * wps < n ? __builtin_amdgcn_exp2f(ml[u].x - top) : 0.f;
           sum = fmaf(x, ml[u].y, sum);
           const float y = normalised ? x * ml[u].y : x;
@@ -435,6 +579,11 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
         M = top;
       }
     };
+    auto fold = [&](int n, bool normalised, auto load) {
+      if (n <= 2 * wps) fold_by(Batch<2>{}, n, normalised, load);
+      else if (n <= 4 * wps) fold_by(Batch<4>{}, n, normalised, load);
+      else fold_by(Batch<8>{}, n, normalised, load);
+    };
     auto half_row = [&](const uint16_t* p, float (&v)[8]) {
       const f16x8_t x = *reinterpret_cast<const f16x8_t*>(p + col);
 #pragma unroll
@@ -442,20 +591,22 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
     };
     if (live && k < nseq) {
       const int64_t rows = static_cast<int64_t>(a.B) * a.H, qrow = static_cast<int64_t>(b) * a.H + h;
-      fold(pre_n, true, [&](int i, float2& ml, float (&v)[8]) {
+      auto pre_row = [&](int i, float2& ml, float (&v)[8]) {
         const int64_t at = i * rows + qrow;
         ml = *reinterpret_cast<const float2*>(a.pre_ml + 2 * at);
         half_row(a.pre_o + at * DC, v);
-      });
-      if (a.own_lens) {
-        if constexpr (WIDE) {
-          const int2 list = a.own_rows[b];
-          fold(list.y, true, [&](int i, float2& ml, float (&v)[8]) {
-            const int64_t at = static_cast<int64_t>(list.x + i) * a.H + h;
-            ml = *reinterpret_cast<const float2*>(a.own_ml + 2 * at);
-            half_row(static_cast<const uint16_t*>(a.own_o) + at * DC, v);
-          });
-        } else {
+      };
+      if constexpr (WIDE) {  // both parts' rows have the same form: one list
+        const int2 list = a.own_rows[b];
+        fold(pre_n + list.y, true, [&](int i, float2& ml, float (&v)[8]) {
+          const bool own = i >= pre_n;
+          const int64_t at = own ? static_cast<int64_t>(list.x + i - pre_n) * a.H + h : i * rows + qrow;
+          ml = *reinterpret_cast<const float2*>((own ? a.own_ml : a.pre_ml) + 2 * at);
+          half_row((own ? static_cast<const uint16_t*>(a.own_o) : a.pre_o) + at * DC, v);
+        });
+      } else {
+        fold(pre_n, true, pre_row);
+        if (a.own_lens) {
           const int L = clamp_len(a.own_lens[b], a.own_cap);
           fold(min((L + a.own_split - 1) / a.own_split, a.own_s_max), false, [&](int i, float2& ml, float (&v)[8]) {
             const int64_t at = (static_cast<int64_t>(b) * a.own_s_max + i) * a.H + h;
