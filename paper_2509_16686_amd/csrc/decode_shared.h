@@ -96,11 +96,9 @@ struct SharedCall {
 // Sequences of a merge work-group: 16, or fewer while that leaves under one work-group per compute unit.
 constexpr int kSharedMergeGroups = 256;
 
-// Split kernel of the prefix (part 0, as one sequence of B H heads) or of the own tokens (part 1).
-hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {
+// Arguments of the split kernel of the prefix (part 0, as one sequence of B H heads) or of the own tokens (part 1).
+SplitArgs shared_split_args(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {
   const DecodePlan& s = part ? c.p.own : c.p.pre;
-  eg_mla_dims ds = c.d;
-  if (part == 0) ds.num_heads = c.batch * c.d.num_heads;
   SplitArgs a{};
   a.qfull = qfull;
   a.cache = c.cache;
@@ -114,7 +112,7 @@ hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull,
   a.scale_log2 = softmax_scale(c.d) * kLog2e;
   a.DH = c.d.head_dim;
   a.B = part ? c.batch : 1;
-  a.H = ds.num_heads;
+  a.H = part ? c.d.num_heads : c.batch * c.d.num_heads;
   a.seq_lens = part ? c.seq_lens : c.prefix_len;
   a.page_table = part ? c.page_table : c.prefix_table;
   a.max_pages = part ? c.max_pages : c.max_prefix_pages;
@@ -130,8 +128,15 @@ hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull,
     a.wg_start = reinterpret_cast<const int2*>(c.ws + s.off_sched + 16);
   }
   *rows = {a.part_ml, a.part_o, a.seq_lens, s.capacity, s.split_tokens, s.s_max};
+  return a;
+}
+
+hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {
+  const SplitArgs a = shared_split_args(c, part, qfull, rows);
+  eg_mla_dims ds = c.d;
+  ds.num_heads = a.H;
   const OneArgs one{c.q, c.w_uk, c.w_uv, c.out, c.d.v_head_dim, 1, 1};
-  return launch_split(ds, s, a, one, c.stream, nullptr, nullptr);
+  return launch_split(ds, part ? c.p.own : c.p.pre, a, one, c.stream, nullptr, nullptr);
 }
 
 template <int DC>
@@ -163,6 +168,9 @@ hipError_t launch_tiled(const SharedCall& c) {
   pa.V = d.vocab_size;
   pa.P = d.page_size;
   pa.cap = p.pre.capacity;
+  pa.keys = p.keys;
+  pa.splits = p.splits;
+  if (p.fused) pa.split_rows = reinterpret_cast<int2*>(c.ws + p.off_rows);
   pa.gate_wgs = std::min((p.pre.capacity + kPrepTokens - 1) / kPrepTokens, kPrepGroups);
   const AbsorbGrid ag = absorb_grid(d, c.batch, p.own.balanced);
   pa.row_blocks = ag.grid.y;
@@ -187,29 +195,46 @@ hipError_t launch_tiled(const SharedCall& c) {
   a.row_blocks = p.row_blocks;
   a.s_max = p.splits;
   a.scale_log2 = softmax_scale(d) * kLog2e;
-  auto attend = shared_prefix_kernel<DC, false>;
-  if constexpr (DC == 512) {
-    if (p.fused) {
-      attend = shared_prefix_kernel<DC, true>;
-      a.cache = pa.cache;
-      a.ids = c.ids;
-      a.gate = pa.gate;
-      a.own_lens = own_tokens ? c.seq_lens : nullptr;
-      a.own_table = c.page_table;
-      a.num_slots = c.num_slots;
-      a.own_cap = p.own.capacity;
-      a.own_pages = c.max_pages;
-      a.blocks_per_seq = d.num_heads / kPrefixRows;
-      a.P = d.page_size;
-      a.V = d.vocab_size;
+  SharedPart own{};
+  const unsigned prefix_wgs = p.row_blocks * p.splits;
+  if (DC == 128 && p.both) {
+    const SplitArgs so = shared_split_args(c, 1, pa.qfull, &own);
+    const int own_wgs = c.batch * p.own.s_max * p.own.head_groups;
+    hipLaunchKernelGGL(shared_both_kernel, dim3(prefix_wgs + own_wgs), dim3(kPrefixThreads), 0, c.stream, a, so, own_wgs);
+  } else {
+    auto attend = shared_prefix_kernel<DC, DC == 512 ? 32 : 64, false>;
+    if constexpr (DC == 512) {
+      if (p.fused) {
+        attend = shared_prefix_kernel<DC, 32, true>;
+        a.cache = pa.cache;
+        a.ids = c.ids;
+        a.gate = pa.gate;
+        a.own_lens = own_tokens ? c.seq_lens : nullptr;
+        a.own_table = c.page_table;
+        a.num_slots = c.num_slots;
+        a.own_cap = p.own.capacity;
+        a.own_pages = c.max_pages;
+        a.blocks_per_seq = d.num_heads / kPrefixRows;
+        a.P = d.page_size;
+        a.V = d.vocab_size;
+      }
+    }
+    hipLaunchKernelGGL(attend, dim3(prefix_wgs), dim3(kPrefixThreads), 0, c.stream, a);
+    if (own_tokens && !p.fused) {
+      const hipError_t e = launch_shared_part(c, 1, wide ? reinterpret_cast<const float*>(pa.qhalf) : pa.qfull, &own);
+      if (e != hipSuccess) return e;
     }
   }
-  hipLaunchKernelGGL(attend, dim3(p.row_blocks * p.splits), dim3(kPrefixThreads), 0, c.stream, a);
-
-  SharedPart own{};
-  if (own_tokens && !p.fused) {
-    const hipError_t e = launch_shared_part(c, 1, wide ? reinterpret_cast<const float*>(pa.qhalf) : pa.qfull, &own);
-    if (e != hipSuccess) return e;
+  if constexpr (DC == 512) {
+    if (p.fused) {  // one row per split and sequence: the wide kernel's merge
+      const hipError_t e = set_lds(combine_wide_kernel, combine_wide_lds_bytes());
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(combine_wide_kernel, dim3(d.num_heads, (c.batch + kCombWideSeq - 1) / kCombWideSeq),
+                         dim3(kCombWideWaves * 64), combine_wide_lds_bytes(), c.stream, a.part_ml, a.part_o,
+                         static_cast<const uint16_t*>(c.w_uv), pa.split_rows, static_cast<uint16_t*>(c.out), c.batch,
+                         d.num_heads);
+      return hipGetLastError();
+    }
   }
   SharedMergeArgs m{};
   m.pre_ml = a.part_ml;
@@ -228,7 +253,7 @@ hipError_t launch_tiled(const SharedCall& c) {
   m.own_cap = own.cap;
   m.own_split = own.split;
   m.own_s_max = own.s_max;
-  m.every_split = p.fused;
+  m.keys = p.keys;
   m.spw = kSharedMergeSeq;
   while (m.spw > 1 && static_cast<int64_t>(d.num_heads) * ((c.batch + m.spw - 1) / m.spw) < kSharedMergeGroups) m.spw /= 2;
   auto merge = shared_merge_kernel<DC, false>;

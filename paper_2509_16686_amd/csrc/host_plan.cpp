@@ -699,6 +699,16 @@ constexpr int64_t kPrefixMinRows = 64;
 // Its work-groups: two per compute unit where their registers and tiles allow (d_c 128).
 int prefix_groups(const eg_mla_dims& d) { return d.latent_dim == 128 ? 512 : 256; }
 
+// d_c 128: with few tiles one, fewer partial rows (prefix 8192 x 32 sequences of
+// 16 heads, 512 tiles: both parts and the merge 19.6 us with 256 work-groups,
+// 25.1 with 512; x 256 sequences of 16384, 8192 tiles: 70.3 and 68.2).
+constexpr int kPrefixGroupsFew = 256;
+constexpr int64_t kPrefixFewTiles = 2048;
+// d_c 128: prefix and own tokens in one launch up to this many tiles (the two
+// of the last paragraph: 33.5 -> 24.8 us and 76 -> 72 a call); its 32-key
+// tiles cost the prefix 6 %, more than hiding the own tokens gains beyond.
+constexpr int64_t kBothMaxTiles = 16384;
+
 bool prefix_tiled(const eg_mla_dims& d, int64_t rows) {
   return d.dtype == EG_MLA_BF16 && d.head_dim == 128 && d.v_head_dim == 128 && d.rope_dim == 64 &&
          (d.latent_dim == 128 || d.latent_dim == 320 || d.latent_dim == 512) && rows >= kPrefixMinRows;
@@ -726,14 +736,19 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     return at;
   };
   if (p.tiled) {
-    const int keys = prefix_keys(d.latent_dim), tiles = ceil_div(p.pre.capacity, keys);
     p.row_blocks = ceil_div(rows64, kPrefixRows);
-    p.splits = std::max(1, std::min(prefix_groups(d) / p.row_blocks, tiles));
-    if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x7fffffff) return EG_MLA_ERR_UNSUPPORTED;
+    const int64_t work = static_cast<int64_t>(p.row_blocks) * ceil_div(p.pre.capacity, 64);  // 64-key tiles of all rows
+    p.both = d.latent_dim == 128 && p.own.capacity > 0 && p.own.path == EG_MLA_PATH_MFMA &&
+             p.own.split_tokens <= kBothList && work <= kBothMaxTiles;
+    p.keys = d.latent_dim == 512 || p.both ? 32 : 64;
+    const int tiles = ceil_div(p.pre.capacity, p.keys);
+    p.splits = std::max(1, std::min((work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d)) / p.row_blocks, tiles));
+    if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x3fffffff) return EG_MLA_ERR_UNSUPPORTED;
     p.fused = d.latent_dim == 512 && d.num_heads % kPrefixRows == 0;  // a row block within a sequence
     p.off_half = take(rows * dq * 2);
     if (!p.own.balanced) p.off_q = take(rows * dq * 4);
-    p.off_tiles = take(static_cast<size_t>(tiles) * keys * (prefix_latent_row(d.latent_dim) + 128));
+    p.off_tiles = take(static_cast<size_t>(tiles) * p.keys * (prefix_latent_row(d.latent_dim) + 128));
+    if (p.fused) p.off_rows = take(static_cast<size_t>(batch) * 8);
     p.pre.off_ml = take(rows * p.splits * 8);
     p.pre.off_o = take(rows * p.splits * dc * 2);
   } else {

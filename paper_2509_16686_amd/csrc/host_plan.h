@@ -193,20 +193,20 @@ eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const f
 // sequence of B H heads over the prefix, `own` that of the batch over its own
 // tokens; their off_ml, off_o and off_sched are offsets into the call's one
 // workspace.
-// Keys of a tile of the tiled prefix attention (shared_prefix.h): 32 of d_c 512,
-// whose accumulators and queries leave few registers for scores and operands
-// (measured there: 64 keys 163 to 185 us, 32 keys 161, prefix 8000 x 64 x 128 heads).
-constexpr int prefix_keys(int dc) { return dc > 320 ? 32 : 64; }
+constexpr int kBothList = 1024;   // own tokens of a split that shares the prefix's launch, at most
 constexpr int kPrefixRows = 128;  // query rows of its work-groups
 constexpr int prefix_latent_row(int dc) { return (2 * dc + 255) / 256 * 256; }  // bytes of a key's latent in a tile
 struct SharedPlan {
   DecodePlan pre, own;
   bool tiled = false;    // the prefix on the tiled kernel, in at most `splits` runs of tiles (pre: capacity and offsets)
   bool fused = false;    // ... which takes the own tokens too
+  bool both = false;     // d_c 128: prefix and own tokens in one launch
+  int keys = 0;          // of a prefix tile
   int row_blocks = 0, splits = 0;
   size_t off_q = 0;      // fp32 [B, H, d_c + d_r] (not tiled, or own tokens not on the wide kernel)
   size_t off_half = 0;   // tiled: 16-bit [B, H, d_c + d_r]
   size_t off_tiles = 0;  // tiled: the gated prefix
+  size_t off_rows = 0;   // fused: int2 [B] partial rows of each sequence
   size_t bytes = 0;
 };
 eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,

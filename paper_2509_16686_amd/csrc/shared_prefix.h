@@ -10,7 +10,7 @@
 //     bf16], and fp32 ones where the own tokens' kernel wants them), the own
 //     tokens' schedule, and, once per prefix token, the gated latent (the exact
 //     fp32 product rounded to fp16) and the RoPE key (bf16), written as tiles of
-//     64 (or 32) keys that are byte for byte what the attention holds in LDS: page
+//     64 or 32 keys that are byte for byte what the attention holds in LDS: page
 //     table, gate and bank swizzle are dealt with once, and a tile is copied
 //     as one run of memory.
 //  2. shared_prefix_kernel: a work-group of 4 waves takes 128 query rows (32
@@ -30,9 +30,9 @@
 
 namespace egmla {
 
-template <int DC>
+template <int DC, int KEYS_>
 struct PrefixCfg {
-  static constexpr int KEYS = prefix_keys(DC);
+  static constexpr int KEYS = KEYS_;                   // of a tile
   static constexpr int LROW = prefix_latent_row(DC);   // bytes per key: gated latent, padded to whole 256 bytes
   static constexpr int RROW = 128;                     // RoPE key
   static constexpr int ROPE = KEYS * LROW;             // its rows lie behind the latent rows
@@ -69,8 +69,9 @@ struct PrefixPrepArgs {
   unsigned char* tiles;
   int64_t num_slots;
   WideSchedArgs sched;  // G = 0: none
+  int2* split_rows;     // null: none; else each sequence's partial rows, one per split
   int32_t B, H, DC, V, P, cap;
-  int32_t absorb_wgs, gate_wgs, row_blocks;
+  int32_t absorb_wgs, gate_wgs, row_blocks, keys, splits;
 };
 
 template <AbsorbRows ROWS_OUT, int BLOCKS, int COLS>
@@ -79,6 +80,8 @@ __global__ __launch_bounds__(256) void shared_prep_kernel(PrefixPrepArgs a) {
   int wg = blockIdx.x;
   if (wg == 0) {
     if (a.sched.G > 0) wide_schedule<256>(a.sched, a.B);
+    if (a.split_rows)
+      for (int b = threadIdx.x; b < a.B; b += 256) a.split_rows[b] = make_int2(b * a.splits, a.splits);
     return;
   }
   wg -= 1;
@@ -90,7 +93,7 @@ __global__ __launch_bounds__(256) void shared_prep_kernel(PrefixPrepArgs a) {
   wg -= a.absorb_wgs;
   // pieces of the prefix's tokens, kPrepTokens tokens at a time; those behind the last token, up to the end of its
   // tile, are zero
-  const int keys = prefix_keys(a.DC);
+  const int keys = a.keys;
   const int L = clamp_len(a.len[0], a.cap), end = (L + keys - 1) / keys * keys;
   const int np = a.DC / 8 + DR / 8, lat = a.DC / 8;
   const int lrow = prefix_latent_row(a.DC), tile_bytes = keys * (lrow + 128);
@@ -146,8 +149,8 @@ struct PrefixArgs {
   const uint16_t* qhalf;       // [rows][DC + 64]: q_lat fp16 | q^R bf16
   const unsigned char* tiles;  // PrefixCfg<DC>::TILE bytes each
   const int32_t* len;
-  float* part_ml;              // [s_max][rows][2]
-  uint16_t* part_o;            // [s_max][rows][DC] fp16: O / l
+  float* part_ml;              // [s_max][rows][2]; OWN: [B][s_max][H][2]
+  uint16_t* part_o;            // [s_max][rows][DC] fp16: O / l; OWN: [B][s_max][H][DC]
   int32_t cap, rows, row_blocks, s_max;
   float scale_log2;
   // OWN: each sequence's own tokens
@@ -183,10 +186,11 @@ __device__ __forceinline__ float half_sum(float x) {
 // LDS a tile ahead, and gated from there into the tile.
 constexpr int kOwnList = 512;  // own tokens listed at a time
 
-template <int DC, bool OWN>
-__global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_prefix_kernel(PrefixArgs a) {
+// Work-group `bid` of `nblocks`.
+template <int DC, int KEYS, bool OWN>
+__device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nblocks) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass knows neither the copies to LDS nor the register constraints
-  using C = PrefixCfg<DC>;
+  using C = PrefixCfg<DC, KEYS>;
   constexpr int DQ = DC + 64, NC = DC / 16, NR = 4, KB = C::KEYS / 32, NDB = DC / 32;
   // How far the LDS reads run ahead of the products: with two waves per SIMD (d_c 128) the other wave covers their
   // latency, with one (d_c 512: 161 us, prefix 8000 x 64 x 128 heads) they have to (184 one chunk ahead and the values
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
   __shared__ __attribute__((aligned(16))) unsigned char lds0[C::TILE];  // two tile buffers
   __shared__ __attribute__((aligned(16))) unsigned char lds1[C::TILE];
   // consecutive items (the row blocks of a split) share an XCD, whose L2 then serves the split's tiles
-  const int item = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int item = xcd_logical_block(bid, nblocks);
   const int rb = item % a.row_blocks, split = item / a.row_blocks;
   const int L = a.len ? clamp_len(a.len[0], a.cap) : 0;
   const int per = prefix_per_split(L, a.s_max, C::KEYS);
@@ -208,19 +212,23 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
   // this lane's query row; rows past the last repeat it and are not stored
   const int row = rb * kPrefixRows + 32 * w + r32;
   const int64_t qrow = static_cast<int64_t>(min(row, a.rows - 1)) * DQ + 8 * h;
+  // d_c 512: q^R and the first QL chunks of q_lat wait in LDS, each lane's own operands (registers are scarce: with them
+  // in registers the value operands could not run ahead, and what the compiler spilled it read back in the tile loop,
+  // waiting for the tile copies too: prefix 8000 x 64 x 128 heads with own tokens 198 to 272 us, 163 so)
+  constexpr int QL = DC == 512 ? 4 : 0;
+  constexpr bool QLDS = QL > 0;
+  __shared__ __attribute__((aligned(16))) u32x4_t q_s[QLDS ? (NR + QL) * kPrefixThreads : 1];
   f16x8_t qv[NC];   // q_lat
   bf16x8_t qr[NR];  // q^R
 #pragma unroll
   for (int c = 0; c < NC; ++c) qv[c] = *reinterpret_cast<const f16x8_t*>(a.qhalf + qrow + 16 * c);
 #pragma unroll
   for (int c = 0; c < NR; ++c) qr[c] = *reinterpret_cast<const bf16x8_t*>(a.qhalf + qrow + DC + 16 * c);
-  // d_c 512: q^R waits in LDS, each lane's own operands (with its 16 registers the value operands could not run ahead:
-  // prefix 8000 x 64 x 128 heads with own tokens 198 us, 163 so)
-  constexpr bool QLDS = DC == 512;
-  __shared__ __attribute__((aligned(16))) bf16x8_t qr_s[QLDS ? NR * kPrefixThreads : 1];
   if constexpr (QLDS) {
 #pragma unroll
-    for (int c = 0; c < NR; ++c) qr_s[c * kPrefixThreads + tid] = qr[c];
+    for (int c = 0; c < NR; ++c) q_s[c * kPrefixThreads + tid] = __builtin_bit_cast(u32x4_t, qr[c]);
+#pragma unroll
+    for (int c = 0; c < QL; ++c) q_s[(NR + c) * kPrefixThreads + tid] = __builtin_bit_cast(u32x4_t, qv[c]);
   }
 
   auto lds_ptr = [](unsigned char* p) { return (__attribute__((address_space(3))) void*)p; };
@@ -271,7 +279,9 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
     if constexpr (QLDS) {
 #pragma unroll
-      for (int c = 0; c < NR; ++c) qr[c] = qr_s[c * kPrefixThreads + tid];
+      for (int c = 0; c < NR; ++c) qr[c] = __builtin_bit_cast(bf16x8_t, q_s[c * kPrefixThreads + tid]);
+#pragma unroll
+      for (int c = 0; c < QL; ++c) qv[c] = __builtin_bit_cast(f16x8_t, q_s[(NR + c) * kPrefixThreads + tid]);
     }
 #pragma unroll
     for (int c = 0; c < NR; ++c)
@@ -290,7 +300,7 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, qv[c], s[kb], 0, 0, 0);
       }
     // issue order: the A operands QA chunks ahead of their products
-    __builtin_amdgcn_sched_group_barrier(0x100, (QA + 1) * KB + (QLDS ? NR : 0), 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, (QA + 1) * KB + (QLDS ? NR + QL : 0), 0);
 #pragma unroll
     for (int c = 0; c < NC + NR - QA; ++c) {
       __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
@@ -470,10 +480,17 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
   // overflowed to -inf (or that had no token) weighs nothing
   const float l = half_sum(l_run);
   const float inv = l > 0.f ? 1.0f / l : 0.f;
-  if (row < a.rows) {
-    const int64_t at = static_cast<int64_t>(split) * a.rows + row;
-    if (h == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(l > 0.f ? m_run : -INFINITY, l);
-    uint16_t* orow = a.part_o + at * DC + 8 * h;
+  int lane_e = tid & 63;  // (the row is formed anew: nothing of it is kept over the loops)
+  asm volatile("" : "+v"(lane_e));
+  const int he = lane_e >> 5, row_e = rb * kPrefixRows + 32 * w + (lane_e & 31);
+  if (row_e < a.rows) {
+    int64_t at = static_cast<int64_t>(split) * a.rows + row_e;
+    if constexpr (OWN) {
+      const int H = a.blocks_per_seq * kPrefixRows, b = rb / a.blocks_per_seq;
+      at = (static_cast<int64_t>(b) * a.s_max + split) * H + (row_e - b * H);
+    }
+    if (he == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(l > 0.f ? m_run : -INFINITY, l);
+    uint16_t* orow = a.part_o + at * DC + 8 * he;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -485,6 +502,21 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
                     pack_f16x2(o[db][8 * j + 6] * inv, o[db][8 * j + 7] * inv)};
   }
 #endif
+}
+
+template <int DC, int KEYS, bool OWN>
+__global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_prefix_kernel(PrefixArgs a) {
+  prefix_item<DC, KEYS, OWN>(a, blockIdx.x, gridDim.x);
+}
+
+// Both parts of a short call in one launch (d_c 128): the first own_wgs
+// work-groups run the own tokens' split kernel, the others the prefix, in 32-key
+// tiles so that both fit a compute unit twice over.  Each part alone would
+// mostly wait for its own chain of loads.
+__global__ __launch_bounds__(kPrefixThreads, 2) void shared_both_kernel(PrefixArgs a, SplitArgs own, int own_wgs) {
+  const int bid = blockIdx.x;
+  if (bid < own_wgs) split_slice_item<128, 64, 4, 2, 1, false, false, kBothList>(own, bid, own_wgs);
+  else prefix_item<128, 32, false>(a, bid - own_wgs, gridDim.x - own_wgs);
 }
 
 // ---------------------------------------------------------------------------
@@ -509,15 +541,14 @@ struct Batch {
 struct SharedMergeArgs {
   const float* pre_ml;      // [s_max][B H][2]
   const uint16_t* pre_o;    // [s_max][B H][DC] fp16, normalised
-  const int32_t* pre_len;   // null: no prefix
+  const int32_t* pre_len;
   const float* own_ml;
   const void* own_o;        // fp32 sums, [B][own_s_max][H][DC]; WIDE: fp16, normalised, rows of own_rows
   const int32_t* own_lens;  // null: no own tokens
   const int2* own_rows;     // WIDE
   const uint16_t* w_uv;
   uint16_t* out;
-  int32_t B, H, pre_cap, pre_s_max, own_cap, own_split, own_s_max, spw;
-  bool every_split;         // the prefix kernel took the own tokens too and left a row in every split
+  int32_t B, H, pre_cap, pre_s_max, own_cap, own_split, own_s_max, spw, keys;
 };
 
 template <int DC, bool WIDE>
@@ -540,9 +571,7 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
   };
   if constexpr (DC <= 128) load_w();
 
-  const int pre_n = a.every_split ? a.pre_s_max
-                    : a.pre_len   ? prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max, prefix_keys(DC))
-                                  : 0;
+  const int pre_n = prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max, a.keys);
   const int wps = max(1, WORKERS / a.spw);  // workers per sequence (spw <= WORKERS where GPW > 1, else rounds)
   const int spr = WORKERS / wps;            // sequences per round
   const int worker = w * GPW + (GPW > 1 ? lane / LPR : 0);

@@ -52,7 +52,8 @@ namespace egmla {
 // Largest number of positions one work item of the sliced kernel scans.
 constexpr int kMaxScanTokens = kMaxSliceSplitTokens;
 
-template <int DC, int DR, int NW>
+// LIST: tokens of a work item, at most.
+template <int DC, int DR, int NW, int LIST = kMaxScanTokens>
 struct SsplitCfg {
   static constexpr int DQ = DC + DR;
   static constexpr int NC = DC / 32;                 // 32-dim latent chunks (score MFMA)
@@ -65,9 +66,9 @@ struct SsplitCfg {
   static constexpr int TPR = RPT > 0 ? 64 / RPT : 1; // tokens per RoPE load instruction
   static constexpr int NRI = RPT > 0 ? 16 / TPR : 0; // RoPE load instructions per unit
   static constexpr int TS = DQ + 8;                  // tile row: latent (fp16) | RoPE key (bf16) | 16 bytes of padding
-  static constexpr int ROWS = kMaxScanTokens / 256;  // scan rows of a work item, at most
+  static constexpr int ROWS = LIST / 256;  // scan rows of a work item, at most
   static constexpr int RPW = ROWS / NW;              // scan rows per wave, at most
-  static constexpr int LDS_LIST = kMaxScanTokens * 8;            // slot + id of every kept token
+  static constexpr int LDS_LIST = LIST * 8;            // slot + id of every kept token
   static constexpr int LDS_ROWS = ROWS * 4;                      // kept tokens per scan row
   static constexpr int LDS_TILE = NW * 16 * TS * 2;              // each wave's gated unit
   static constexpr int LDS_MERGE = NW * NB * 64 * 16;            // every wave's accumulators (aliases the above)
@@ -339,33 +340,34 @@ __device__ __forceinline__ void tok_schedule(const TokSchedArgs& sa, int B) {
   put(tid + NT, s1);
 }
 
-template <int DC, int DR, int NW, int D, int SL, bool FUSED = false, bool BAL = false>
-__global__ __launch_bounds__(NW * 64, 2) void split_slice_kernel(SplitArgs a) {
-  using Cfg = SsplitCfg<DC, DR, NW>;
+// Work-group `bid` of `nblocks`.
+template <int DC, int DR, int NW, int D, int SL, bool FUSED, bool BAL, int LIST>
+__device__ __forceinline__ void split_slice_item(const SplitArgs& a, int bid, int nblocks) {
+  using Cfg = SsplitCfg<DC, DR, NW, LIST>;
   constexpr int NC = Cfg::NC, NR = Cfg::NR, NB = Cfg::NB, DQ = Cfg::DQ, TS = Cfg::TS;
   constexpr int LPT = Cfg::LPT, TPL = Cfg::TPL, NLI = Cfg::NLI;
   constexpr int RPT = Cfg::RPT > 0 ? Cfg::RPT : 1, TPR = Cfg::TPR, NRI = Cfg::NRI;
   static_assert(SL == 1 || SL == 8, "id slices");
   __shared__ __attribute__((aligned(16))) unsigned char lds[Cfg::LDS_BYTES];
-  int* l_slot = reinterpret_cast<int*>(lds);                   // [kMaxScanTokens]
-  int* l_id = l_slot + kMaxScanTokens;                         // [kMaxScanTokens]
-  int* rowcnt = l_id + kMaxScanTokens;                         // [ROWS]
+  int* l_slot = reinterpret_cast<int*>(lds);                   // [LIST]
+  int* l_id = l_slot + LIST;                         // [LIST]
+  int* rowcnt = l_id + LIST;                         // [ROWS]
   uint16_t* tile_all = reinterpret_cast<uint16_t*>(lds + Cfg::LDS_LIST + Cfg::LDS_ROWS);  // [NW][16][TS]
   f32x4_t* obuf = reinterpret_cast<f32x4_t*>(lds);             // [NW][NB][64], after the units
   float* mbuf = reinterpret_cast<float*>(lds + Cfg::LDS_MAIN); // [NW][16]
   float* lbuf = mbuf + NW * 16;                                // [NW][16]
 
   // work-group x runs slice x % SL (its XCD); the rest is the (b, s, group) item
-  const int k = SL > 1 ? static_cast<int>(blockIdx.x % SL) : 0;
-  const int item = SL > 1 ? static_cast<int>(blockIdx.x / SL) : xcd_logical_block(blockIdx.x, gridDim.x);
+  const int k = SL > 1 ? bid % SL : 0;
+  const int item = SL > 1 ? bid / SL : xcd_logical_block(bid, nblocks);
   int hg = item % a.groups, s = (item / a.groups) % a.s_max, b = item / (a.groups * a.s_max), t0 = s * a.split;
   int n, piece = 0, L = 0;
   if constexpr (BAL) {
-    wide_block(blockIdx.x, a.groups, piece, hg);
+    wide_block(bid, a.groups, piece, hg);
     const int4 r = a.tok_pieces[piece];
     b = r.x;
     t0 = r.y;
-    n = min(r.z, kMaxScanTokens);  // (never more: tok_sizes)
+    n = min(r.z, LIST);  // (never more: tok_sizes)
     if (n <= 0) return;
   } else {
     L = clamp_len(a.seq_lens[b], a.cap);
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(NW * 64, 2) void split_slice_kernel(SplitArgs a) {
   if constexpr (SL == 1) {
     // ---- phase 1 without slices: the list is the split's positions ----
     // slot and id of every position (all loads first, clamped into the split)
-    constexpr int PER = kMaxScanTokens / (NW * 64);
+    constexpr int PER = LIST / (NW * 64);
     const int nper = (n + NW * 64 - 1) / (NW * 64);  // uniform
     int pp[PER], psl[PER], pid[PER];
 #pragma unroll
@@ -784,6 +786,11 @@ __global__ __launch_bounds__(NW * 64, 2) void split_slice_kernel(SplitArgs a) {
     __builtin_nontemporal_store(M, a.part_ml + (pbase + r16) * 2 + 0);
     __builtin_nontemporal_store(Ls, a.part_ml + (pbase + r16) * 2 + 1);
   }
+}
+
+template <int DC, int DR, int NW, int D, int SL, bool FUSED = false, bool BAL = false>
+__global__ __launch_bounds__(NW * 64, 2) void split_slice_kernel(SplitArgs a) {
+  split_slice_item<DC, DR, NW, D, SL, FUSED, BAL, kMaxScanTokens>(a, blockIdx.x, gridDim.x);
 }
 
 }  // namespace egmla
