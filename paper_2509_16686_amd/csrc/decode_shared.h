@@ -139,6 +139,17 @@ hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull,
   return launch_split(ds, part ? c.p.own : c.p.pre, a, one, c.stream, nullptr, nullptr);
 }
 
+// Both parts on the fp32 matrix-core kernel: one launch.
+template <bool BF16>
+hipError_t launch_f32_pair(const SplitArgs& a, const SplitArgs& b, int na, int nb, hipStream_t stream) {
+  auto kern = a.DC <= 64    ? split_f32_pair_kernel<BF16, 64>
+              : a.DC <= 128 ? split_f32_pair_kernel<BF16, 128>
+              : a.DC <= 256 ? split_f32_pair_kernel<BF16, 256>
+                            : split_f32_pair_kernel<BF16, 320>;
+  hipLaunchKernelGGL(kern, dim3(na + nb), dim3(256), 0, stream, SplitPair{{a, b}}, na);
+  return hipGetLastError();
+}
+
 template <int DC>
 hipError_t launch_tiled(const SharedCall& c) {
   const eg_mla_dims& d = c.d;
@@ -274,9 +285,19 @@ eg_mla_status run_decode_shared(const SharedCall& c) {
   float* qfull = reinterpret_cast<float*>(c.ws + c.p.off_q);
   if (launch_absorb(d, c.batch, c.q, c.w_uk, qfull, c.stream) != hipSuccess) return EG_MLA_ERR_HIP;
   SharedPart parts[2] = {};
-  for (int part = 0; part < 2; ++part)
-    if ((part ? c.p.own : c.p.pre).capacity > 0 && launch_shared_part(c, part, qfull, &parts[part]) != hipSuccess)
-      return EG_MLA_ERR_HIP;
+  const DecodePlan &pre = c.p.pre, &own = c.p.own;
+  const int64_t na = static_cast<int64_t>(pre.s_max) * pre.head_groups;
+  const int64_t nb = static_cast<int64_t>(c.batch) * own.s_max * own.head_groups;
+  if (pre.f32_mfma && own.f32_mfma && pre.capacity > 0 && own.capacity > 0 && na + nb <= 0x7fffffff) {
+    const SplitArgs a = shared_split_args(c, 0, qfull, &parts[0]), b = shared_split_args(c, 1, qfull, &parts[1]);
+    const hipError_t e = d.dtype == EG_MLA_BF16 ? launch_f32_pair<true>(a, b, static_cast<int>(na), static_cast<int>(nb), c.stream)
+                                                : launch_f32_pair<false>(a, b, static_cast<int>(na), static_cast<int>(nb), c.stream);
+    if (e != hipSuccess) return EG_MLA_ERR_HIP;
+  } else {
+    for (int part = 0; part < 2; ++part)
+      if ((part ? own : pre).capacity > 0 && launch_shared_part(c, part, qfull, &parts[part]) != hipSuccess)
+        return EG_MLA_ERR_HIP;
+  }
   auto kern = d.dtype == EG_MLA_BF16 ? shared_combine_kernel<true> : shared_combine_kernel<false>;
   hipLaunchKernelGGL(kern, dim3(d.num_heads, c.batch), dim3(256), sizeof(float) * d.latent_dim, c.stream, parts[0],
                      parts[1], c.w_uv, c.out, c.batch, d.num_heads, d.latent_dim, d.v_head_dim);

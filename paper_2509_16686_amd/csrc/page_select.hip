@@ -340,7 +340,9 @@ __global__ __launch_bounds__(kScoreWaves * 64) void page_scores_mfma_kernel(Scor
 // an unsigned number of the same order (a NaN counts as -inf, -0 as 0; pages
 // that are always kept come first); the K-th largest key is found by four
 // passes over 8 bits each (a histogram in LDS), then every key above it and
-// the first ones equal to it are written in the order of the sequence.
+// the first ones equal to it are written in the order of the sequence.  A
+// thread keeps its first page's key and number; where the lanes of a wave share a digit,
+// as scores of like size do in the first ones, one lane counts for all of them.
 // ---------------------------------------------------------------------------
 constexpr int kSelThreads = 1024;
 
@@ -379,16 +381,25 @@ __global__ __launch_bounds__(kSelThreads) void select_pages_kernel(SelectArgs a)
     return;
   }
   const float* score = a.scores + static_cast<int64_t>(b) * a.W;
-  auto key_of = [&](int j) {
+  auto load_key = [&](int j) {
     return j < a.keep_first || j >= n - a.keep_last ? 0xffffffffu : score_key(score[j]);
   };
+  const uint32_t first_key = tid < n ? load_key(tid) : 0u;
+  const int32_t first_page = tid < n ? page_of(tid) : 0;
+  auto key_of = [&](int j) { return j == tid ? first_key : load_key(j); };
   uint32_t prefix = 0, want = a.K;
   for (int shift = 24; shift >= 0; shift -= 8) {
     if (tid < 256) hist[tid] = 0;
     __syncthreads();
     for (int j = tid; j < n; j += kSelThreads) {
       const uint32_t k = key_of(j);
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+      if (shift == 24 || (k >> (shift + 8)) == prefix) {
+        const uint32_t digit = (k >> shift) & 255u;
+        const uint32_t common = __builtin_amdgcn_readfirstlane(digit);
+        const uint64_t same = __ballot(digit == common);
+        if (digit != common) atomicAdd(&hist[digit], 1u);
+        else if (__builtin_ctzll(same) == lane) atomicAdd(&hist[common], static_cast<uint32_t>(__popcll(same)));
+      }
     }
     __syncthreads();
     if (w == 0) {  // the digit whose keys hold the `want`-th from the top: lane l looks at digits 255 - 4 l ...
@@ -447,7 +458,7 @@ __global__ __launch_bounds__(kSelThreads) void select_pages_kernel(SelectArgs a)
     re += __popcll(me & low);
     if (is_above || (is_equal && re < want)) {
       const uint32_t at = ra + min(re, want);
-      sel[at] = page_of(j);
+      sel[at] = j == tid ? first_page : page_of(j);
       if (index) index[at] = j;
     }
   }

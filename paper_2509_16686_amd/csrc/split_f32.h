@@ -89,8 +89,9 @@ __device__ __forceinline__ void widen_piece(u32x4_t w, float (&o)[BF16 ? 8 : 4])
   }
 }
 
+// Work-group `bid` of `nblocks`.
 template <bool BF16, int DCM, int NW, bool ONE>
-__global__ __launch_bounds__(NW * 64, DCM <= 128 ? 2 : 1) void split_f32_kernel(SplitArgs a, OneArgs one) {
+__device__ __forceinline__ void split_f32_item(const SplitArgs& a, const OneArgs& one, int bid, int nblocks) {
   using C = F32Cfg<BF16, DCM, NW, ONE>;
   constexpr int EPP = C::EPP, NLL = C::NLL, NLR = C::NLR, NB = C::NB, TS = C::TS, D = C::D, NT = NW * 64;
   constexpr int DQM = DCM + C::DRM;
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(NW * 64, DCM <= 128 ? 2 : 1) void split_f32_kernel(
   float* mbuf = reinterpret_cast<float*>(lds + C::LDS_MAIN);                 // [NW][16]
   float* lbuf = mbuf + NW * 16;                                              // [NW][16]
 
-  const int item = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int item = xcd_logical_block(bid, nblocks);
   const int hg = item % a.groups;
   const int s = ONE ? 0 : (item / a.groups) % a.s_max;
   const int b = ONE ? item / a.groups : item / (a.groups * a.s_max);
@@ -415,6 +416,22 @@ __global__ __launch_bounds__(NW * 64, DCM <= 128 ? 2 : 1) void split_f32_kernel(
       if (sub == 0) st<BF16>(one.out, (static_cast<int64_t>(b) * a.H + h0) * one.DV + i, acc);
     }
   }
+}
+
+template <bool BF16, int DCM, int NW, bool ONE>
+__global__ __launch_bounds__(NW * 64, DCM <= 128 ? 2 : 1) void split_f32_kernel(SplitArgs a, OneArgs one) {
+  split_f32_item<BF16, DCM, NW, ONE>(a, one, blockIdx.x, gridDim.x);
+}
+
+// The first na work-groups one call's items, the others another's (the prefix and the own tokens of a shared decode).
+struct SplitPair {
+  SplitArgs part[2];
+};
+template <bool BF16, int DCM>
+__global__ __launch_bounds__(256, DCM <= 128 ? 2 : 1) void split_f32_pair_kernel(SplitPair p, int na) {
+  const int bid = blockIdx.x;
+  const int second = bid >= na;
+  split_f32_item<BF16, DCM, 4, false>(p.part[second], OneArgs{}, second ? bid - na : bid, second ? gridDim.x - na : na);
 }
 
 }  // namespace egmla
