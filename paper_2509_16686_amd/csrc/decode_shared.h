@@ -33,20 +33,37 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedPart pre, Sha
   extern __shared__ float o_s[];  // [DC]
   const int h = blockIdx.x, b = blockIdx.y;
   float M = -INFINITY, sum = 0.f, acc[kSharedCols] = {0.f, 0.f, 0.f};
+  constexpr int U = 8;  // rows in flight
   auto fold = [&](const SharedPart& p, int64_t row0, int64_t step, int len) {
     const int ns = min((clamp_len(len, p.cap) + p.split - 1) / p.split, p.s_max);
-    for (int s = 0; s < ns; ++s) {
-      const int64_t row = row0 + s * step;
-      const float m = p.ml[2 * row];
-      const float Mn = fmaxf(M, m);
-      if (!(Mn > -INFINITY)) continue;  // nothing weighs anything yet
-      const float keep = exp2f(M - Mn), e = exp2f(m - Mn);  // exp2(-inf) = 0
-      M = Mn;
-      sum = sum * keep + p.ml[2 * row + 1] * e;
+    for (int s0 = 0; s0 < ns; s0 += U) {
+      float2 ml[U];
+      float v[U][kSharedCols];
 #pragma unroll
-      for (int k = 0; k < kSharedCols; ++k) {
-        const int c = threadIdx.x + 256 * k;
-        if (c < DC) acc[k] = acc[k] * keep + p.o[row * DC + c] * e;
+      for (int u = 0; u < U; ++u) {
+        const int64_t row = row0 + min(s0 + u, ns - 1) * step;
+        ml[u] = *reinterpret_cast<const float2*>(p.ml + 2 * row);
+#pragma unroll
+        for (int k = 0; k < kSharedCols; ++k) {
+          const int c = threadIdx.x + 256 * k;
+          v[u][k] = c < DC ? p.o[row * DC + c] : 0.f;
+        }
+      }
+      float Mn = M;
+#pragma unroll
+      for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, ml[u].x);  // repeats of the last row change no maximum
+      if (!(Mn > -INFINITY)) continue;                      // nothing weighs anything yet
+      const float keep = exp2f(M - Mn);
+      M = Mn;
+      sum *= keep;
+#pragma unroll
+      for (int k = 0; k < kSharedCols; ++k) acc[k] *= keep;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float e = s0 + u < ns ? exp2f(ml[u].x - Mn) : 0.f;  // exp2(-inf) = 0
+        sum = fmaf(e, ml[u].y, sum);
+#pragma unroll
+        for (int k = 0; k < kSharedCols; ++k) acc[k] = fmaf(e, v[u][k], acc[k]);
       }
     }
   };
@@ -95,6 +112,11 @@ struct SharedCall {
 
 // Sequences of a merge work-group: 16, or fewer while that leaves under one work-group per compute unit.
 constexpr int kSharedMergeGroups = 256;
+
+// Partial rows of a sequence up to which the fused kernel's go to the wide
+// merge, which takes them four at a time and 32 sequences a work-group (64
+// sequences, 4 rows: 14.5 us against 19.6); more go to shared_merge_kernel.
+constexpr int kFusedWideSplits = 8;
 
 // Arguments of the split kernel of the prefix (part 0, as one sequence of B H heads) or of the own tokens (part 1).
 SplitArgs shared_split_args(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {
@@ -237,7 +259,7 @@ hipError_t launch_tiled(const SharedCall& c) {
     }
   }
   if constexpr (DC == 512) {
-    if (p.fused) {  // one row per split and sequence: the wide kernel's merge
+    if (p.fused && p.splits <= kFusedWideSplits) {  // few rows a sequence: the wide kernel's merge
       const hipError_t e = set_lds(combine_wide_kernel, combine_wide_lds_bytes());
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(combine_wide_kernel, dim3(d.num_heads, (c.batch + kCombWideSeq - 1) / kCombWideSeq),
@@ -250,7 +272,9 @@ hipError_t launch_tiled(const SharedCall& c) {
   SharedMergeArgs m{};
   m.pre_ml = a.part_ml;
   m.pre_o = a.part_o;
-  m.pre_len = c.prefix_len;
+  m.pre_len = p.fused ? nullptr : c.prefix_len;
+  m.pre_step = p.fused ? d.num_heads : static_cast<int64_t>(c.batch) * d.num_heads;
+  m.pre_seq = p.fused ? static_cast<int64_t>(p.splits) * d.num_heads : d.num_heads;
   m.own_ml = own.ml;
   m.own_o = own.o;
   m.own_lens = own.lens;

@@ -539,9 +539,10 @@ struct Batch {
 };
 
 struct SharedMergeArgs {
-  const float* pre_ml;      // [s_max][B H][2]
-  const uint16_t* pre_o;    // [s_max][B H][DC] fp16, normalised
-  const int32_t* pre_len;
+  const float* pre_ml;      // [rows][2]: split i of sequence b and head h at row i pre_step + b pre_seq + h
+  const uint16_t* pre_o;    // [rows][DC] fp16, normalised
+  const int32_t* pre_len;   // null: a row in every split
+  int64_t pre_step, pre_seq;
   const float* own_ml;
   const void* own_o;        // fp32 sums, [B][own_s_max][H][DC]; WIDE: fp16, normalised, rows of own_rows
   const int32_t* own_lens;  // null: no own tokens
@@ -571,7 +572,7 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
   };
   if constexpr (DC <= 128) load_w();
 
-  const int pre_n = prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max, a.keys);
+  const int pre_n = a.pre_len ? prefix_splits(clamp_len(a.pre_len[0], a.pre_cap), a.pre_s_max, a.keys) : a.pre_s_max;
   const int wps = max(1, WORKERS / a.spw);  // workers per sequence (spw <= WORKERS where GPW > 1, else rounds)
   const int spr = WORKERS / wps;            // sequences per round
   const int worker = w * GPW + (GPW > 1 ? lane / LPR : 0);
@@ -619,9 +620,9 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
       for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
     };
     if (live && k < nseq) {
-      const int64_t rows = static_cast<int64_t>(a.B) * a.H, qrow = static_cast<int64_t>(b) * a.H + h;
+      const int64_t pre0 = b * a.pre_seq + h;
       auto pre_row = [&](int i, float2& ml, float (&v)[8]) {
-        const int64_t at = i * rows + qrow;
+        const int64_t at = i * a.pre_step + pre0;
         ml = *reinterpret_cast<const float2*>(a.pre_ml + 2 * at);
         half_row(a.pre_o + at * DC, v);
       };
@@ -629,7 +630,7 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
         const int2 list = a.own_rows[b];
         fold(pre_n + list.y, true, [&](int i, float2& ml, float (&v)[8]) {
           const bool own = i >= pre_n;
-          const int64_t at = own ? static_cast<int64_t>(list.x + i - pre_n) * a.H + h : i * rows + qrow;
+          const int64_t at = own ? static_cast<int64_t>(list.x + i - pre_n) * a.H + h : i * a.pre_step + pre0;
           ml = *reinterpret_cast<const float2*>((own ? a.own_ml : a.pre_ml) + 2 * at);
           half_row((own ? static_cast<const uint16_t*>(a.own_o) : a.pre_o) + at * DC, v);
         });
