@@ -594,8 +594,14 @@ eg_mla_status validate_qk(const eg_mla_dims* d, int32_t n_tokens, const void* q,
   // the rotated query may take its source's place where the rows are the same; nothing else may overlap
   const Span qs{q, ((n - 1) * q_stride + q_row) * eb}, ks{kv, ((n - 1) * kv_stride + row) * eb};
   const Span qo{q ? q_out : nullptr, n * q_row * eb}, cache{kv ? latent_cache : nullptr, num_slots * row * eb};
+  const Span ids{kv ? token_id_cache : nullptr, num_slots * 4};
+  const Span qw{q ? q_norm_w : nullptr, static_cast<int64_t>(d->head_dim + d->rope_dim) * eb};
+  const Span kw{kv ? kv_norm_w : nullptr, static_cast<int64_t>(d->latent_dim) * eb};
+  const Span rw{kv ? k_norm_w : nullptr, static_cast<int64_t>(d->rope_dim) * eb};
   const bool in_place = q && q == q_out && q_stride == q_row;
-  if ((!in_place && overlap(qs, qo)) || outputs_overlap({qo, cache}, {ks}) || overlap(cache, qs))
+  if ((!in_place && overlap(qs, qo)) || overlap(cache, qs) || overlap(ids, qs) ||
+      outputs_overlap({qo, cache, ids}, {ks, qw, kw, rw, {positions, 4 * n}, {kv ? token_ids : nullptr, 4 * n},
+                                         {kv ? slots : nullptr, 4 * n}}))
     return EG_MLA_ERR_INVALID_ARG;
   return EG_MLA_OK;
 }

@@ -76,6 +76,16 @@ def test_qk_norm_rope(change, expect):
     assert B.lib().eg_mla_qk_norm_rope(*args.values()) == expect
 
 
+@pytest.mark.parametrize("change", [
+    dict(id_cache=at(6)), dict(id_cache=at(8, 28)), dict(id_cache=at(7)), dict(id_cache=at(9, 128)), dict(id_cache=at(0)),
+    dict(id_cache=at(3)), dict(cache=at(4)), dict(cache=at(5, 112)), dict(cache=at(6, 16)), dict(q_out=at(1, 368)),
+    dict(q_out=at(7, 16)), dict(q_out=at(10)),
+])
+def test_qk_norm_rope_outputs_over_weights_and_indices(change):
+    d = dims()
+    assert B.lib().eg_mla_qk_norm_rope(*{**QK, **change, "dims": ctypes.byref(d)}.values()) == ARG
+
+
 def test_bad_dims_are_refused_everywhere():
     for kw, expect in [(dict(num_heads=0), ARG), (dict(gate_dim=64), UNSUP), (dict(latent_dim=132), UNSUP)]:
         d = dims(**kw)
