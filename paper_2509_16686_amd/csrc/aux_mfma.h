@@ -117,32 +117,38 @@ __device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, cons
       const bf16x8_t bv = __builtin_bit_cast(bf16x8_t, u32x4_t{l2[0], l2[1], h2[0], h2[1]});
 #pragma unroll
       for (int rb = 0; rb < BLOCKS; ++rb)
-        acc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, qa[rb][ks]), bv, acc[rb], 0, 0, 0);
+        acc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv, __builtin_bit_cast(bf16x8_t, qa[rb][ks]), acc[rb], 0, 0, 0);
     }
-    // lane holds D[b = 4g + r][c = nt*16 + r16] of each row block
-    const int c = c0 + nt * 16 + r16;
+    // lane holds D[c = nt*16 + 4g + r][b = r16] of each row block: 4 columns of a row, stored together (d_c is a
+    // multiple of 8)
+    const int c = c0 + nt * 16 + 4 * g;
+    if (c >= DC) continue;
 #pragma unroll
     for (int rb = 0; rb < BLOCKS; ++rb) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int b = b0 + rb * kAbsRows + 4 * g + r;
-        if (b < B && c < DC) {
-          if constexpr (HALF)
-            reinterpret_cast<_Float16*>(qhalf)[(static_cast<int64_t>(b) * H + h) * DQ + c] =
-                static_cast<_Float16>(acc[rb][r]);
-          if constexpr (PARTS) {
-            const PartsLayout at(H, DC, DR);
-            const float x = acc[rb][r];
-            const uint16_t p0 = f32_to_bf16(x);
-            const float left = x - bf16_to_f32(p0);  // exact
-            const uint16_t p1 = f32_to_bf16(left);
-            qhalf[at(b, h, 0, c)] = p0;
-            qhalf[at(b, h, 1, c)] = p1;
-            qhalf[at(b, h, 2, c)] = f32_to_bf16(left - bf16_to_f32(p1));
-          }
-          if constexpr (FLOAT) qfull[(static_cast<int64_t>(b) * H + h) * DQ + c] = acc[rb][r];
-        }
+      const int b = b0 + rb * kAbsRows + r16;
+      if (b >= B) continue;
+      const f32x4_t x = acc[rb];
+      const int64_t at = (static_cast<int64_t>(b) * H + h) * DQ + c;
+      if constexpr (HALF) {
+        typedef __attribute__((ext_vector_type(4))) _Float16 f16x4_t;
+        *reinterpret_cast<f16x4_t*>(qhalf + at) = __builtin_convertvector(x, f16x4_t);
       }
+      if constexpr (PARTS) {
+        const PartsLayout layout(H, DC, DR);
+        uint16_t p[3][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p[0][r] = f32_to_bf16(x[r]);
+          const float left = x[r] - bf16_to_f32(p[0][r]);  // exact
+          p[1][r] = f32_to_bf16(left);
+          p[2][r] = f32_to_bf16(left - bf16_to_f32(p[1][r]));
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          *reinterpret_cast<uint2*>(qhalf + layout(b, h, i, c)) =
+              make_uint2(p[i][0] | static_cast<uint32_t>(p[i][1]) << 16, p[i][2] | static_cast<uint32_t>(p[i][3]) << 16);
+      }
+      if constexpr (FLOAT) *reinterpret_cast<f32x4_t*>(qfull + at) = x;
     }
   }
   if (rope_vec) {
