@@ -406,9 +406,9 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
   }
 
   if constexpr (OWN) {
-    // own tokens: raw rows of the next tile in `lds1`, its gate rows in `gate_s`, the tile in `lds0`
-    static_assert(C::KEYS == 32 && C::TILE == 32 * DQ * 2, "a tile buffer holds 32 raw rows");
-    constexpr int RP = DQ / 8, GP = DC / 8;  // 16-byte pieces of a raw and of a gate row
+    // own tokens: raw rows of the next tile in `lds1` (latents, then RoPE keys), its gate rows in `gate_s`, the tile in
+    // `lds0`; wave w copies and gates rows 8 w .. 8 w + 7, a row's latent one piece (16 bytes) a lane
+    static_assert(C::KEYS == 32 && DC == 512 && C::TILE == 32 * DQ * 2, "a row's latent is a wave's 64 pieces");
     __shared__ __attribute__((aligned(16))) unsigned char gate_s[32 * DC * 2];
     __shared__ int2 list[kOwnList];  // (cache row, id)
     const int b = rb / a.blocks_per_seq;
@@ -425,39 +425,35 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
         }
       }
     };
+    auto copy = [&](const uint16_t* from, unsigned char* to) __attribute__((always_inline)) {  // 16 bytes a lane
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, lds_ptr(to), 16, 0, 0);
+    };
     auto issue_raw = [&](int t, int base) __attribute__((always_inline)) {  // tokens past the last repeat it and are masked
       int lane = threadIdx.x & 63;  // (not known to be the same each time: the addresses are not kept over `attend`)
       asm volatile("" : "+v"(lane));
 #pragma unroll
-      for (int j = 0; j < RP / 8; ++j) {
-        const int i = 64 * (RP / 8 * w + j) + lane, k = i / RP, p = i % RP;
-        const int slot = list[min(t + k, k1 - 1) - base].x;
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void*)(a.cache + static_cast<int64_t>(slot) * DQ + 8 * p),
-            lds_ptr(lds1 + 1024 * (RP / 8 * w + j)), 16, 0, 0);
+      for (int j = 0; j < 8; ++j) {
+        const int k = 8 * w + j;
+        const int2 e = list[min(t + k, k1 - 1) - base];
+        const int slot = __builtin_amdgcn_readfirstlane(e.x), id = __builtin_amdgcn_readfirstlane(e.y);
+        copy(a.cache + static_cast<int64_t>(slot) * DQ + 8 * lane, lds1 + 1024 * k);
+        copy(a.gate + static_cast<int64_t>(id) * DC + 8 * lane, gate_s + 1024 * k);
       }
-#pragma unroll
-      for (int j = 0; j < GP / 8; ++j) {
-        const int i = 64 * (GP / 8 * w + j) + lane, k = i / GP, p = i % GP;
-        const int id = list[min(t + k, k1 - 1) - base].y;
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void*)(a.gate + static_cast<int64_t>(id) * DC + 8 * p),
-            lds_ptr(gate_s + 1024 * (GP / 8 * w + j)), 16, 0, 0);
-      }
+      const int slot = list[min(t + 8 * w + (lane >> 3), k1 - 1) - base].x;
+      copy(a.cache + static_cast<int64_t>(slot) * DQ + DC + 8 * (lane & 7), lds1 + 32 * 1024 + 1024 * w);
     };
     auto gate_tile = [&]() __attribute__((always_inline)) {  // raw rows and gate rows into the tile
-      int tid = threadIdx.x;
-      asm volatile("" : "+v"(tid));
-#pragma unroll 4
-      for (int j = 0; j < 32 * GP / kPrefixThreads; ++j) {
-        const int i = tid + j * kPrefixThreads, k = i / GP, p = i % GP;
-        *reinterpret_cast<u32x4_t*>(lds0 + k * C::LROW + prefix_latent_byte(k, p)) =
-            gate_chunk_f16(*reinterpret_cast<const u32x4_t*>(lds1 + k * DQ * 2 + 16 * p),
-                           *reinterpret_cast<const u32x4_t*>(gate_s + 16 * i));
+      int lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(lane));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = 8 * w + j, at = 1024 * k + 16 * lane;
+        *reinterpret_cast<u32x4_t*>(lds0 + k * C::LROW + prefix_latent_byte(k, lane)) =
+            gate_chunk_f16(*reinterpret_cast<const u32x4_t*>(lds1 + at), *reinterpret_cast<const u32x4_t*>(gate_s + at));
       }
-      const int k = tid / 8, p = tid % 8;
-      *reinterpret_cast<u32x4_t*>(lds0 + C::ROPE + k * C::RROW + prefix_rope_byte(k, p)) =
-          *reinterpret_cast<const u32x4_t*>(lds1 + k * DQ * 2 + DC * 2 + 16 * p);
+      const int k = 8 * w + (lane >> 3);
+      *reinterpret_cast<u32x4_t*>(lds0 + C::ROPE + k * C::RROW + prefix_rope_byte(k, lane & 7)) =
+          *reinterpret_cast<const u32x4_t*>(lds1 + 32 * 1024 + 1024 * w + 16 * lane);
     };
     for (int base = k0; base < k1; base += kOwnList) {
       fill_list(base);
