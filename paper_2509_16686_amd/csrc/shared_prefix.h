@@ -430,7 +430,8 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
     auto copy = [&](const uint16_t* from, unsigned char* to) __attribute__((always_inline)) {  // 16 bytes a lane
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, lds_ptr(to), 16, 0, 0);
     };
-    auto issue_raw = [&](int t, int base, unsigned char* tb) __attribute__((always_inline)) {  // tokens past the last repeat it and are masked
+    // (tokens past the last repeat it and are masked)
+    auto issue_raw = [&](int t, int base, unsigned char* tb) __attribute__((always_inline)) {
       int lane = threadIdx.x & 63;  // (not known to be the same each time: the addresses are not kept over `attend`)
       asm volatile("" : "+v"(lane));
 #pragma unroll
