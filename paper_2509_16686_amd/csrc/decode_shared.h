@@ -52,15 +52,15 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedPart pre, Sha
       float Mn = M;
 #pragma unroll
       for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, ml[u].x);  // repeats of the last row change no maximum
-      if (!(Mn > -INFINITY)) continue;                      // nothing weighs anything yet
-      const float keep = exp2f(M - Mn);
+      const bool any = Mn > -INFINITY;  // else nothing weighs anything yet; rows are added all the same, for a NaN's sake
+      const float keep = any ? exp2f(M - Mn) : 1.f;
       M = Mn;
       sum *= keep;
 #pragma unroll
       for (int k = 0; k < kSharedCols; ++k) acc[k] *= keep;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float e = s0 + u < ns ? exp2f(ml[u].x - Mn) : 0.f;  // exp2(-inf) = 0
+        const float e = any && s0 + u < ns ? exp2f(ml[u].x - Mn) : 0.f;  // exp2(-inf) = 0
         sum = fmaf(e, ml[u].y, sum);
 #pragma unroll
         for (int k = 0; k < kSharedCols; ++k) acc[k] = fmaf(e, v[u][k], acc[k]);
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedPart pre, Sha
   };
   if (pre.s_max > 0) fold(pre, static_cast<int64_t>(b) * H + h, static_cast<int64_t>(B) * H, pre.lens[0]);
   if (own.s_max > 0) fold(own, static_cast<int64_t>(b) * own.s_max * H + h, H, own.lens[b]);
-  const float inv = M > -INFINITY ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
   for (int k = 0; k < kSharedCols; ++k) {
     const int c = threadIdx.x + 256 * k;

@@ -479,9 +479,10 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
   }
 
   // O / l: lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row whose scores all
-  // overflowed to -inf (or that had no token) weighs nothing
+  // overflowed to -inf (or that had no token) weighs nothing; a NaN among them stays one
   const float l = half_sum(l_run);
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  const bool none = l == 0.f;
+  const float inv = none ? 0.f : 1.0f / l;
   int lane_e = tid & 63;  // (the row is formed anew: nothing of it is kept over the loops)
   asm volatile("" : "+v"(lane_e));
   const int he = lane_e >> 5, row_e = rb * kPrefixRows + 32 * w + (lane_e & 31);
@@ -491,7 +492,7 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
       const int H = a.blocks_per_seq * kPrefixRows, b = rb / a.blocks_per_seq;
       at = (static_cast<int64_t>(b) * a.s_max + split) * H + (row_e - b * H);
     }
-    if (he == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(l > 0.f ? m_run : -INFINITY, l);
+    if (he == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(none ? -INFINITY : m_run, l);
     uint16_t* orow = a.part_o + at * DC + 8 * he;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -664,18 +665,18 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
       }
     }
     __syncthreads();
-    // merged rows of the round's sequences (zero without tokens and past the batch)
+    // merged rows of the round's sequences (zero without tokens and past the batch; rows that weigh nothing are added
+    // all the same, for a NaN among them)
     for (int i = tid; i < spr * DC; i += kSharedMergeWaves * 64) {
       const int kk = i / DC, c = i - kk * DC;
       float top = -INFINITY, num = 0.f, den = 0.f;
       for (int p = 0; p < wps; ++p) top = fmaxf(top, m_part[kk * wps + p]);
-      if (top > -INFINITY)
-        for (int p = 0; p < wps; ++p) {
-          const float x = __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top);
-          num = fmaf(x, part[kk * wps + p][c], num);
-          den = fmaf(x, l_part[kk * wps + p], den);
-        }
-      const float v = top > -INFINITY ? num / den : 0.f;
+      for (int p = 0; p < wps; ++p) {
+        const float x = top > -INFINITY ? __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top) : 0.f;
+        num = fmaf(x, part[kk * wps + p][c], num);
+        den = fmaf(x, l_part[kk * wps + p], den);
+      }
+      const float v = den == 0.f ? 0.f : num / den;
       const __bf16 hi = static_cast<__bf16>(v);
       o_s[0][r0 + kk][c] = __builtin_bit_cast(uint16_t, hi);
       o_s[1][r0 + kk][c] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - static_cast<float>(hi)));
