@@ -542,8 +542,9 @@ eg_mla_status eg_mla_decode_shared(const eg_mla_dims* dims, int32_t batch, const
  * eg_mla_page_scores: for column j < ceil(seq_lens[b] / P) of sequence b
  *   scores[b, j] = max_h tau (q_lat[b,h] . mean_c + q^R[b,h] . mean_r)
  * with mean = page_means[p] of its page (clamped into the cache) and
- * q_lat[h] = W_UK[h]^T q^C[h]; -inf behind.  fp32 (bf16 storage: the absorbed
- * query enters the matrix products as three bf16 parts, which hold all of it).
+ * q_lat[h] = W_UK[h]^T q^C[h]; -inf behind.  NaN if a head's is.  fp32 (bf16
+ * storage: the absorbed query enters the matrix products as three bf16 parts,
+ * which hold all of it).
  *   q [B, H, d_h + d_r];  scores [B, max_pages_per_seq] fp32
  *   workspace  eg_mla_page_scores_workspace_size(dims, B) bytes, 256-byte aligned
  *

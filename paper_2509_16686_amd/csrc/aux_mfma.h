@@ -138,8 +138,11 @@ __device__ __forceinline__ void absorb_tile(const uint16_t* __restrict__ q, cons
         uint16_t p[3][4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+          // an infinity has no rest (infinity - infinity), and a finite value past bf16's largest keeps its upper bits
+          const bool inf = fabsf(x[r]) == INFINITY;
           p[0][r] = f32_to_bf16(x[r]);
-          const float left = x[r] - bf16_to_f32(p[0][r]);  // exact
+          if (!inf && fabsf(bf16_to_f32(p[0][r])) == INFINITY) p[0][r] = static_cast<uint16_t>(__float_as_uint(x[r]) >> 16);
+          const float left = inf ? 0.f : x[r] - bf16_to_f32(p[0][r]);  // exact
           p[1][r] = f32_to_bf16(left);
           p[2][r] = f32_to_bf16(left - bf16_to_f32(p[1][r]));
         }

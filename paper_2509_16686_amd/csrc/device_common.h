@@ -196,6 +196,8 @@ __device__ __forceinline__ float wave_max(float v) {
   for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
+// The larger of two values, NaN where one of them is (fmaxf drops it).
+__device__ __forceinline__ float max_or_nan(float a, float b) { return b > a || b != b ? b : a; }
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);

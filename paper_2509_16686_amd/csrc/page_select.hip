@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256) void page_scores_kernel(ScoreArgs a) {
 #pragma unroll
         for (int i = 0; i < 10; ++i)
           if (lane + 64 * i < a.DQ) s = fmaf(q[lane + 64 * i], m[i], s);
-        best = fmaxf(best, wave_sum(s) * a.scale);
+        best = max_or_nan(best, wave_sum(s) * a.scale);
       }
     }
     if (lane == 0) a.scores[static_cast<int64_t>(b) * a.W + j] = best;
@@ -178,6 +178,9 @@ __global__ __launch_bounds__(256) void page_scores_kernel(ScoreArgs a) {
 // three parts hold all of the fp32 query, so the scores are fp32 ones.  HW
 // waves share a tile of TPW x 16 pages, each with every HW-th block of 16
 // heads, and join their maxima in LDS; the other 8 / HW take the next tiles.
+// An infinite mean times a zero part, or times parts of both signs, is a NaN
+// that the fp32 product does not have: NaN scores are formed again from the
+// whole query.
 // Bound by latency for few heads, and by the query's parts through L2 for many
 // (6 d_c + 2 d_r bytes a head, read once per tile of pages).
 constexpr int kScoreWaves = 8;
@@ -309,13 +312,36 @@ __global__ __launch_bounds__(kScoreWaves * 64) void page_scores_mfma_kernel(Scor
       }
       // lane: heads h0 + 4 g + 0..3 of page r16
 #pragma unroll
-      for (int t = 0; t < TPW; ++t)
+      for (int t = 0; t < TPW; ++t) {
+        bool lost = false;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lost = lost || (h0 + 4 * g + r < H && acc[t][r] != acc[t][r]);
+        if (lost) {
+          const uint16_t* m = a.means + score_page(a.s, b, min(p0 + 16 * t + r16, pages - 1)) * DQ;
+          f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+          for (int c = 0; c < DQ; ++c) {
+            const float mv = bf16_to_f32(m[c]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int h = min(h0 + 4 * g + r, H - 1);
+              float q = bf16_to_f32(a.parts[layout(b, h, 0, c)]);
+              if (c < DC) q += bf16_to_f32(a.parts[layout(b, h, 1, c)]) + bf16_to_f32(a.parts[layout(b, h, 2, c)]);
+              s[r] = fmaf(q, mv, s[r]);
+            }
+          }
+          acc[t] = s;
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (h0 + 4 * g + r < H) best[t] = fmaxf(best[t], acc[t][r]);
+          if (h0 + 4 * g + r < H) best[t] = max_or_nan(best[t], acc[t][r]);
+      }
     }
 #pragma unroll
-    for (int t = 0; t < TPW; ++t) best[t] = max_over_row_groups(best[t]) * a.s.scale;
+    for (int t = 0; t < TPW; ++t) {  // over the lanes of a page
+      best[t] = max_or_nan(best[t], __shfl_xor(best[t], 16, 64));
+      best[t] = max_or_nan(best[t], __shfl_xor(best[t], 32, 64)) * a.s.scale;
+    }
   }
   if constexpr (HW > 1) {
     if (g == 0) {
@@ -326,7 +352,7 @@ __global__ __launch_bounds__(kScoreWaves * 64) void page_scores_mfma_kernel(Scor
     if (w % HW) return;
 #pragma unroll
     for (int t = 0; t < TPW; ++t)
-      for (int k = 1; k < HW; ++k) best[t] = fmaxf(best[t], best_s[w + k][16 * t + r16]);
+      for (int k = 1; k < HW; ++k) best[t] = max_or_nan(best[t], best_s[w + k][16 * t + r16]);
   }
 #pragma unroll
   for (int t = 0; t < TPW; ++t) {
