@@ -155,10 +155,8 @@ SplitArgs shared_split_args(const SharedCall& c, int part, const float* qfull, S
 
 hipError_t launch_shared_part(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {
   const SplitArgs a = shared_split_args(c, part, qfull, rows);
-  eg_mla_dims ds = c.d;
-  ds.num_heads = a.H;
   const OneArgs one{c.q, c.w_uk, c.w_uv, c.out, c.d.v_head_dim, 1, 1};
-  return launch_split(ds, part ? c.p.own : c.p.pre, a, one, c.stream, nullptr, nullptr);
+  return launch_split(c.d, part ? c.p.own : c.p.pre, a, one, c.stream, nullptr, nullptr);
 }
 
 // Both parts on the fp32 matrix-core kernel: one launch.

@@ -82,8 +82,9 @@ eg_mla_status check_dims(const eg_mla_dims* d) {
 }
 
 eg_mla_status make_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,
-                               const eg_mla_plan* plan, DecodePlan* out, PlanRows rows_rule) {
+                               const eg_mla_plan* plan, DecodePlan* out, PlanRows rows_rule, int32_t query_rows) {
   DecodePlan p;
+  const int heads = query_rows > 0 ? query_rows : d.num_heads;
   const int forced = plan ? plan->path : EG_MLA_PATH_AUTO;
   if (forced != EG_MLA_PATH_AUTO && forced != EG_MLA_PATH_VALU && forced != EG_MLA_PATH_MFMA)
     return EG_MLA_ERR_INVALID_ARG;
@@ -105,9 +106,9 @@ eg_mla_status make_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     p.heads_per_group = 16;
   } else {
     // Heads per VALU work item: at most 8192 latent accumulators per workgroup.
-    p.heads_per_group = std::max(1, std::min({d.num_heads, 8192 / d.latent_dim, 256}));
+    p.heads_per_group = std::max(1, std::min({heads, 8192 / d.latent_dim, 256}));
   }
-  p.head_groups = ceil_div(d.num_heads, p.heads_per_group);
+  p.head_groups = ceil_div(heads, p.heads_per_group);
 
   const int req_slices = plan ? plan->id_slices : 0;
   if (req_slices != 0 && req_slices != 1 && req_slices != kIdSlices) return EG_MLA_ERR_INVALID_ARG;
@@ -183,7 +184,7 @@ eg_mla_status make_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
   // work-groups are resident at once.
   p.one_launch = p.f32_mfma && (plan == nullptr || plan->split_tokens == 0) && p.capacity > 0 &&
                  p.capacity <= kOneMaxTokens && d.latent_dim <= kOneMaxLatent &&
-                 static_cast<int64_t>(std::min(d.num_heads, 16)) * std::max(d.head_dim, d.v_head_dim) * d.latent_dim *
+                 static_cast<int64_t>(std::min(heads, 16)) * std::max(d.head_dim, d.v_head_dim) * d.latent_dim *
                          elem_bytes(d) <= kOneMaxWeightBytes &&
                  static_cast<int64_t>(std::max(batch, 0)) * p.head_groups <= kTargetWorkItemsF32;
   // The head-split kernel balances tokens over its work-groups whatever the
@@ -192,7 +193,7 @@ eg_mla_status make_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
   if (p.balanced && (plan == nullptr || plan->split_tokens == 0)) p.split_tokens = kMaxSplitTokens;
 
   const size_t B = static_cast<size_t>(std::max(batch, 0));
-  const size_t H = static_cast<size_t>(d.num_heads);
+  const size_t H = static_cast<size_t>(heads);
   const size_t DQ = static_cast<size_t>(d.latent_dim + d.rope_dim);
   // The split kernel absorbs the query itself when that costs each work-group
   // at most 2 heads' W_UK (8 or more splits per sequence, the first 16 of them
@@ -671,19 +672,21 @@ eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const f
 
 namespace {
 
-// The split kernel of one part of a shared decode: the decode's plan without
-// its absorption, schedules and single-launch form (the call absorbs once for
-// both parts and merges them itself).  The wide kernel, with its schedule,
-// stays where the tiled prefix kernel prepares both (`wide`).
-eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages, bool wide, DecodePlan* p) {
-  const eg_mla_status st = make_decode_plan(d, batch, max_pages, nullptr, p);
+// The split kernel of one part of a shared decode, `rows` query rows a
+// sequence: the decode's plan without its absorption, schedules and
+// single-launch form (the call absorbs once for both parts and merges them
+// itself).  The wide kernel, with its schedule, stays where the tiled prefix
+// kernel prepares both (`wide`).
+eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t rows, int32_t max_pages, bool wide,
+                               DecodePlan* p) {
+  const eg_mla_status st = make_decode_plan(d, batch, max_pages, nullptr, p, PlanRows::kFast, rows);
   if (st != EG_MLA_OK) return st;
   p->fused_absorb = p->one_launch = p->tok_balanced = false;
   p->pieces = 0;
   if (p->balanced && !wide) {
     p->balanced = false;
     p->heads_per_group = 16;
-    p->head_groups = ceil_div(d.num_heads, 16);
+    p->head_groups = ceil_div(rows, 16);
     const int64_t s = ceil_div(static_cast<int64_t>(batch) * std::max(p->capacity, 1) * p->head_groups, kTargetWorkItems);
     p->split_tokens = static_cast<int>(std::min<int64_t>(std::max<int64_t>((s + kTile - 1) / kTile * kTile, 256), kMaxSplitTokens));
     p->s_max = ceil_div(std::max(p->capacity, 1), p->split_tokens);
@@ -693,7 +696,7 @@ eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     while (p->heads_per_group > 1 &&
            4 * static_cast<int64_t>(p->heads_per_group) * (d.latent_dim + d.rope_dim + kTile + 1) > 64 * 1024)
       p->heads_per_group /= 2;
-    p->head_groups = ceil_div(d.num_heads, p->heads_per_group);
+    p->head_groups = ceil_div(rows, p->heads_per_group);
   }
   if (p->capacity > 0 && static_cast<int64_t>(batch) * p->s_max * p->head_groups > 0x7fffffff)
     return EG_MLA_ERR_UNSUPPORTED;
@@ -713,12 +716,12 @@ constexpr int64_t kPrefixFewTiles = 2048;
 // tiles cost the prefix 6 %, more than hiding the own tokens gains beyond.
 constexpr int64_t kBothMaxTiles = 16384;
 
-// Tiled prefix attention: its shapes, whatever the rows (one sequence of 16
-// heads, an eighth of a row block, prefix 8000: 19.7 us against 86 with the
-// decode's split kernel, whose merge reads its many partial rows).
+// Tiled prefix attention: the layers that the decode takes with the same
+// roundings, whatever the rows (one sequence of 16 heads, an eighth of a row
+// block, prefix 8000: 19.7 us against 86 with the decode's split kernel, whose
+// merge reads its many partial rows).
 bool prefix_tiled(const eg_mla_dims& d) {
-  return d.dtype == EG_MLA_BF16 && d.head_dim == 128 && d.v_head_dim == 128 && d.rope_dim == 64 &&
-         (d.latent_dim == 128 || d.latent_dim == 320 || d.latent_dim == 512);
+  return mfma_shape_supported(d) && d.head_dim == 128 && d.v_head_dim == 128;
 }
 
 }  // namespace
@@ -729,11 +732,9 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
   // all heads of all sequences are the prefix's heads; merge grid
   const int64_t rows64 = static_cast<int64_t>(batch) * d.num_heads;
   if (rows64 > (1 << 30) || batch > 65535) return EG_MLA_ERR_UNSUPPORTED;
-  eg_mla_dims all = d;
-  all.num_heads = std::max(1, batch * d.num_heads);
-  eg_mla_status st = shared_part_plan(all, 1, max_prefix_pages, false, &p.pre);
+  eg_mla_status st = shared_part_plan(d, 1, std::max(1, batch * d.num_heads), max_prefix_pages, false, &p.pre);
   p.tiled = p.pre.capacity > 0 && rows64 > 0 && prefix_tiled(d);
-  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, max_pages_per_seq, p.tiled, &p.own);
+  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, d.num_heads, max_pages_per_seq, p.tiled, &p.own);
   if (st != EG_MLA_OK) return st;
   const size_t rows = static_cast<size_t>(rows64), dc = static_cast<size_t>(d.latent_dim), dq = dc + d.rope_dim;
   size_t off = 0;

@@ -84,9 +84,11 @@ eg_mla_status check_dims(const eg_mla_dims* d);
 
 // Resolves `plan` (NULL = automatic) for a decode call.  Returns
 // EG_MLA_ERR_UNSUPPORTED when a forced path is unavailable for the shape.
+// `query_rows` > 0: rows of a sequence, where they are not the layer's heads (a
+// shared prefix); the kernels, and with them the arithmetic, are the layer's.
 eg_mla_status make_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,
                                const eg_mla_plan* plan, DecodePlan* out,
-                               PlanRows rows = PlanRows::kFast);
+                               PlanRows rows = PlanRows::kFast, int32_t query_rows = 0);
 // The plan for a call with `workspace_bytes` of workspace (EG_MLA_ERR_WORKSPACE if
 // neither the fast plan nor the one with few rows fits), and the size to ask for.
 eg_mla_status fit_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq, const eg_mla_plan* plan,
