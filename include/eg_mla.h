@@ -511,7 +511,8 @@ eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_tokens, con
  *              max_prefix_pages) bytes, 256-byte aligned, no initialisation
  *              (a smaller batch or context may ask for more); calls that share
  *              it must be ordered.
- * Arithmetic as for eg_mla_decode (any shape and storage type).  out is
+ * Arithmetic as for eg_mla_decode (any shape and storage type): the kernels
+ * are chosen from the layer, whatever the batch.  out is
  * 16-byte aligned.  batch above 65535 is EG_MLA_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------------- */
 size_t eg_mla_decode_shared_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_pages_per_seq,

@@ -220,7 +220,7 @@ hipError_t launch_tiled(const SharedCall& c) {
   a.tiles = pa.tiles;
   a.len = c.prefix_len;
   a.part_ml = reinterpret_cast<float*>(c.ws + p.pre.off_ml);
-  a.part_o = reinterpret_cast<uint16_t*>(c.ws + p.pre.off_o);
+  a.part_o = c.ws + p.pre.off_o;
   a.cap = p.pre.capacity;
   a.rows = c.batch * d.num_heads;
   a.row_blocks = p.row_blocks;
@@ -233,10 +233,11 @@ hipError_t launch_tiled(const SharedCall& c) {
     const int own_wgs = c.batch * p.own.s_max * p.own.head_groups;
     hipLaunchKernelGGL(shared_both_kernel, dim3(prefix_wgs + own_wgs), dim3(kPrefixThreads), 0, c.stream, a, so, own_wgs);
   } else {
-    auto attend = shared_prefix_kernel<DC, DC == 512 ? 32 : 64, false>;
+    auto attend = shared_prefix_kernel<DC, DC == 512 ? 32 : 64, false, false>;
     if constexpr (DC == 512) {
+      if (p.half_rows) attend = shared_prefix_kernel<DC, 32, false, true>;
       if (p.fused) {
-        attend = shared_prefix_kernel<DC, 32, true>;
+        attend = shared_prefix_kernel<DC, 32, true, true>;
         a.cache = pa.cache;
         a.ids = c.ids;
         a.gate = pa.gate;
@@ -261,8 +262,8 @@ hipError_t launch_tiled(const SharedCall& c) {
       const hipError_t e = set_lds(combine_wide_kernel, combine_wide_lds_bytes());
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(combine_wide_kernel, dim3(d.num_heads, (c.batch + kCombWideSeq - 1) / kCombWideSeq),
-                         dim3(kCombWideWaves * 64), combine_wide_lds_bytes(), c.stream, a.part_ml, a.part_o,
-                         static_cast<const uint16_t*>(c.w_uv), pa.split_rows, static_cast<uint16_t*>(c.out), c.batch,
+                         dim3(kCombWideWaves * 64), combine_wide_lds_bytes(), c.stream, a.part_ml,
+                         static_cast<const uint16_t*>(a.part_o), static_cast<const uint16_t*>(c.w_uv), pa.split_rows, static_cast<uint16_t*>(c.out), c.batch,
                          d.num_heads);
       return hipGetLastError();
     }
@@ -276,7 +277,7 @@ hipError_t launch_tiled(const SharedCall& c) {
   m.own_ml = own.ml;
   m.own_o = own.o;
   m.own_lens = own.lens;
-  m.own_rows = seq_rows;
+  m.own_rows = wide ? seq_rows : nullptr;
   m.w_uv = static_cast<const uint16_t*>(c.w_uv);
   m.out = static_cast<uint16_t*>(c.out);
   m.B = c.batch;
@@ -290,7 +291,7 @@ hipError_t launch_tiled(const SharedCall& c) {
   m.spw = kSharedMergeSeq;
   while (m.spw > 1 && static_cast<int64_t>(d.num_heads) * ((c.batch + m.spw - 1) / m.spw) < kSharedMergeGroups) m.spw /= 2;
   auto merge = shared_merge_kernel<DC, false>;
-  if constexpr (DC == 512) merge = wide ? shared_merge_kernel<DC, true> : merge;
+  if constexpr (DC == 512) merge = p.half_rows ? shared_merge_kernel<DC, true> : merge;
   hipLaunchKernelGGL(merge, dim3(d.num_heads, (c.batch + m.spw - 1) / m.spw), dim3(kSharedMergeWaves * 64), 0, c.stream, m);
   return hipGetLastError();
 }

@@ -754,12 +754,13 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     p.splits = std::max(1, std::min((work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d)) / p.row_blocks, tiles));
     if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x3fffffff) return EG_MLA_ERR_UNSUPPORTED;
     p.fused = d.latent_dim == 512 && d.num_heads % kPrefixRows == 0;  // a row block within a sequence
+    p.half_rows = heads_kernel_shape(d);
     p.off_half = take(rows * dq * 2);
     if (!p.own.balanced) p.off_q = take(rows * dq * 4);
     p.off_tiles = take(static_cast<size_t>(tiles) * p.keys * (prefix_latent_row(d.latent_dim) + 128));
     if (p.fused) p.off_rows = take(static_cast<size_t>(batch) * 8);
     p.pre.off_ml = take(rows * p.splits * 8);
-    p.pre.off_o = take(rows * p.splits * dc * 2);
+    p.pre.off_o = take(rows * p.splits * dc * (p.half_rows ? 2 : 4));
   } else {
     p.off_q = take(rows * dq * 4);
     const size_t n = p.pre.capacity > 0 ? rows * static_cast<size_t>(p.pre.s_max) : 0;

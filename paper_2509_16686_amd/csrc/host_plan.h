@@ -203,6 +203,7 @@ struct SharedPlan {
   bool tiled = false;    // the prefix on the tiled kernel, in at most `splits` runs of tiles (pre: capacity and offsets)
   bool fused = false;    // ... which takes the own tokens too
   bool both = false;     // d_c 128: prefix and own tokens in one launch
+  bool half_rows = false;  // partial rows O / l in fp16, as the head-split kernel's, instead of fp32 sums
   int keys = 0;          // of a prefix tile
   int row_blocks = 0, splits = 0;
   size_t off_q = 0;      // fp32 [B, H, d_c + d_r] (not tiled, or own tokens not on the wide kernel)

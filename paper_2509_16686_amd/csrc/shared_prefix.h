@@ -24,8 +24,10 @@
 // rows), online softmax per row in the log2 domain with lazy rescale, values
 // O^T[dim][row] += C~^T P^T with the probabilities as the B operand as they
 // lie in the score accumulators and transposed LDS reads as the A operand.
-// Each LDS byte read feeds 32 rows.  A partial row is O / l in fp16 (a convex
-// combination of fp16 values) with its maximum and sum in fp32.
+// Each LDS byte read feeds 32 rows.  A partial row is as the layer's decode has
+// it: the fp32 sums O with their maximum and sum l, or, for the layers of the
+// head-split kernel (d_c 512, heads a multiple of 64), O / l in fp16, a convex
+// combination of fp16 values.
 #pragma once
 
 namespace egmla {
@@ -150,7 +152,7 @@ struct PrefixArgs {
   const unsigned char* tiles;  // PrefixCfg<DC>::TILE bytes each
   const int32_t* len;
   float* part_ml;              // [s_max][rows][2]; OWN: [B][s_max][H][2]
-  uint16_t* part_o;            // [s_max][rows][DC] fp16: O / l; OWN: [B][s_max][H][DC]
+  void* part_o;                // [s_max][rows][DC] fp32: O, or (HALF) fp16: O / l; OWN: [B][s_max][H][DC]
   int32_t cap, rows, row_blocks, s_max;
   float scale_log2;
   // OWN: each sequence's own tokens
@@ -187,8 +189,8 @@ __device__ __forceinline__ float half_sum(float x) {
 // piece's address formed twice: prefix 8000 x 64 x 128 heads with up to 1500 own tokens 208.5 us a call, 203.5 so).
 constexpr int kOwnList = 512;  // own tokens listed at a time
 
-// Work-group `bid` of `nblocks`.
-template <int DC, int KEYS, bool OWN>
+// Work-group `bid` of `nblocks`.  HALF: the form of the partial rows.
+template <int DC, int KEYS, bool OWN, bool HALF>
 __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nblocks) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass knows neither the copies to LDS nor the register constraints
   using C = PrefixCfg<DC, KEYS>;
@@ -478,11 +480,11 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
     }
   }
 
-  // O / l: lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row whose scores all
-  // overflowed to -inf (or that had no token) weighs nothing; a NaN among them stays one
+  // lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row whose scores all overflowed to -inf
+  // (or that had no token) weighs nothing; a NaN among them stays one
   const float l = half_sum(l_run);
   const bool none = l == 0.f;
-  const float inv = none ? 0.f : 1.0f / l;
+  [[maybe_unused]] const float inv = none ? 0.f : 1.0f / l;
   int lane_e = tid & 63;  // (the row is formed anew: nothing of it is kept over the loops)
   asm volatile("" : "+v"(lane_e));
   const int he = lane_e >> 5, row_e = rb * kPrefixRows + 32 * w + (lane_e & 31);
@@ -493,23 +495,33 @@ __device__ __forceinline__ void prefix_item(const PrefixArgs& a, int bid, int nb
       at = (static_cast<int64_t>(b) * a.s_max + split) * H + (row_e - b * H);
     }
     if (he == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(none ? -INFINITY : m_run, l);
-    uint16_t* orow = a.part_o + at * DC + 8 * he;
+    if constexpr (HALF) {
+      uint16_t* orow = static_cast<uint16_t*>(a.part_o) + at * DC + 8 * he;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+      for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        *reinterpret_cast<u32x4_t*>(orow + 32 * db + 16 * j) =
-            u32x4_t{pack_f16x2(o[db][8 * j] * inv, o[db][8 * j + 1] * inv),
-                    pack_f16x2(o[db][8 * j + 2] * inv, o[db][8 * j + 3] * inv),
-                    pack_f16x2(o[db][8 * j + 4] * inv, o[db][8 * j + 5] * inv),
-                    pack_f16x2(o[db][8 * j + 6] * inv, o[db][8 * j + 7] * inv)};
+        for (int j = 0; j < 2; ++j)
+          *reinterpret_cast<u32x4_t*>(orow + 32 * db + 16 * j) =
+              u32x4_t{pack_f16x2(o[db][8 * j] * inv, o[db][8 * j + 1] * inv),
+                      pack_f16x2(o[db][8 * j + 2] * inv, o[db][8 * j + 3] * inv),
+                      pack_f16x2(o[db][8 * j + 4] * inv, o[db][8 * j + 5] * inv),
+                      pack_f16x2(o[db][8 * j + 6] * inv, o[db][8 * j + 7] * inv)};
+    } else {
+      float* orow = static_cast<float*>(a.part_o) + at * DC + 8 * he;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<f32x4_t*>(orow + 32 * db + 16 * (j >> 1) + 4 * (j & 1)) =
+              f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+    }
   }
 #endif
 }
 
-template <int DC, int KEYS, bool OWN>
+template <int DC, int KEYS, bool OWN, bool HALF>
 __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_prefix_kernel(PrefixArgs a) {
-  prefix_item<DC, KEYS, OWN>(a, blockIdx.x, gridDim.x);
+  prefix_item<DC, KEYS, OWN, HALF>(a, blockIdx.x, gridDim.x);
 }
 
 // Both parts of a short call in one launch (d_c 128): the first own_wgs
@@ -519,7 +531,7 @@ __global__ __launch_bounds__(kPrefixThreads, DC == 128 ? 2 : 1) void shared_pref
 __global__ __launch_bounds__(kPrefixThreads, 2) void shared_both_kernel(PrefixArgs a, SplitArgs own, int own_wgs) {
   const int bid = blockIdx.x;
   if (bid < own_wgs) split_slice_item<128, 64, 4, 2, 1, false, false, kBothList>(own, bid, own_wgs);
-  else prefix_item<128, 32, false>(a, bid - own_wgs, gridDim.x - own_wgs);
+  else prefix_item<128, 32, false, false>(a, bid - own_wgs, gridDim.x - own_wgs);
 }
 
 // ---------------------------------------------------------------------------
@@ -543,19 +555,19 @@ struct Batch {
 
 struct SharedMergeArgs {
   const float* pre_ml;      // [rows][2]: split i of sequence b and head h at row i pre_step + b pre_seq + h
-  const uint16_t* pre_o;    // [rows][DC] fp16, normalised
+  const void* pre_o;        // [rows][DC] fp32 sums; HALF: fp16, normalised
   const int32_t* pre_len;   // null: a row in every split
   int64_t pre_step, pre_seq;
   const float* own_ml;
-  const void* own_o;        // fp32 sums, [B][own_s_max][H][DC]; WIDE: fp16, normalised, rows of own_rows
-  const int32_t* own_lens;  // null: no own tokens
-  const int2* own_rows;     // WIDE
+  const void* own_o;        // fp32 sums, [B][own_s_max][H][DC]; HALF: fp16, normalised, rows of own_rows
+  const int32_t* own_lens;  // null: no own tokens (HALF: not used)
+  const int2* own_rows;     // HALF; null: no own tokens' rows
   const uint16_t* w_uv;
   uint16_t* out;
   int32_t B, H, pre_cap, pre_s_max, own_cap, own_split, own_s_max, spw, keys;
 };
 
-template <int DC, bool WIDE>
+template <int DC, bool HALF>
 __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(SharedMergeArgs a) {
   constexpr int DV = 128, NKC = DC / 32, OS = DC + 8;
   constexpr int LPR = DC / 8, GPW = 64 / LPR;       // lanes per row, rows (workers) per wave
@@ -586,7 +598,7 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
     const int b = b0 + k;
     float M = -INFINITY, sum = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     // rows me, me + wps, ... < n of a part, U at a time; load(i, ml, v) reads row i
-    auto fold_by = [&](auto batch, int n, bool normalised, auto load) {
+    auto fold_by = [&](auto batch, int n, auto load) {
       constexpr int U = decltype(batch)::value;
       for (int i0 = me; i0 < n; i0 += wps * U) {
         float2 ml[U];
@@ -605,52 +617,49 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
         for (int u = 0; u < U; ++u) {
           const float x = any && i0 + u * wps < n ? __builtin_amdgcn_exp2f(ml[u].x - top) : 0.f;
           sum = fmaf(x, ml[u].y, sum);
-          const float y = normalised ? x * ml[u].y : x;
+          const float y = HALF ? x * ml[u].y : x;
 #pragma unroll
           for (int e = 0; e < 8; ++e) acc[e] = fmaf(y, v[u][e], acc[e]);
         }
         M = top;
       }
     };
-    auto fold = [&](int n, bool normalised, auto load) {
-      if (n <= 2 * wps) fold_by(Batch<2>{}, n, normalised, load);
-      else if (n <= 4 * wps) fold_by(Batch<4>{}, n, normalised, load);
-      else fold_by(Batch<8>{}, n, normalised, load);
+    auto fold = [&](int n, auto load) {
+      if (n <= 2 * wps) fold_by(Batch<2>{}, n, load);
+      else if (n <= 4 * wps) fold_by(Batch<4>{}, n, load);
+      else fold_by(Batch<8>{}, n, load);
     };
-    auto half_row = [&](const uint16_t* p, float (&v)[8]) {
-      const f16x8_t x = *reinterpret_cast<const f16x8_t*>(p + col);
+    auto row = [&](const float* part_ml, const void* part_o, int64_t at, float2& ml, float (&v)[8]) {
+      ml = *reinterpret_cast<const float2*>(part_ml + 2 * at);
+      if constexpr (HALF) {
+        const f16x8_t x = *reinterpret_cast<const f16x8_t*>(static_cast<const uint16_t*>(part_o) + at * DC + col);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
+      } else {
+        const f32x4_t* p = reinterpret_cast<const f32x4_t*>(static_cast<const float*>(part_o) + at * DC + col);
+        const f32x4_t x = p[0], y = p[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = x[e];
+          v[4 + e] = y[e];
+        }
+      }
     };
     if (live && k < nseq) {
       const int64_t pre0 = b * a.pre_seq + h;
-      auto pre_row = [&](int i, float2& ml, float (&v)[8]) {
-        const int64_t at = i * a.pre_step + pre0;
-        ml = *reinterpret_cast<const float2*>(a.pre_ml + 2 * at);
-        half_row(a.pre_o + at * DC, v);
-      };
-      if constexpr (WIDE) {  // both parts' rows have the same form: one list
-        const int2 list = a.own_rows[b];
-        fold(pre_n + list.y, true, [&](int i, float2& ml, float (&v)[8]) {
+      if constexpr (HALF) {  // one list
+        const int2 list = a.own_rows ? a.own_rows[b] : make_int2(0, 0);
+        fold(pre_n + list.y, [&](int i, float2& ml, float (&v)[8]) {
           const bool own = i >= pre_n;
           const int64_t at = own ? static_cast<int64_t>(list.x + i - pre_n) * a.H + h : i * a.pre_step + pre0;
-          ml = *reinterpret_cast<const float2*>((own ? a.own_ml : a.pre_ml) + 2 * at);
-          half_row((own ? static_cast<const uint16_t*>(a.own_o) : a.pre_o) + at * DC, v);
+          row(own ? a.own_ml : a.pre_ml, own ? a.own_o : a.pre_o, at, ml, v);
         });
       } else {
-        fold(pre_n, true, pre_row);
+        fold(pre_n, [&](int i, float2& ml, float (&v)[8]) { row(a.pre_ml, a.pre_o, i * a.pre_step + pre0, ml, v); });
         if (a.own_lens) {
           const int L = clamp_len(a.own_lens[b], a.own_cap);
-          fold(min((L + a.own_split - 1) / a.own_split, a.own_s_max), false, [&](int i, float2& ml, float (&v)[8]) {
-            const int64_t at = (static_cast<int64_t>(b) * a.own_s_max + i) * a.H + h;
-            ml = *reinterpret_cast<const float2*>(a.own_ml + 2 * at);
-            const f32x4_t* p = reinterpret_cast<const f32x4_t*>(static_cast<const float*>(a.own_o) + at * DC + col);
-            const f32x4_t x = p[0], y = p[1];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[e] = x[e];
-              v[4 + e] = y[e];
-            }
+          fold(min((L + a.own_split - 1) / a.own_split, a.own_s_max), [&](int i, float2& ml, float (&v)[8]) {
+            row(a.own_ml, a.own_o, (static_cast<int64_t>(b) * a.own_s_max + i) * a.H + h, ml, v);
           });
         }
       }
