@@ -751,10 +751,12 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
              static_cast<int64_t>(batch) * p.own.s_max * p.own.head_groups < (1 << 30);
     p.keys = d.latent_dim == 512 || p.both ? 32 : 64;
     const int tiles = ceil_div(p.pre.capacity, p.keys);
-    p.splits = std::max(1, std::min((work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d)) / p.row_blocks, tiles));
-    if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x3fffffff) return EG_MLA_ERR_UNSUPPORTED;
     p.fused = d.latent_dim == 512 && d.num_heads % kPrefixRows == 0;  // a row block within a sequence
     p.half_rows = heads_kernel_shape(d);
+    // the fused kernel's work-groups take the own tokens too, whose tiles may be the more
+    const int most = p.fused ? std::max(tiles, ceil_div(p.own.capacity, 32)) : tiles;
+    p.splits = std::max(1, std::min((work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d)) / p.row_blocks, most));
+    if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x3fffffff) return EG_MLA_ERR_UNSUPPORTED;
     p.off_half = take(rows * dq * 2);
     if (!p.own.balanced) p.off_q = take(rows * dq * 4);
     p.off_tiles = take(static_cast<size_t>(tiles) * p.keys * (prefix_latent_row(d.latent_dim) + 128));

@@ -38,3 +38,16 @@ LAYERS = [(16, 128, 128, 128, 64, 1), (128, 128, 128, 512, 64, 1), (16, 128, 128
 def test_kernels_are_the_layers(shared_plan, layer):
     """Whatever the batch, both parts run on the kernels of the layer's decode, and so with its arithmetic."""
     assert shared_plan("layer", *layer) == (0,)
+
+
+H128 = (128, 128, 128, 512, 64, 1)
+
+
+@pytest.mark.parametrize("page,batch,pages,prefix,splits", [
+    (64, 1, 64, 1, 128), (16, 8, 250, 1, 32), (64, 4, 1024, 4, 64), (32, 2, 3, 1, 3),  # few prefix tiles, many own ones
+    (64, 64, 24, 125, 4), (64, 1, 1, 125, 250), (64, 300, 64, 1, 1), (32, 1, 0, 5, 5),
+])
+def test_splits_of_the_fused_kernel_follow_the_longer_part(shared_plan, page, batch, pages, prefix, splits):
+    """Its work-groups take own tokens as well as the prefix's: as many as fill the chip while either part has tiles."""
+    got = shared_plan("plan", *H128, page, batch, pages, prefix)
+    assert got[3:7] == (1, 1, splits, batch)
