@@ -505,7 +505,8 @@ eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_tokens, con
  *   seq_lens [B], page_table [B, max_pages_per_seq] or NULL (contiguous own
  *   rows: token j of sequence b is row b * max_pages_per_seq * P + j): OWN
  *   tokens, the prefix not counted.  max_prefix_pages or max_pages_per_seq may
- *   be 0 (prefix_len and prefix_table, or seq_lens, may then be NULL).
+ *   be 0 (prefix_len and prefix_table, or seq_lens, may then be NULL); without
+ *   prefix pages the call is eg_mla_decode.
  *   The other arguments are those of eg_mla_decode.
  *   workspace  eg_mla_decode_shared_workspace_size(dims, B, max_pages_per_seq,
  *              max_prefix_pages) bytes, 256-byte aligned, no initialisation

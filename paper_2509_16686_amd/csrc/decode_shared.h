@@ -298,6 +298,9 @@ hipError_t launch_tiled(const SharedCall& c) {
 
 eg_mla_status run_decode_shared(const SharedCall& c) {
   const eg_mla_dims& d = c.d;
+  if (c.p.plain)
+    return run_decode(d, c.p.own, c.batch, c.q, c.cache, c.ids, c.gate, c.w_uk, c.w_uv, c.seq_lens, c.page_table,
+                      c.max_pages, c.num_slots, c.ws, c.out, c.stream, nullptr);
   (void)hipGetLastError();
   if (c.p.tiled) {
     const hipError_t e = d.latent_dim == 128   ? launch_tiled<128>(c)

@@ -732,6 +732,13 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
   // all heads of all sequences are the prefix's heads; merge grid
   const int64_t rows64 = static_cast<int64_t>(batch) * d.num_heads;
   if (rows64 > (1 << 30) || batch > 65535) return EG_MLA_ERR_UNSUPPORTED;
+  if (max_prefix_pages == 0 && max_pages_per_seq > 0) {
+    p.plain = true;
+    p.bytes = decode_workspace_bytes(d, batch, max_pages_per_seq, nullptr);
+    const eg_mla_status st = make_decode_plan(d, batch, max_pages_per_seq, nullptr, &p.own);
+    *out = p;
+    return st;
+  }
   eg_mla_status st = shared_part_plan(d, 1, std::max(1, batch * d.num_heads), max_prefix_pages, false, &p.pre);
   p.tiled = p.pre.capacity > 0 && rows64 > 0 && prefix_tiled(d);
   if (st == EG_MLA_OK) st = shared_part_plan(d, batch, d.num_heads, max_pages_per_seq, p.tiled, &p.own);

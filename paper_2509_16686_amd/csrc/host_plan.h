@@ -200,6 +200,7 @@ constexpr int kPrefixRows = 128;  // query rows of its work-groups
 constexpr int prefix_latent_row(int dc) { return (2 * dc + 255) / 256 * 256; }  // bytes of a key's latent in a tile
 struct SharedPlan {
   DecodePlan pre, own;
+  bool plain = false;    // no prefix in the tables: the decode of the own tokens, by its own plan `own`
   bool tiled = false;    // the prefix on the tiled kernel, in at most `splits` runs of tiles (pre: capacity and offsets)
   bool fused = false;    // ... which takes the own tokens too
   bool both = false;     // d_c 128: prefix and own tokens in one launch
