@@ -510,8 +510,9 @@ eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_tokens, con
  *   The other arguments are those of eg_mla_decode.
  *   workspace  eg_mla_decode_shared_workspace_size(dims, B, max_pages_per_seq,
  *              max_prefix_pages) bytes, 256-byte aligned, no initialisation
- *              (a smaller batch or context may ask for more); calls that share
- *              it must be ordered.
+ *              (no less than for a smaller batch or fewer pages: one sized at a
+ *              server's largest serves its smaller calls); calls that share it
+ *              must be ordered.
  * Arithmetic as for eg_mla_decode (any shape and storage type): the kernels
  * are chosen from the layer, whatever the batch.  out is
  * 16-byte aligned.  batch above 65535 is EG_MLA_ERR_UNSUPPORTED.

@@ -142,6 +142,9 @@ eg_mla_status make_decode_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     const int min_split = unit_kernel ? kMinSplitTok
                           : p.path == EG_MLA_PATH_MFMA || p.f32_mfma ? 256
                                                                      : 128;
+    p.target_items = static_cast<int>(target);
+    p.min_split = min_split;
+    p.max_split = max_split;
     s = std::max<int64_t>(s, min_split);
     if (unit_kernel) s = std::max<int64_t>(s, (p.capacity / kMaxPartialsTok + kTile - 1) / kTile * kTile);
     // the general merge reads a sequence's partials one after the other: no more
@@ -673,24 +676,14 @@ eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const f
 namespace {
 
 // The split kernel of one part of a shared decode, `rows` query rows a
-// sequence: the decode's plan without its absorption, schedules and
-// single-launch form (the call absorbs once for both parts and merges them
-// itself).  The wide kernel, with its schedule, stays where the tiled prefix
-// kernel prepares both (`wide`).
-eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t rows, int32_t max_pages, bool wide,
-                               DecodePlan* p) {
+// sequence: the decode's plan without its absorption, the d_c 128 schedule and
+// the single-launch form (the call absorbs once for both parts and merges them
+// itself).
+eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t rows, int32_t max_pages, DecodePlan* p) {
   const eg_mla_status st = make_decode_plan(d, batch, max_pages, nullptr, p, PlanRows::kFast, rows);
   if (st != EG_MLA_OK) return st;
   p->fused_absorb = p->one_launch = p->tok_balanced = false;
   p->pieces = 0;
-  if (p->balanced && !wide) {
-    p->balanced = false;
-    p->heads_per_group = 16;
-    p->head_groups = ceil_div(rows, 16);
-    const int64_t s = ceil_div(static_cast<int64_t>(batch) * std::max(p->capacity, 1) * p->head_groups, kTargetWorkItems);
-    p->split_tokens = static_cast<int>(std::min<int64_t>(std::max<int64_t>((s + kTile - 1) / kTile * kTile, 256), kMaxSplitTokens));
-    p->s_max = ceil_div(std::max(p->capacity, 1), p->split_tokens);
-  }
   if (p->path == EG_MLA_PATH_VALU && !p->f32_mfma) {
     // the vector kernel's queries and probabilities of a group of heads lie in LDS
     while (p->heads_per_group > 1 &&
@@ -724,6 +717,29 @@ bool prefix_tiled(const eg_mla_dims& d) {
   return mfma_shape_supported(d) && d.head_dim == 128 && d.v_head_dim == 128;
 }
 
+// Partial rows that a part's automatic plan has at most for `rows` query rows
+// of all its sequences, or for fewer of them or a smaller capacity: whole
+// splits of the smallest size, and items of up to `heads` rows, of which there
+// are target_items and one more a sequence and group of heads, or those of the
+// largest split.  A workspace of this size serves every smaller call too.
+int64_t part_rows(const DecodePlan& p, int64_t rows) {
+  if (p.capacity == 0) return 0;
+  const int64_t heads = p.path == EG_MLA_PATH_VALU && !p.f32_mfma ? 256 : 16;
+  return std::min(rows * ceil_div(p.capacity, p.min_split),
+                  std::max(heads * p.target_items, rows * p.capacity / p.max_split) + rows);
+}
+
+// The same of the decode's own plan, and its workspace in all (make_decode_plan's layout).
+size_t plain_bytes(const eg_mla_dims& d, int32_t batch, const DecodePlan& p) {
+  const int64_t q_rows = static_cast<int64_t>(batch) * d.num_heads;
+  int64_t rows = part_rows(p, q_rows);
+  if (p.balanced) rows = (int64_t{kWideMaxGroups} + batch) * d.num_heads;
+  else if (p.path == EG_MLA_PATH_MFMA && tok_kernel_shape(d) && batch > 32) rows = std::max<int64_t>(rows, kTokMaxPieces * 16);
+  const size_t dq = static_cast<size_t>(d.latent_dim + d.rope_dim);
+  return align_up(q_rows * dq * 4) + align_up(rows * 8) + align_up(rows * static_cast<size_t>(d.latent_dim) * (p.balanced ? 2 : 4)) +
+         align_up(16 + kTokMaxPieces * 16 + static_cast<size_t>(batch) * 8) + align_up(2 * kTargetWorkItemsTok * 8);
+}
+
 }  // namespace
 
 eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_pages_per_seq,
@@ -732,16 +748,20 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
   // all heads of all sequences are the prefix's heads; merge grid
   const int64_t rows64 = static_cast<int64_t>(batch) * d.num_heads;
   if (rows64 > (1 << 30) || batch > 65535) return EG_MLA_ERR_UNSUPPORTED;
+  DecodePlan plain;  // a call without prefix pages is this decode; others leave its room
+  eg_mla_status st = make_decode_plan(d, batch, max_pages_per_seq, nullptr, &plain);
+  if (st != EG_MLA_OK) return st;
+  const size_t least = plain_bytes(d, batch, plain);
   if (max_prefix_pages == 0 && max_pages_per_seq > 0) {
     p.plain = true;
-    p.bytes = decode_workspace_bytes(d, batch, max_pages_per_seq, nullptr);
-    const eg_mla_status st = make_decode_plan(d, batch, max_pages_per_seq, nullptr, &p.own);
+    p.own = plain;
+    p.bytes = least;
     *out = p;
-    return st;
+    return EG_MLA_OK;
   }
-  eg_mla_status st = shared_part_plan(d, 1, std::max(1, batch * d.num_heads), max_prefix_pages, false, &p.pre);
+  st = shared_part_plan(d, 1, std::max(1, batch * d.num_heads), max_prefix_pages, &p.pre);
   p.tiled = p.pre.capacity > 0 && rows64 > 0 && prefix_tiled(d);
-  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, d.num_heads, max_pages_per_seq, p.tiled, &p.own);
+  if (st == EG_MLA_OK) st = shared_part_plan(d, batch, d.num_heads, max_pages_per_seq, &p.own);
   if (st != EG_MLA_OK) return st;
   const size_t rows = static_cast<size_t>(rows64), dc = static_cast<size_t>(d.latent_dim), dq = dc + d.rope_dim;
   size_t off = 0;
@@ -762,28 +782,32 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     p.half_rows = heads_kernel_shape(d);
     // the fused kernel's work-groups take the own tokens too, whose tiles may be the more
     const int most = p.fused ? std::max(tiles, ceil_div(p.own.capacity, 32)) : tiles;
-    p.splits = std::max(1, std::min((work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d)) / p.row_blocks, most));
+    const int groups = work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d);
+    p.splits = std::max(1, std::min(groups / p.row_blocks, most));
     if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x3fffffff) return EG_MLA_ERR_UNSUPPORTED;
     p.off_half = take(rows * dq * 2);
     if (!p.own.balanced) p.off_q = take(rows * dq * 4);
-    p.off_tiles = take(static_cast<size_t>(tiles) * p.keys * (prefix_latent_row(d.latent_dim) + 128));
+    // tiles of either size, and what fewer rows in more splits would need (part_rows)
+    p.off_tiles = take(static_cast<size_t>(ceil_div(p.pre.capacity, 64)) * 64 * (prefix_latent_row(d.latent_dim) + 128));
     if (p.fused) p.off_rows = take(static_cast<size_t>(batch) * 8);
-    p.pre.off_ml = take(rows * p.splits * 8);
-    p.pre.off_o = take(rows * p.splits * dc * (p.half_rows ? 2 : 4));
+    const size_t tiles32 = static_cast<size_t>(ceil_div(std::max(p.pre.capacity, p.fused ? p.own.capacity : 0), 32));
+    const size_t n = std::min(rows * tiles32, std::max(rows, static_cast<size_t>(kPrefixRows) * groups));
+    p.pre.off_ml = take(n * 8);
+    p.pre.off_o = take(n * dc * (p.half_rows ? 2 : 4));
   } else {
     p.off_q = take(rows * dq * 4);
-    const size_t n = p.pre.capacity > 0 ? rows * static_cast<size_t>(p.pre.s_max) : 0;
+    const size_t n = static_cast<size_t>(part_rows(p.pre, rows64));
     p.pre.off_ml = take(n * 8);
     p.pre.off_o = take(n * dc * 4);
   }
   if (p.own.capacity > 0 && !p.fused) {
     const size_t n = p.own.balanced ? (static_cast<size_t>(kWideMaxGroups) + batch) * d.num_heads
-                                    : rows * static_cast<size_t>(p.own.s_max);
+                                    : static_cast<size_t>(part_rows(p.own, rows64));
     p.own.off_ml = take(n * 8);
     p.own.off_o = take(n * dc * (p.own.balanced ? 2 : 4));
     if (p.own.balanced) p.own.off_sched = take(16 + kWideMaxGroups * 8 + static_cast<size_t>(batch) * 8);
   }
-  p.bytes = std::max<size_t>(off, kAlign);
+  p.bytes = std::max({off, least, kAlign});
   *out = p;
   return EG_MLA_OK;
 }

@@ -56,6 +56,8 @@ struct DecodePlan {
   int capacity = 0;             // max_pages_per_seq * page_size
   int head_groups = 1;          // work items per (b, split) along heads
   int heads_per_group = 0;
+  int target_items = 0;         // work items that an automatic split aims at,
+  int min_split = 0, max_split = 0;  // and its bounds (of the layer, whatever the batch)
   int slices = 1;               // partials per (b, split, head group): token-id slices of the sliced kernel
   bool balanced = false;        // head-split kernel: balanced schedule (split_tokens = list chunk)
   bool f32_mfma = false;        // VALU-path shape served by the fp32 matrix-core kernel (split_f32.h)

@@ -51,3 +51,10 @@ def test_splits_of_the_fused_kernel_follow_the_longer_part(shared_plan, page, ba
     """Its work-groups take own tokens as well as the prefix's: as many as fill the chip while either part has tiles."""
     got = shared_plan("plan", *H128, page, batch, pages, prefix)
     assert got[3:7] == (1, 1, splits, batch)
+
+
+@pytest.mark.parametrize("layer", LAYERS, ids=str)
+@pytest.mark.parametrize("page,batch,pages,prefix", [(64, 300, 64, 128), (16, 128, 300, 600), (1, 40, 3000, 9000)])
+def test_a_workspace_serves_smaller_calls(shared_plan, layer, page, batch, pages, prefix):
+    """No smaller batch, own or prefix table asks for more than the largest, and every plan's rows end within its own."""
+    assert shared_plan("sizes", *layer, page, batch, pages, prefix) == (0,)
