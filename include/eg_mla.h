@@ -514,8 +514,9 @@ eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_tokens, con
  *              server's largest serves its smaller calls); calls that share it
  *              must be ordered.
  * Arithmetic as for eg_mla_decode (any shape and storage type): the kernels
- * are chosen from the layer, whatever the batch.  out is
- * 16-byte aligned.  batch above 65535 is EG_MLA_ERR_UNSUPPORTED.
+ * are chosen from the layer, whatever the batch.  out is 16-byte aligned; out
+ * and workspace overlap neither an input nor each other
+ * (EG_MLA_ERR_INVALID_ARG).  batch above 65535 is EG_MLA_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------------- */
 size_t eg_mla_decode_shared_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_pages_per_seq,
                                            int32_t max_prefix_pages);
@@ -563,7 +564,8 @@ eg_mla_status eg_mla_decode_shared(const eg_mla_dims* dims, int32_t batch, const
  * other pages only.  keep >= keep_first + keep_last.
  *
  * Lengths are clamped to the capacity, 0 gives no pages.  Of a page table only
- * the entries of a sequence's pages are read.
+ * the entries of a sequence's pages are read.  No output or workspace overlaps
+ * an input or another output (EG_MLA_ERR_INVALID_ARG).
  * ------------------------------------------------------------------------- */
 eg_mla_status eg_mla_page_means(const eg_mla_dims* dims, int32_t batch, const void* latent_cache,
                                 const int32_t* token_id_cache, const void* gate_table, const int32_t* first_tokens,

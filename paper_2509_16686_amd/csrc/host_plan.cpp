@@ -622,17 +622,20 @@ size_t page_scores_workspace_bytes(const eg_mla_dims& d, int32_t batch) {
 }
 
 eg_mla_status validate_page_means(const eg_mla_dims* d, int32_t batch, const void* latent_cache,
-                                  const int32_t* token_id_cache, const void* gate_table, const int32_t* seq_lens,
-                                  const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
-                                  const void* page_means) {
+                                  const int32_t* token_id_cache, const void* gate_table, const int32_t* first_tokens,
+                                  const int32_t* seq_lens, const int32_t* page_table, int32_t max_pages_per_seq,
+                                  int64_t num_slots, const void* page_means) {
   eg_mla_status st = check_dims(d);
   if (st != EG_MLA_OK) return st;
   st = check_pages(*d, batch, max_pages_per_seq, num_slots, page_table != nullptr);
   if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
   if (!latent_cache || !token_id_cache || !gate_table || !seq_lens || !page_means) return EG_MLA_ERR_INVALID_ARG;
   if (!aligned16(latent_cache) || !aligned16(gate_table) || !aligned16(page_means)) return EG_MLA_ERR_INVALID_ARG;
-  const int64_t row = static_cast<int64_t>(d->latent_dim + d->rope_dim) * elem_bytes(*d);
-  if (overlap({page_means, num_slots / d->page_size * row}, {latent_cache, num_slots * row}))
+  const int64_t eb = elem_bytes(*d), row = (d->latent_dim + d->rope_dim) * eb, n = 4 * static_cast<int64_t>(batch);
+  if (outputs_overlap({{page_means, num_slots / d->page_size * row}},
+                      {{latent_cache, num_slots * row}, {token_id_cache, num_slots * 4},
+                       {gate_table, eb * d->vocab_size * d->latent_dim}, {first_tokens, n}, {seq_lens, n},
+                       {page_table, n * max_pages_per_seq}}))
     return EG_MLA_ERR_INVALID_ARG;
   return EG_MLA_OK;
 }
@@ -647,8 +650,15 @@ eg_mla_status validate_page_scores(const eg_mla_dims* d, int32_t batch, const vo
   if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
   if (!q || !w_uk || !page_means || !seq_lens || !scores) return EG_MLA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(w_uk) || !aligned16(page_means)) return EG_MLA_ERR_INVALID_ARG;
-  if (!workspace || workspace_bytes < page_scores_workspace_bytes(*d, batch)) return EG_MLA_ERR_WORKSPACE;
+  const size_t need = page_scores_workspace_bytes(*d, batch);
+  if (!workspace || workspace_bytes < need) return EG_MLA_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
+  const int64_t eb = elem_bytes(*d), n = 4 * static_cast<int64_t>(batch), h = d->num_heads, dc = d->latent_dim;
+  if (outputs_overlap({{scores, n * max_pages_per_seq}, {workspace, static_cast<int64_t>(need)}},
+                      {{q, batch * h * (d->head_dim + d->rope_dim) * eb}, {w_uk, h * d->head_dim * dc * eb},
+                       {page_means, num_slots / d->page_size * (dc + d->rope_dim) * eb}, {seq_lens, n},
+                       {page_table, n * max_pages_per_seq}}))
+    return EG_MLA_ERR_INVALID_ARG;
   return EG_MLA_OK;
 }
 
@@ -835,6 +845,14 @@ eg_mla_status validate_decode_shared(const eg_mla_dims* d, int32_t batch, const 
     return EG_MLA_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < p->bytes) return EG_MLA_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
+  const int64_t eb = elem_bytes(*d), n = 4 * static_cast<int64_t>(batch), h = d->num_heads, dc = d->latent_dim;
+  if (outputs_overlap({{out, batch * h * d->v_head_dim * eb}, {workspace, static_cast<int64_t>(p->bytes)}},
+                      {{q, batch * h * (d->head_dim + d->rope_dim) * eb}, {latent_cache, num_slots * (dc + d->rope_dim) * eb},
+                       {token_id_cache, num_slots * 4}, {gate_table, d->vocab_size * dc * eb},
+                       {w_uk, h * d->head_dim * dc * eb}, {w_uv, h * d->v_head_dim * dc * eb}, {prefix_len, 4},
+                       {prefix_table, 4 * static_cast<int64_t>(max_prefix_pages)}, {seq_lens, n},
+                       {page_table, n * max_pages_per_seq}}))
+    return EG_MLA_ERR_INVALID_ARG;
   return EG_MLA_OK;
 }
 

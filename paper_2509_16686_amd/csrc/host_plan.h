@@ -181,9 +181,9 @@ bool page_scores_mfma(const eg_mla_dims& d);  // whether the scores run on the m
 // Absorbed queries: fp32 [B, H, d_c + d_r], or (matrix cores) the bf16 parts of PartsLayout (absorb.h).
 size_t page_scores_workspace_bytes(const eg_mla_dims& d, int32_t batch);
 eg_mla_status validate_page_means(const eg_mla_dims* d, int32_t batch, const void* latent_cache,
-                                  const int32_t* token_id_cache, const void* gate_table, const int32_t* seq_lens,
-                                  const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
-                                  const void* page_means);
+                                  const int32_t* token_id_cache, const void* gate_table, const int32_t* first_tokens,
+                                  const int32_t* seq_lens, const int32_t* page_table, int32_t max_pages_per_seq,
+                                  int64_t num_slots, const void* page_means);
 eg_mla_status validate_page_scores(const eg_mla_dims* d, int32_t batch, const void* q, const void* w_uk,
                                    const void* page_means, const int32_t* seq_lens, const int32_t* page_table,
                                    int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,

@@ -521,8 +521,8 @@ extern "C" eg_mla_status eg_mla_page_means(const eg_mla_dims* dims, int32_t batc
                                            const int32_t* first_tokens, const int32_t* seq_lens,
                                            const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
                                            void* page_means, void* stream_) {
-  const eg_mla_status st = validate_page_means(dims, batch, latent_cache, token_id_cache, gate_table, seq_lens,
-                                               page_table, max_pages_per_seq, num_slots, page_means);
+  const eg_mla_status st = validate_page_means(dims, batch, latent_cache, token_id_cache, gate_table, first_tokens,
+                                               seq_lens, page_table, max_pages_per_seq, num_slots, page_means);
   if (st != EG_MLA_OK || batch == 0 || max_pages_per_seq == 0) return st;
   const eg_mla_dims& d = *dims;
   MeansArgs a{latent_cache, token_id_cache, gate_table, first_tokens, seq_lens, page_table, page_means, num_slots,
