@@ -496,7 +496,12 @@ struct Span {
 bool overlap(const Span& a, const Span& b) {
   if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+  return x < y ? y - x < static_cast<uintptr_t>(a.bytes) : x - y < static_cast<uintptr_t>(b.bytes);  // (no end wraps round)
+}
+// Product of non-negative sizes, held at the largest: an array of that many bytes meets every one behind it.
+int64_t held_product(int64_t a, int64_t b) {
+  int64_t r;
+  return __builtin_mul_overflow(a, b, &r) ? INT64_MAX : r;
 }
 // Whether any of the outputs overlaps another output or an input.
 bool outputs_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
@@ -596,9 +601,9 @@ eg_mla_status validate_qk(const eg_mla_dims* d, int32_t n_tokens, const void* q,
       return EG_MLA_ERR_INVALID_ARG;
   }
   // the rotated query may take its source's place where the rows are the same; nothing else may overlap
-  const Span qs{q, ((n - 1) * q_stride + q_row) * eb}, ks{kv, ((n - 1) * kv_stride + row) * eb};
-  const Span qo{q ? q_out : nullptr, n * q_row * eb}, cache{kv ? latent_cache : nullptr, num_slots * row * eb};
-  const Span ids{kv ? token_id_cache : nullptr, num_slots * 4};
+  const Span qs{q, held_product((n - 1) * q_stride + q_row, eb)}, ks{kv, held_product((n - 1) * kv_stride + row, eb)};
+  const Span qo{q ? q_out : nullptr, held_product(n * eb, q_row)}, cache{kv ? latent_cache : nullptr, held_product(num_slots, row * eb)};
+  const Span ids{kv ? token_id_cache : nullptr, held_product(num_slots, 4)};
   const Span qw{q ? q_norm_w : nullptr, static_cast<int64_t>(d->head_dim + d->rope_dim) * eb};
   const Span kw{kv ? kv_norm_w : nullptr, static_cast<int64_t>(d->latent_dim) * eb};
   const Span rw{kv ? k_norm_w : nullptr, static_cast<int64_t>(d->rope_dim) * eb};
@@ -677,8 +682,9 @@ eg_mla_status validate_select_pages(const eg_mla_dims* d, int32_t batch, const f
   if (batch == 0) return EG_MLA_OK;
   if (!seq_lens || !sel_pages || !sel_lens || (max_pages_per_seq > 0 && !scores)) return EG_MLA_ERR_INVALID_ARG;
   const int64_t n = 4 * static_cast<int64_t>(batch);
-  if (outputs_overlap({{sel_pages, n * keep}, {sel_lens, n}, {sel_index, n * keep}},
-                      {{seq_lens, n}, {page_table, 4 * entries}, {scores, 4 * entries}}))
+  const int64_t kept = held_product(n, keep), all = held_product(4, entries);
+  if (outputs_overlap({{sel_pages, kept}, {sel_lens, n}, {sel_index, kept}},
+                      {{seq_lens, n}, {page_table, all}, {scores, all}}))
     return EG_MLA_ERR_INVALID_ARG;
   return EG_MLA_OK;
 }
