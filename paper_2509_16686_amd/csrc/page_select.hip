@@ -119,7 +119,11 @@ __global__ __launch_bounds__(kMeanThreads) void page_means_kernel(MeansArgs a) {
     for (int i = tid; i < DQ; i += kMeanThreads) {
       double s = 0.0;
       for (int k = 0; k < rows; ++k) s += red[(i % N) * kMeanThreads + k * np + i / N];
-      st<BF16>(a.means, page * DQ + i, static_cast<float>(s / n));
+      // (straight from 64 bits: by way of fp32 it would be rounded twice, but for the compiler's folding the two)
+      if constexpr (BF16)
+        static_cast<uint16_t*>(a.means)[page * DQ + i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(s / n));
+      else
+        static_cast<float*>(a.means)[page * DQ + i] = static_cast<float>(s / n);
     }
     __syncthreads();
   }
