@@ -377,15 +377,14 @@ __global__ __launch_bounds__(kCombWaves * 64) void combine_mfma_kernel(const flo
     if (kk < nseq) {
       float Mx = -INFINITY;
       for (int p = 0; p < wps; ++p) Mx = fmaxf(Mx, m_part[kk * wps + p]);
-      if (Mx > -INFINITY) {
-        float num = 0.f, den = 0.f;
-        for (int p = 0; p < wps; ++p) {
-          const float e = __builtin_amdgcn_exp2f(m_part[kk * wps + p] - Mx);  // empty part: exp2(-inf) = 0
-          num = fmaf(e, o_part[(kk * wps + p) * DC + c], num);
-          den = fmaf(e, l_part[kk * wps + p], den);
-        }
-        v = num / den;
+      // (parts that weigh nothing are added all the same: a NaN in one stays one)
+      float num = 0.f, den = 0.f;
+      for (int p = 0; p < wps; ++p) {
+        const float e = Mx > -INFINITY ? __builtin_amdgcn_exp2f(m_part[kk * wps + p] - Mx) : 0.f;  // empty part: exp2(-inf) = 0
+        num = fmaf(e, o_part[(kk * wps + p) * DC + c], num);
+        den = fmaf(e, l_part[kk * wps + p], den);
       }
+      v = den == 0.f ? 0.f : num / den;
     }
     const __bf16 hi = static_cast<__bf16>(v);
     o_s[kk * OS + c] = __builtin_bit_cast(uint16_t, hi);
