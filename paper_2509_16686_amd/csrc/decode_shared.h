@@ -114,9 +114,12 @@ struct SharedCall {
 constexpr int kSharedMergeGroups = 256;
 
 // Partial rows of a sequence up to which the fused kernel's go to the wide
-// merge, which takes them four at a time and 32 sequences a work-group (64
-// sequences, 4 rows: 14.5 us against 19.6); more go to shared_merge_kernel.
-constexpr int kFusedWideSplits = 8;
+// merge, which takes them four at a time and 32 sequences a work-group; more
+// go to shared_merge_kernel (us a call with it / the wide merge, prefix 8000:
+// 64 sequences, 4 rows, 168.3 / 163.9; 28, 9 rows, 100.5 / 99.0; 20, 12 rows,
+// 83.6 / 81.3; 18, 14 rows, 80.7 / 79.3; 16, 16 rows, 73.8 / 75.3; 8, 32 rows,
+// 55.9 / 59.2).
+constexpr int kFusedWideSplits = 14;
 
 // Arguments of the split kernel of the prefix (part 0, as one sequence of B H heads) or of the own tokens (part 1).
 SplitArgs shared_split_args(const SharedCall& c, int part, const float* qfull, SharedPart* rows) {

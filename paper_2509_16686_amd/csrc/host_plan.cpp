@@ -712,17 +712,30 @@ eg_mla_status shared_part_plan(const eg_mla_dims& d, int32_t batch, int32_t rows
   return EG_MLA_OK;
 }
 
-// Work-groups: two per compute unit where their registers and tiles allow (d_c 128).
-int prefix_groups(const eg_mla_dims& d) { return d.latent_dim == 128 ? 512 : 256; }
+// Work-groups of the prefix kernel for `tiles` 64-key tiles over all row blocks.  More of them share the tiles out
+// evenly but write more fp32 partial rows for the merge to read; two fit a compute unit at d_c 128, one above.
+// Measured, us a call with 128 / 256 / 512 (prefix 8192 but for the last two, 16 to 100 own tokens):
+//   d_c 128, 16 heads   1 sequence (128 tiles)  20.2 /  21.4 / 22.2   d_c 320   16 (256)    43.3 / 46.1
+//                      16 (256)                 25.7 /  30.1 / 36.9             32 (512)    48.1 / 49.2
+//                      32 (512)                 27.1 /  30.4 / 36.2             64 (1024)   56.7 / 54.2
+//                      64 (1024)                31.6 /  32.4 / 35.8            128 (2048)   73.6 / 64.1
+//                     128 (2048)                44.6 /  37.3 / 39.4
+//                     256 (4096)                65.1 /  47.9 / 50.1
+//                     256 of 16384 (8192)      107.8 /  71.0 / 70.8
+//                     256 of 32768 (16384)     192.8 / 116.1 / 111.4
+constexpr int64_t kPrefixFewTiles = 1024, kPrefixManyTiles = 8192;
+int prefix_groups(const eg_mla_dims& d, int64_t tiles) {
+  if (d.latent_dim < 512 && tiles < kPrefixFewTiles) return 128;
+  return d.latent_dim == 128 && tiles >= kPrefixManyTiles ? 512 : 256;
+}
 
-// d_c 128: with few tiles one, fewer partial rows (prefix 8192 x 32 sequences of
-// 16 heads, 512 tiles: both parts and the merge 19.6 us with 256 work-groups,
-// 25.1 with 512; x 256 sequences of 16384, 8192 tiles: 70.3 and 68.2).
-constexpr int kPrefixGroupsFew = 256;
-constexpr int64_t kPrefixFewTiles = 2048;
-// d_c 128: prefix and own tokens in one launch up to this many tiles (the two
-// of the last paragraph: 33.5 -> 24.8 us and 76 -> 72 a call); its 32-key
-// tiles cost the prefix 6 %, more than hiding the own tokens gains beyond.
+// d_c 128: prefix and own tokens in one launch up to this many tiles.  Hiding the own tokens gains less and less, its
+// 32-key tiles cost more (us a call in two launches / one, 16 heads, up to 100 own tokens and up to 1000):
+//     64 x  8192 (1024 tiles)    39.0 /  32.9     41.3 /  31.4
+//    256 x 16384 (8192)          75.9 /  71.6     89.7 /  80.8
+//    256 x 32768 (16384)        115.5 / 112.8    129.2 / 122.2
+//    256 x 49152 (24576)        155.9 / 155.2    168.9 / 163.4
+//    256 x 65536 (32768)        194.6 / 195.6    208.4 / 205.1
 constexpr int64_t kBothMaxTiles = 16384;
 
 // Tiled prefix attention: the layers that the decode takes with the same
@@ -798,7 +811,7 @@ eg_mla_status make_shared_plan(const eg_mla_dims& d, int32_t batch, int32_t max_
     p.half_rows = heads_kernel_shape(d);
     // the fused kernel's work-groups take the own tokens too, whose tiles may be the more
     const int most = p.fused ? std::max(tiles, ceil_div(p.own.capacity, 32)) : tiles;
-    const int groups = work < kPrefixFewTiles ? kPrefixGroupsFew : prefix_groups(d);
+    const int groups = prefix_groups(d, work);
     p.splits = std::max(1, std::min(groups / p.row_blocks, most));
     if (static_cast<int64_t>(p.row_blocks) * p.splits > 0x3fffffff) return EG_MLA_ERR_UNSUPPORTED;
     p.off_half = take(rows * dq * 2);

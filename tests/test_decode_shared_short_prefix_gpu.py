@@ -25,3 +25,9 @@ def test_wide_tables_with_few_tokens(gpu, layer):
     assert_close(c.run(), c.ref(prefix=0), "bf16", "no prefix token")
     c.seq_lens.zero_()
     assert not c.run().any()
+
+
+@pytest.mark.parametrize("batch", [15, 17, 18, 19, 20, 22, 24, 26, 28])
+def test_partial_rows_of_each_merge(gpu, batch):
+    # 17 to 9 rows a sequence, around the change from one merge to the other
+    Case("h128", 700, [(53 * b) % 140 for b in range(batch)], page=16).check(f"h128 batch={batch}")
