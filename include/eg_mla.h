@@ -465,8 +465,9 @@ eg_mla_status eg_mla_page_release(int32_t batch, int32_t page_size, int32_t max_
  *           (r' = r if k_norm_w == NULL)
  *     latent_cache[slots[i]] = [c | k^R],  token_id_cache[slots[i]] = token_ids[i]
  * RoPE as in eg_mla_append (adjacent pairs, angle pos * theta^(-2m/d_r)); the
- * angle is reduced in 64-bit fixed point, so that it is exact to 2^-30 turns
- * at any position.  Arithmetic is fp32, rounded once to the storage type.
+ * angle is reduced to a turn in 64-bit fixed point and then rounded to fp32,
+ * so that it is off by at most 2^-26 turns and a little at any position.
+ * Arithmetic is fp32, rounded once to the storage type.
  *
  *   q    [n_tokens] rows of num_heads * (d_h + d_r) values, q_stride elements
  *        apart, or NULL (no queries: q_norm_w and q_out are not used)
@@ -499,7 +500,12 @@ eg_mla_status eg_mla_qk_norm_rope(const eg_mla_dims* dims, int32_t n_tokens, con
  * which equals eg_mla_decode over sequences of L + seq_lens[b] tokens whose
  * first L are the prefix's (up to the rounding of the partial sums).  A
  * sequence without own tokens attends to the prefix alone, one without any
- * token gets zeros.
+ * token gets zeros.  For a small product of sequences and prefix tokens, and a
+ * prefix of whole pages, eg_mla_decode over tables that name the prefix's
+ * pages for every sequence is the faster of the two: with 16 heads below about
+ * 200 000 pairs at d_c 128 (24 sequences of 8192, 32 of 4096) and 130 000 at
+ * d_c 320, and for bf16 layers whose decode is fp32; not with 128 heads of d_c
+ * 512, nor for fp32 layers.
  *
  *   prefix_len    [1] int32 on the device;  prefix_table [max_prefix_pages]
  *   seq_lens [B], page_table [B, max_pages_per_seq] or NULL (contiguous own

@@ -17,9 +17,9 @@
 //
 // Angles: position times frequency in turns, in 64-bit fixed point modulo one
 // turn (the frequencies, scaled by 2^64 / 2 pi, come from the host in extended
-// precision), so that far positions keep full accuracy: an error below
-// 2^-30 turns for any 32-bit position.  Sine and cosine of the remainder are
-// fp32.  Sums of squares and every product are fp32; the result is rounded
+// precision), off by less than 2^-30 turns for any 32-bit position; the
+// remainder, in half turns of (-1, 1), is then rounded to fp32: 2^-26 turns at
+// most, wherever the position.  Sine and cosine of it are fp32.  Sums of squares and every product are fp32; the result is rounded
 // once to the storage type.
 #include <hip/hip_runtime.h>
 
