@@ -185,8 +185,9 @@ __device__ __forceinline__ float half_sum(float x) {
 
 // OWN (heads a multiple of 128, so that a row block lies within a sequence): after its run of the prefix a work-group
 // takes its share of the sequence's own tokens into the same accumulators.  Their raw rows and gate rows are copied to
-// LDS a tile ahead and gated in place there (from raw rows in a buffer of their own, with a barrier more and every
-// piece's address formed twice: prefix 8000 x 64 x 128 heads with up to 1500 own tokens 208.5 us a call, 203.5 so).
+// LDS a tile ahead and gated in place there (prefix 8000 x 64 x 128 heads with up to 1500 own tokens: a wave's whole rows
+// at a time 208.5 -> 204.5 us a call; raw rows in a buffer of their own, with a barrier more and every piece's address
+// formed twice, 209.0, in place 208.1 in the same run).
 constexpr int kOwnList = 512;  // own tokens listed at a time
 
 // Work-group `bid` of `nblocks`.  HALF: the form of the partial rows.
