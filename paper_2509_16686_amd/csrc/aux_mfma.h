@@ -377,10 +377,11 @@ __global__ __launch_bounds__(kCombWaves * 64) void combine_mfma_kernel(const flo
     if (kk < nseq) {
       float Mx = -INFINITY;
       for (int p = 0; p < wps; ++p) Mx = fmaxf(Mx, m_part[kk * wps + p]);
-      // (parts that weigh nothing are added all the same: a NaN in one stays one)
+      // (where no part weighs anything they are added all the same, with exp2(-inf) = 0: a NaN in one stays one)
+      const float ref = Mx > -INFINITY ? Mx : 0.f;
       float num = 0.f, den = 0.f;
       for (int p = 0; p < wps; ++p) {
-        const float e = Mx > -INFINITY ? __builtin_amdgcn_exp2f(m_part[kk * wps + p] - Mx) : 0.f;  // empty part: exp2(-inf) = 0
+        const float e = __builtin_amdgcn_exp2f(m_part[kk * wps + p] - ref);  // empty part: exp2(-inf) = 0
         num = fmaf(e, o_part[(kk * wps + p) * DC + c], num);
         den = fmaf(e, l_part[kk * wps + p], den);
       }

@@ -681,8 +681,9 @@ __global__ __launch_bounds__(kSharedMergeWaves * 64) void shared_merge_kernel(Sh
       const int kk = i / DC, c = i - kk * DC;
       float top = -INFINITY, num = 0.f, den = 0.f;
       for (int p = 0; p < wps; ++p) top = fmaxf(top, m_part[kk * wps + p]);
+      const float ref = top > -INFINITY ? top : 0.f;
       for (int p = 0; p < wps; ++p) {
-        const float x = top > -INFINITY ? __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top) : 0.f;
+        const float x = __builtin_amdgcn_exp2f(m_part[kk * wps + p] - ref);
         num = fmaf(x, part[kk * wps + p][c], num);
         den = fmaf(x, l_part[kk * wps + p], den);
       }
