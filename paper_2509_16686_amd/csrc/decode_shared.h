@@ -266,8 +266,8 @@ hipError_t launch_tiled(const SharedCall& c) {
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(combine_wide_kernel, dim3(d.num_heads, (c.batch + kCombWideSeq - 1) / kCombWideSeq),
                          dim3(kCombWideWaves * 64), combine_wide_lds_bytes(), c.stream, a.part_ml,
-                         static_cast<const uint16_t*>(a.part_o), static_cast<const uint16_t*>(c.w_uv), pa.split_rows, static_cast<uint16_t*>(c.out), c.batch,
-                         d.num_heads);
+                         static_cast<const uint16_t*>(a.part_o), static_cast<const uint16_t*>(c.w_uv), pa.split_rows,
+                         static_cast<uint16_t*>(c.out), c.batch, d.num_heads);
       return hipGetLastError();
     }
   }

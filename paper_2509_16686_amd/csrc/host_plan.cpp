@@ -620,10 +620,11 @@ bool page_scores_mfma(const eg_mla_dims& d) {
 }
 
 size_t page_scores_workspace_bytes(const eg_mla_dims& d, int32_t batch) {
-  const size_t n = static_cast<size_t>(std::max(batch, 0)), dq = static_cast<size_t>(d.latent_dim + d.rope_dim);
-  const size_t runs = static_cast<size_t>(ceil_div(d.latent_dim + d.rope_dim, 32) + 2 * ceil_div(d.latent_dim, 32));
-  const size_t bytes = page_scores_mfma(d) ? n * ceil_div(d.num_heads, 16) * runs * 1024 : n * d.num_heads * dq * 4;
-  return std::max<size_t>(align_up(bytes), kAlign);
+  const int64_t n = std::max(batch, 0), dq = d.latent_dim + d.rope_dim;
+  const int64_t runs = ceil_div(dq, 32) + 2 * ceil_div(d.latent_dim, 32);
+  const int64_t bytes = page_scores_mfma(d) ? held_product(n * ceil_div(d.num_heads, 16), runs * 1024)
+                                            : held_product(n * d.num_heads, dq * 4);
+  return std::max<size_t>(align_up(static_cast<size_t>(bytes)), kAlign);
 }
 
 eg_mla_status validate_page_means(const eg_mla_dims* d, int32_t batch, const void* latent_cache,
@@ -660,7 +661,7 @@ eg_mla_status validate_page_scores(const eg_mla_dims* d, int32_t batch, const vo
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
   const int64_t eb = elem_bytes(*d), n = 4 * static_cast<int64_t>(batch), h = d->num_heads, dc = d->latent_dim;
   if (outputs_overlap({{scores, n * max_pages_per_seq}, {workspace, static_cast<int64_t>(need)}},
-                      {{q, batch * h * (d->head_dim + d->rope_dim) * eb}, {w_uk, h * d->head_dim * dc * eb},
+                      {{q, held_product(batch * h, (d->head_dim + d->rope_dim) * eb)}, {w_uk, h * d->head_dim * dc * eb},
                        {page_means, num_slots / d->page_size * (dc + d->rope_dim) * eb}, {seq_lens, n},
                        {page_table, n * max_pages_per_seq}}))
     return EG_MLA_ERR_INVALID_ARG;

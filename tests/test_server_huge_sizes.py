@@ -4,7 +4,7 @@ import ctypes
 import pytest
 
 from paper_2509_16686_amd import binding as B
-from test_server_refusals import QK, SELECT, dims
+from test_server_refusals import QK, SCORES, SELECT, dims
 
 INT_MAX = 2 ** 31 - 1
 
@@ -38,3 +38,11 @@ def test_qk_norm_rope(change):
 def test_select_pages(change):
     d = dims(page_size=16)
     assert B.lib().eg_mla_select_pages(*{**far(SELECT), **change, "dims": ctypes.byref(d)}.values()) == B.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(dtype=B.FP32), dict(head_dim=32)])
+def test_page_scores(kw):
+    d = dims(num_heads=1 << 30, latent_dim=512, **kw)
+    assert B.page_scores_workspace_size(d, 1 << 30) >= 2 ** 63 - 1
+    args = {**far(SCORES), "batch": 1 << 30, "dims": ctypes.byref(d)}
+    assert B.lib().eg_mla_page_scores(*args.values()) == B.ERR_WORKSPACE
