@@ -1,6 +1,6 @@
 // Attention of many query rows over one prefix on gfx950 MFMA (bf16 storage,
-// d_h = d_v = 128, d_r = 64, d_c 128, 320 or 512): the prefix part of the
-// shared decode.  Included by decode.hip.
+// heads a multiple of 16, d_h = d_v = 128, d_r = 64, d_c 128, 320 or 512): the
+// prefix part of the shared decode.  Included by decode.hip.
 //
 // With all heads on one latent, the B H query rows of a batch attend to the
 // same keys [c~ | k^R] and values c~: a flash attention with d_c + d_r wide
