@@ -6,11 +6,11 @@ the row (a byte: 127 plus the exponent) and the RoPE key in bf16 behind the code
 
   rope    rotation of the RoPE part of query rows, pairs adjacent or half a part away, with plain frequencies or those of
           a stretched context; forward, or the gradient's way back (rope_rows)
-  write   norm, gate and rotation of the key rows of a step's tokens, written to their slots in 8 bits (q8_write), and the
-          same tokens read back, packed by sequence (q8_read)
-  read    cached sequences read back (q8_read)
+  write   norm, gate and rotation of the key rows of a step's tokens, written to their slots in 8 bits (quant_write), and the
+          same tokens read back, packed by sequence (quant_read)
+  read    cached sequences read back (quant_read)
   attend  attention of the new tokens of each sequence, causal among themselves, over the cache: one new token a
-          sequence (decode), or several (a chunk of a prompt, drafted tokens to verify) (q8_attend)
+          sequence (decode), or several (a chunk of a prompt, drafted tokens to verify) (quant_attend)
 
 and "layer" one of LAYERS.  Lengths are spread evenly over [min_len, max_len] and handed out in a random order; "min_new"
 and "max_new" are the new tokens of a sequence, among its length.
@@ -191,7 +191,7 @@ def prepare(case, seed):
         s["positions"] = at.to(torch.int32)
         s["slots"] = (table[of, at // page] * page + at % page).to(torch.int32)
     else:
-        # what q8_write leaves: gated latents near one, quantised, and RoPE keys
+        # what quant_write leaves: gated latents near one, quantised, and RoPE keys
         c = r.normal((rows, dc), torch.float32) * r.normal((rows, 1), torch.float32, 0.3, 1.0)
         codes, s["scales"] = _quantise(c)
         s["codes"][:, :dc] = codes.view(torch.uint8)
@@ -328,7 +328,7 @@ def _keep(s):
         s["rope"] = lib.make_rope(layout=lib.ROPE_HALF if case["half"] else lib.ROPE_PAIRS, theta=THETA, frequencies=freq,
                                   magnitude=_magnitude(case["factor"]))
     if case["kind"] == "attend":
-        s["ws"] = lib.alloc_workspace(lib.q8_attend_workspace_size(s["dims"], case["batch"], s["total"], s["width"]))
+        s["ws"] = lib.alloc_workspace(lib.quant_attend_workspace_size(s["dims"], case["batch"], s["total"], s["width"]))
     return lib
 
 
@@ -340,20 +340,20 @@ def _own_rope(s):
 
 def _own_read(s):
     lib = _keep(s)
-    lib.q8_read(s["dims"], s["codes"], s["scales"], s["first"], s["cu"], s["table"], s["out"])
+    lib.quant_read(s["dims"], s["codes"], s["scales"], s["first"], s["cu"], s["table"], s["out"])
     return s["out"]
 
 
 def _own_write(s):
     lib = _keep(s)
-    lib.q8_write(s["dims"], s["rope"], s["kv"], s["positions"], s["slots"], s["codes"], s["scales"], gate_table=s["gate"],
+    lib.quant_write(s["dims"], s["rope"], s["kv"], s["positions"], s["slots"], s["codes"], s["scales"], gate_table=s["gate"],
                  token_ids=s["ids"], kv_norm_w=s["kv_w"], k_norm_w=s["k_w"])
     return _own_read(s)
 
 
 def _own_attend(s):
     lib = _keep(s)
-    lib.q8_attend(s["dims"], s["q"], None if s["case"]["max_new"] == 1 else s["cu"], s["codes"], s["scales"], s["w_uk"],
+    lib.quant_attend(s["dims"], s["q"], None if s["case"]["max_new"] == 1 else s["cu"], s["codes"], s["scales"], s["w_uk"],
                   s["w_uv"], s["lens"], s["table"], s["width"], s["ws"], s["out"])
     return s["out"]
 
