@@ -590,6 +590,144 @@ eg_mla_status eg_mla_select_pages(const eg_mla_dims* dims, int32_t batch, const 
                                   int32_t keep, int32_t keep_first, int32_t keep_last, int32_t* sel_pages,
                                   int32_t* sel_lens, int32_t* sel_index, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Position rotation of a pair (a, b) of a row's part of d_r values (App. C
+ * Eq. (C.10)), pair m at position i:
+ *   (a, b) -> magnitude (a cos x - b sin x, a sin x + b cos x),  x = i f_m.
+ * frequencies: d_r / 2 host values f_m, radians a position, magnitudes up to
+ * 64, read before the call returns; NULL: theta^(-2m/d_r), theta <= 0 selects
+ * 10000.  magnitude <= 0 selects 1.  The angle is off by at most 2^-26 turns and
+ * a little, as in eg_mla_qk_norm_rope, and by the rounding of f_m.
+ * ------------------------------------------------------------------------- */
+typedef enum eg_mla_rope_layout {
+  EG_MLA_ROPE_PAIRS = 0, /* pair m is values 2m and 2m + 1 of the part (eg_mla_append's) */
+  EG_MLA_ROPE_HALF = 1   /* pair m is values m and d_r / 2 + m */
+} eg_mla_rope_layout;
+
+typedef struct eg_mla_rope {
+  int32_t layout; /* eg_mla_rope_layout */
+  float theta;
+  const double* frequencies;
+  float magnitude;
+} eg_mla_rope;
+
+/* Frequencies of a layer whose context is stretched `factor` >= 1 times over
+ * the trained_positions that it was trained on: with f_m = theta^(-2m/d_r) and
+ * t = trained_positions f_m / 2 pi the turns of pair m over these,
+ *   f'_m = f_m (k + (1 - k) / factor),  k = (t - slow) / (fast - slow) held to [0, 1]
+ * (arXiv 2309.00071, Sec. 3.2: pairs that turn often keep their frequency, slow
+ * ones are slowed).  slow_turns, fast_turns <= 0 select 1 and 32;
+ * trained_positions 0: every pair is slowed.  `frequencies` is a host array of
+ * rope_dim / 2.  On the host. */
+eg_mla_status eg_mla_rope_frequencies(int32_t rope_dim, float theta, float factor, int32_t trained_positions,
+                                      float slow_turns, float fast_turns, double* frequencies);
+
+/* ---------------------------------------------------------------------------
+ * Rotation of rows: the values rope_offset .. rope_offset + rope_dim - 1 of each
+ * head's row are rotated by its token's position, the others copied; `inverse`
+ * != 0 turns by -x (the gradient's way back through the rotation, and the undoing
+ * of one of magnitude 1).  Arithmetic is fp32, rounded once to the storage type.
+ *   x, out   [n_tokens, num_heads, head_dim] of `dtype` (eg_mla_dtype), rows of
+ *            adjacent values, their tokens and heads any strides (in elements, 0
+ *            to 2^32) apart; the rows of out do not overlap each other.  out may be
+ *            x with the same strides (in place), and else overlaps no input
+ *            (EG_MLA_ERR_INVALID_ARG)
+ *   positions [n_tokens] int32
+ * Any sizes and alignment of whole elements (fastest where offset, half of the
+ * part, the rest and the strides are multiples of 16 bytes).  rope_dim is even, at
+ * most 640 (EG_MLA_ERR_UNSUPPORTED).  n_tokens == 0 is a no-op.
+ * ------------------------------------------------------------------------- */
+eg_mla_status eg_mla_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t n_tokens, int32_t num_heads,
+                               int32_t head_dim, int32_t rope_offset, int32_t rope_dim, const void* x,
+                               int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions,
+                               int32_t inverse, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                               void* stream);
+
+/* ---------------------------------------------------------------------------
+ * 8-bit latent cache.  A token's row is the gated latent c~ = c (.) G[id]
+ * (Sec. 3.1 Eq. (3)-(5); the gate depends on the token alone, so it is applied
+ * once, as the row is written) as d_c e4m3 codes and, behind them, k^R in bf16;
+ * its scale is one byte, 127 + e, with e the least power of two that brings the
+ * row's largest magnitude within e4m3's 448 (-126 <= e <= 120; 0 for a row of
+ * zeros):
+ *   code = RNE(c~ 2^-e),   c~ ~ code 2^e.
+ * Scale 255: the row has an infinity or NaN among its gated latents and stands
+ * for NaN (its codes are 0).
+ *   codes  [num_slots, eg_mla_quant_row_bytes(dims)] bytes, d_c + 2 d_r a row, 16-byte aligned
+ *   scales [num_slots] bytes
+ * For bf16 layers with d_c a multiple of 16 up to 512 and d_r up to 64; other
+ * layers: EG_MLA_ERR_UNSUPPORTED (eg_mla_quant_row_bytes: 0).
+ *
+ * eg_mla_quant_write: key rows [c | r] of projected tokens into their slots:
+ *   c   = c / sqrt(mean(c^2) + 1e-6) * kv_norm_w   (only if kv_norm_w != NULL)
+ *   c~  = c (.) gate_table[token_ids[i]]           (only if gate_table != NULL)
+ *   k^R = RoPE(r', positions[i])                   (only if rope != NULL),
+ *         r' = r / sqrt(mean(r^2) + 1e-6) * k_norm_w (r' = r if k_norm_w == NULL)
+ * in fp32, rounded once, c~ to its codes and k^R to bf16.  (Rows of a bf16 cache
+ * are turned into 8-bit ones with rope and the norms NULL.)
+ *   kv [n_tokens] rows of d_c + d_r values, kv_stride elements apart (a multiple of
+ *      8, at most 2^32), 16-byte aligned; token_ids, positions, slots [n_tokens]
+ *      int32 (token_ids clamped to the table and NULL without one, positions NULL
+ *      without rope); slots outside [0, num_slots) are skipped, duplicate ones race.
+ *   gate_table and kv_norm_w 16-byte aligned.  n_tokens == 0 is a no-op.
+ *
+ * eg_mla_quant_read: rows back in bf16 [c~ | k^R] (exact but for magnitudes below
+ * bf16's smallest), packed by sequence: row cu_seqlens[b] + i of `out` is token
+ * first_tokens[b] + i (i if first_tokens is NULL) of sequence b, for what lies
+ * between cu_seqlens[b] and cu_seqlens[b + 1].  Rows of no sequence are left as
+ * they are.  With a gate table of one row of ones and token ids of 0 they are what
+ * the bf16 calls (eg_mla_prefill_varlen, eg_mla_decode over contiguous rows) take.
+ *   cu_seqlens [batch + 1] as for eg_mla_prefill_varlen; tokens past the capacity
+ *   read its last one;  out [total_tokens, d_c + d_r], 16-byte aligned.
+ *
+ * eg_mla_quant_attend: attention of the new tokens of each sequence (one: decode;
+ * several: a chunk of a prompt, drafted tokens) over its cached ones, which the
+ * new tokens' own rows, written before, are the last of.  New token i of n of
+ * sequence b attends to the tokens j < seq_lens[b] - n + i + 1:
+ *   s[j]   = tau (q_lat[h] . c~_j + q^R[h] . k^R_j),  q_lat[h] = W_UK[h]^T q^C[h]
+ *   out[h] = W_UV[h] sum_j softmax_j(s) c~_j
+ * and one that attends to no token gets zeros.
+ *   q [n_queries, H, d_h + d_r] packed by sequence, q^R already rotated;
+ *   cu_seqlens [batch + 1] or NULL (one new token a sequence, n_queries = batch);
+ *      rows of `out` behind cu_seqlens[batch] are left as they are, so that a call
+ *      captured with a fixed n_queries serves smaller steps
+ *   seq_lens [batch], new tokens included, clamped to [0, max_pages_per_seq * P];
+ *   page_table [batch, max_pages_per_seq] or NULL (contiguous rows) as for
+ *      eg_mla_decode;  w_uk, w_uv as there;  out [n_queries, H, d_v]
+ *   workspace  eg_mla_quant_attend_workspace_size(dims, batch, n_queries,
+ *      max_pages_per_seq) bytes, 256-byte aligned, no initialisation (no less than
+ *      for a smaller batch, fewer queries or fewer pages); calls that share it must be
+ *      ordered.  The size query returns 0 where the call would refuse.
+ * The absorbed query, c~ and the probabilities enter the matrix products in fp16
+ * (magnitudes below 65504), q^R and k^R in bf16; sums are fp32.  Which tokens a row
+ * does not attend to does not matter to it, whatever they hold.
+ *
+ * Batch above 4096, n_queries above 2^19 or n_queries * H above 2^30:
+ * EG_MLA_ERR_UNSUPPORTED.  Lengths, ids, pages and offsets on the device are made
+ * safe, not checked.  No output or workspace overlaps an input or another output
+ * (EG_MLA_ERR_INVALID_ARG).
+ * ------------------------------------------------------------------------- */
+int64_t eg_mla_quant_row_bytes(const eg_mla_dims* dims);
+
+eg_mla_status eg_mla_quant_write(const eg_mla_dims* dims, const eg_mla_rope* rope, int32_t n_tokens, const void* kv,
+                              int64_t kv_stride, const void* kv_norm_w, const void* k_norm_w, const void* gate_table,
+                              const int32_t* token_ids, const int32_t* positions, const int32_t* slots, uint8_t* codes,
+                              uint8_t* scales, int64_t num_slots, void* stream);
+
+eg_mla_status eg_mla_quant_read(const eg_mla_dims* dims, int32_t batch, int32_t total_tokens, const uint8_t* codes,
+                             const uint8_t* scales, const int32_t* first_tokens, const int32_t* cu_seqlens,
+                             const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots, void* out,
+                             void* stream);
+
+size_t eg_mla_quant_attend_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t n_queries,
+                                       int32_t max_pages_per_seq);
+
+eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t batch, int32_t n_queries, const void* q,
+                               const int32_t* cu_seqlens, const uint8_t* codes, const uint8_t* scales, const void* w_uk,
+                               const void* w_uv, const int32_t* seq_lens, const int32_t* page_table,
+                               int32_t max_pages_per_seq, int64_t num_slots, void* workspace, size_t workspace_bytes,
+                               void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

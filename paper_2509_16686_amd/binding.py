@@ -28,9 +28,12 @@ EXPORTS = ["eg_mla_status_string", "eg_mla_check_dims", "eg_mla_append", "eg_mla
            "eg_mla_append_workspace_size", "eg_mla_append_ws", "eg_mla_gate_table_marks_size",
            "eg_mla_gate_table", "eg_mla_page_plan", "eg_mla_page_release", "eg_mla_qk_norm_rope",
            "eg_mla_decode_shared_workspace_size", "eg_mla_decode_shared", "eg_mla_page_means",
-           "eg_mla_page_scores_workspace_size", "eg_mla_page_scores", "eg_mla_select_pages"]
+           "eg_mla_page_scores_workspace_size", "eg_mla_page_scores", "eg_mla_select_pages",
+           "eg_mla_rope_frequencies", "eg_mla_rope_rows", "eg_mla_quant_row_bytes", "eg_mla_quant_write", "eg_mla_quant_read",
+           "eg_mla_quant_attend_workspace_size", "eg_mla_quant_attend"]
 NOALLOC_SCRATCH_BYTES = 32 << 20  # EG_MLA_NOALLOC_SCRATCH_BYTES
 LITERAL_NO_LN, LITERAL_ADD = 1, 2
+ROPE_PAIRS, ROPE_HALF = 0, 1
 
 
 class Dims(ctypes.Structure):
@@ -44,6 +47,12 @@ class Plan(ctypes.Structure):
     _fields_ = [("path", ctypes.c_int32), ("split_tokens", ctypes.c_int32),
                 ("split_start_event", ctypes.c_void_p), ("split_stop_event", ctypes.c_void_p),
                 ("id_slices", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    """eg_mla_rope; `frequencies` points into an array that make_rope keeps beside it."""
+    _fields_ = [("layout", ctypes.c_int32), ("theta", ctypes.c_float),
+                ("frequencies", ctypes.POINTER(ctypes.c_double)), ("magnitude", ctypes.c_float)]
 
 
 class EgMlaError(RuntimeError):
@@ -123,6 +132,21 @@ def lib() -> ctypes.CDLL:
     L.eg_mla_page_scores.argtypes = [pd, i32, vp, vp, vp, vp, vp, i32, i64, vp, sz, vp, vp]
     L.eg_mla_select_pages.restype = ctypes.c_int
     L.eg_mla_select_pages.argtypes = [pd, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
+    pr, f32 = ctypes.POINTER(Rope), ctypes.c_float
+    L.eg_mla_rope_frequencies.restype = ctypes.c_int
+    L.eg_mla_rope_frequencies.argtypes = [i32, f32, f32, i32, f32, f32, ctypes.POINTER(ctypes.c_double)]
+    L.eg_mla_rope_rows.restype = ctypes.c_int
+    L.eg_mla_rope_rows.argtypes = [pr, i32, i32, i32, i32, i32, i32, vp, i64, i64, vp, i32, vp, i64, i64, vp]
+    L.eg_mla_quant_row_bytes.restype = i64
+    L.eg_mla_quant_row_bytes.argtypes = [pd]
+    L.eg_mla_quant_write.restype = ctypes.c_int
+    L.eg_mla_quant_write.argtypes = [pd, pr, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.eg_mla_quant_read.restype = ctypes.c_int
+    L.eg_mla_quant_read.argtypes = [pd, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp, vp]
+    L.eg_mla_quant_attend_workspace_size.restype = sz
+    L.eg_mla_quant_attend_workspace_size.argtypes = [pd, i32, i32, i32]
+    L.eg_mla_quant_attend.restype = ctypes.c_int
+    L.eg_mla_quant_attend.argtypes = [pd, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i64, vp, sz, vp, vp]
     _lib = L
     return L
 
@@ -467,6 +491,121 @@ def select_pages(dims: Dims, scores, seq_lens, page_table, max_pages_per_seq: in
     _check(lib().eg_mla_select_pages(ctypes.byref(dims), b, scores.data_ptr(), _ptr(seq_lens), _ptr(page_table),
                                      max_pages_per_seq, keep, keep_first, keep_last, sel_pages.data_ptr(), sel_lens.data_ptr(),
                                      _ptr(sel_index), _stream(stream)), name)
+
+
+# ---------------------------------------------------------------------------
+# rotation of rows, and the 8-bit latent cache
+# ---------------------------------------------------------------------------
+def rope_frequencies(rope_dim: int, factor: float, trained_positions: int, theta: float = 10000.0,
+                     slow_turns: float = 1.0, fast_turns: float = 32.0) -> list:
+    """eg_mla_rope_frequencies: radians a position of each pair of a layer whose context is stretched."""
+    f = (ctypes.c_double * max(rope_dim // 2, 1))()
+    _check(lib().eg_mla_rope_frequencies(rope_dim, theta, factor, trained_positions, slow_turns, fast_turns, f),
+           "eg_mla_rope_frequencies")
+    return list(f)
+
+
+def make_rope(layout: int = ROPE_PAIRS, theta: float = 10000.0, frequencies=None, magnitude: float = 1.0) -> Rope:
+    """A rotation; `frequencies` (d_r / 2 numbers, radians a position) take the place of theta's."""
+    r = Rope(layout, theta, None, magnitude)
+    if frequencies is not None:
+        r.values = (ctypes.c_double * len(frequencies))(*frequencies)
+        r.frequencies = r.values
+    return r
+
+
+def _rope_of(name: str, rope: Optional[Rope], rope_dim: int):
+    """The rotation's pointer; its frequencies have to be those of rope_dim / 2 pairs."""
+    if rope is None:
+        return None
+    values = getattr(rope, "values", None)
+    if values is not None and len(values) != rope_dim // 2:
+        raise ValueError(f"{name}: {len(values)} frequencies for {rope_dim // 2} pairs")
+    return ctypes.byref(rope)
+
+
+def rope_rows(rope: Rope, x, positions, out, rope_dim: int, rope_offset: Optional[int] = None, inverse: bool = False,
+              stream=None) -> None:
+    """eg_mla_rope_rows over device tensors: x and out [n, heads, head_dim] of one type, or views whose last dimension
+    is contiguous; out may be x.  The part starts at rope_offset (the row's last rope_dim values unless given)."""
+    import torch
+    name = "eg_mla_rope_rows"
+    n, heads, dim = x.shape
+    here = torch.cuda.current_device() if x.get_device() >= 0 else 0
+    for key, t in (("x", x), ("out", out)):
+        if (t.dtype not in (torch.bfloat16, torch.float32) or t.dtype is not x.dtype or t.shape != x.shape
+                or (t.stride(2) != 1 and dim > 1) or t.get_device() != here):
+            raise ValueError(f"{name}: {key} is {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}; expected "
+                             f"bfloat16 or float32 {tuple(x.shape)}, alike in x and out, with a contiguous last dimension "
+                             "on the current GPU")
+    _expect(name, ("positions", positions, torch.int32, (n,)))
+    _check(lib().eg_mla_rope_rows(_rope_of(name, rope, rope_dim), BF16 if x.dtype is torch.bfloat16 else FP32, n, heads,
+                                  dim, dim - rope_dim if rope_offset is None else rope_offset, rope_dim, x.data_ptr(),
+                                  x.stride(0), x.stride(1), positions.data_ptr(), int(inverse), out.data_ptr(),
+                                  out.stride(0), out.stride(1), _stream(stream)), name)
+
+
+def quant_row_bytes(dims: Dims) -> int:
+    return lib().eg_mla_quant_row_bytes(ctypes.byref(dims))
+
+
+def _quant_cache(dims: Dims, codes, scales) -> list:
+    import torch
+    n = codes.shape[0]
+    return [("codes", codes, torch.uint8, (n, dims.latent_dim + 2 * dims.rope_dim)), ("scales", scales, torch.uint8, (n,))]
+
+
+def quant_write(dims: Dims, rope: Optional[Rope], kv, positions, slots, codes, scales, gate_table=None, token_ids=None,
+             kv_norm_w=None, k_norm_w=None, stream=None) -> None:
+    """eg_mla_quant_write over device tensors: kv [n, d_c + d_r], or a view with a stride between its rows, into rows of
+    codes [num_slots, d_c + 2 d_r] and scales [num_slots] (uint8)."""
+    from torch import bfloat16, int32 as i
+    name, n = "eg_mla_quant_write", kv.shape[0]
+    stride = _row_stride(name, "kv", kv, n, dims.latent_dim + dims.rope_dim, bfloat16)
+    _expect(name, ("slots", slots, i, (n,)), ("positions", positions, i, (n,)), ("token_ids", token_ids, i, (n,)),
+            ("gate_table", gate_table, bfloat16, (dims.vocab_size, dims.latent_dim)),
+            ("kv_norm_w", kv_norm_w, bfloat16, (dims.latent_dim,)), ("k_norm_w", k_norm_w, bfloat16, (dims.rope_dim,)),
+            *_quant_cache(dims, codes, scales))
+    _check(lib().eg_mla_quant_write(ctypes.byref(dims), _rope_of(name, rope, dims.rope_dim), n, kv.data_ptr(), stride,
+                                 _ptr(kv_norm_w), _ptr(k_norm_w), _ptr(gate_table), _ptr(token_ids), _ptr(positions),
+                                 slots.data_ptr(), codes.data_ptr(), scales.data_ptr(), codes.shape[0], _stream(stream)), name)
+
+
+def quant_read(dims: Dims, codes, scales, first_tokens, cu_seqlens, page_table, out, max_pages_per_seq: Optional[int] = None,
+            stream=None) -> None:
+    """eg_mla_quant_read over device tensors: out [total, d_c + d_r] (bf16), packed by cu_seqlens [B + 1]; max_pages_per_seq
+    is page_table's width where there is one."""
+    from torch import bfloat16, int32 as i
+    name, b = "eg_mla_quant_read", cu_seqlens.shape[0] - 1
+    width = page_table.shape[1] if page_table is not None else max_pages_per_seq
+    if width is None:
+        raise ValueError(f"{name}: neither page_table nor max_pages_per_seq")
+    _expect(name, ("cu_seqlens", cu_seqlens, i, (b + 1,)), ("first_tokens", first_tokens, i, (b,)),
+            ("page_table", page_table, i, (b, width)), ("out", out, bfloat16, (out.shape[0], dims.latent_dim + dims.rope_dim)),
+            *_quant_cache(dims, codes, scales))
+    _check(lib().eg_mla_quant_read(ctypes.byref(dims), b, out.shape[0], codes.data_ptr(), scales.data_ptr(), _ptr(first_tokens),
+                                cu_seqlens.data_ptr(), _ptr(page_table), width, codes.shape[0], out.data_ptr(),
+                                _stream(stream)), name)
+
+
+def quant_attend_workspace_size(dims: Dims, batch: int, n_queries: int, max_pages_per_seq: int) -> int:
+    return lib().eg_mla_quant_attend_workspace_size(ctypes.byref(dims), batch, n_queries, max_pages_per_seq)
+
+
+def quant_attend(dims: Dims, q, cu_seqlens, codes, scales, w_uk, w_uv, seq_lens, page_table, max_pages_per_seq: int,
+              workspace, out, stream=None) -> None:
+    """eg_mla_quant_attend over device tensors: q [n, H, d_h + d_r] packed by cu_seqlens [B + 1], or (None) one new token a
+    sequence; out [n, H, d_v]."""
+    from torch import bfloat16 as bf, int32 as i, uint8
+    name, n, b, h = "eg_mla_quant_attend", q.shape[0], seq_lens.shape[0], dims.num_heads
+    _expect(name, ("q", q, bf, (n, h, dims.head_dim + dims.rope_dim)), ("cu_seqlens", cu_seqlens, i, (b + 1,)),
+            ("w_uk", w_uk, bf, (h, dims.head_dim, dims.latent_dim)), ("w_uv", w_uv, bf, (h, dims.v_head_dim, dims.latent_dim)),
+            ("seq_lens", seq_lens, i, (b,)), ("page_table", page_table, i, (b, max_pages_per_seq)),
+            ("out", out, bf, (n, h, dims.v_head_dim)), ("workspace", workspace, uint8, None), *_quant_cache(dims, codes, scales))
+    _check(lib().eg_mla_quant_attend(ctypes.byref(dims), b, n, q.data_ptr(), _ptr(cu_seqlens), codes.data_ptr(),
+                                  scales.data_ptr(), w_uk.data_ptr(), w_uv.data_ptr(), seq_lens.data_ptr(), _ptr(page_table),
+                                  max_pages_per_seq, codes.shape[0], workspace.data_ptr(), workspace.numel(), out.data_ptr(),
+                                  _stream(stream)), name)
 
 
 # ---------------------------------------------------------------------------

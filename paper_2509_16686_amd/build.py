@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libegmla.so")
 
 SOURCES = ["host_plan.cpp", "decode.hip", "append.hip", "prefill.hip", "gate.hip", "literal.hip", "pages.hip",
-           "qk_rope.hip", "page_select.hip"]
+           "qk_rope.hip", "page_select.hip", "quant.hip", "quant_attend.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -876,6 +876,169 @@ eg_mla_status validate_decode_shared(const eg_mla_dims* d, int32_t batch, const 
   return EG_MLA_OK;
 }
 
+namespace {
+
+// Frequencies and magnitude of a rotation.
+eg_mla_status check_rope(const eg_mla_rope* r, int32_t rope_dim) {
+  if (!r) return EG_MLA_ERR_INVALID_ARG;
+  if (r->layout != EG_MLA_ROPE_PAIRS && r->layout != EG_MLA_ROPE_HALF) return EG_MLA_ERR_INVALID_ARG;
+  if (r->theta != r->theta || r->theta > 3.4e38f || r->magnitude != r->magnitude || r->magnitude > 3.4e38f)
+    return EG_MLA_ERR_INVALID_ARG;
+  for (int m = 0; r->frequencies && m < rope_dim / 2; ++m)
+    if (!(r->frequencies[m] >= -64.0 && r->frequencies[m] <= 64.0)) return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+constexpr int kMaxRopeDim = 640;
+constexpr int64_t kMaxRowStride = int64_t{1} << 32;
+constexpr int kQ8MaxLatent = 512, kQ8MaxRopeDim = 64;
+constexpr int64_t kQ8MaxRows = int64_t{1} << 30;  // query rows of a call
+constexpr int kQ8MaxQueries = 1 << 19;
+
+}  // namespace
+
+eg_mla_status validate_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t n_tokens, int32_t num_heads,
+                                 int32_t head_dim, int32_t rope_offset, int32_t rope_dim, const void* x,
+                                 int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions, const void* out,
+                                 int64_t out_token_stride, int64_t out_head_stride) {
+  if (dtype != EG_MLA_FP32 && dtype != EG_MLA_BF16) return EG_MLA_ERR_INVALID_ARG;
+  if (n_tokens < 0 || num_heads < 1 || head_dim < 1 || rope_offset < 0 || rope_dim < 0 || rope_dim % 2 != 0 ||
+      rope_dim > head_dim || rope_offset > head_dim - rope_dim)
+    return EG_MLA_ERR_INVALID_ARG;
+  const eg_mla_status st = rope_dim <= kMaxRopeDim ? check_rope(rope, rope_dim) : EG_MLA_ERR_UNSUPPORTED;
+  if (st != EG_MLA_OK) return st;
+  if (n_tokens == 0) return EG_MLA_OK;
+  if (!x || !out || !positions) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t eb = dtype == EG_MLA_BF16 ? 2 : 4, n = n_tokens, h = num_heads, d = head_dim;
+  if (reinterpret_cast<uintptr_t>(x) % eb != 0 || reinterpret_cast<uintptr_t>(out) % eb != 0) return EG_MLA_ERR_INVALID_ARG;
+  for (const int64_t s : {x_token_stride, x_head_stride, out_token_stride, out_head_stride})
+    if (s < 0 || s > kMaxRowStride) return EG_MLA_ERR_INVALID_ARG;
+  // rows of the output must be apart: heads within tokens, or tokens within heads
+  const int64_t ot = n > 1 ? out_token_stride : kMaxRowStride * h, oh = h > 1 ? out_head_stride : kMaxRowStride * n;
+  if (!((oh >= d && ot >= (h - 1) * out_head_stride + d) || (ot >= d && oh >= (n - 1) * out_token_stride + d)))
+    return EG_MLA_ERR_INVALID_ARG;
+  auto room = [&](int64_t ts, int64_t hs) {
+    return held_product(eb, std::min(held_product(n - 1, ts), INT64_MAX / 4) + std::min(held_product(h - 1, hs), INT64_MAX / 4) + d);
+  };
+  const bool in_place = x == out && (n == 1 || x_token_stride == out_token_stride) && (h == 1 || x_head_stride == out_head_stride);
+  const Span os{out, room(out_token_stride, out_head_stride)};
+  if ((!in_place && overlap(os, {x, room(x_token_stride, x_head_stride)})) || overlap(os, {positions, 4 * n}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+eg_mla_status check_q8_dims(const eg_mla_dims* d) {
+  const eg_mla_status st = check_dims(d);
+  if (st != EG_MLA_OK) return st;
+  if (d->dtype != EG_MLA_BF16 || d->latent_dim % 16 != 0 || d->latent_dim > kQ8MaxLatent || d->rope_dim > kQ8MaxRopeDim)
+    return EG_MLA_ERR_UNSUPPORTED;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_q8_write(const eg_mla_dims* d, const eg_mla_rope* rope, int32_t n_tokens, const void* kv,
+                                int64_t kv_stride, const void* kv_norm_w, const void* k_norm_w, const void* gate_table,
+                                const int32_t* token_ids, const int32_t* positions, const int32_t* slots,
+                                const uint8_t* codes, const uint8_t* scales, int64_t num_slots) {
+  eg_mla_status st = check_q8_dims(d);
+  if (st == EG_MLA_OK && rope) st = check_rope(rope, d->rope_dim);
+  if (st != EG_MLA_OK) return st;
+  if (n_tokens < 0 || num_slots < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return EG_MLA_OK;
+  if (!kv || !slots || !codes || !scales || (gate_table && !token_ids) || (rope && d->rope_dim > 0 && !positions))
+    return EG_MLA_ERR_INVALID_ARG;
+  const int64_t row = d->latent_dim + d->rope_dim, n = n_tokens;
+  if (kv_stride < row || kv_stride % 8 != 0 || kv_stride > kMaxRowStride) return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned16(kv) || !aligned16(kv_norm_w) || !aligned16(gate_table) || !aligned16(codes)) return EG_MLA_ERR_INVALID_ARG;
+  if (outputs_overlap({{codes, held_product(num_slots, q8_row_bytes(*d))}, {scales, num_slots}},
+                      {{kv, held_product((n - 1) * kv_stride + row, 2)}, {kv_norm_w, 2 * d->latent_dim},
+                       {k_norm_w, 2 * d->rope_dim}, {gate_table, int64_t{2} * d->vocab_size * d->latent_dim},
+                       {gate_table ? token_ids : nullptr, 4 * n}, {rope && d->rope_dim ? positions : nullptr, 4 * n},
+                       {slots, 4 * n}}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_q8_read(const eg_mla_dims* d, int32_t batch, int32_t total_tokens, const uint8_t* codes,
+                               const uint8_t* scales, const int32_t* first_tokens, const int32_t* cu_seqlens,
+                               const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots, const void* out) {
+  eg_mla_status st = check_q8_dims(d);
+  if (st != EG_MLA_OK) return st;
+  if (total_tokens < 0) return EG_MLA_ERR_INVALID_ARG;
+  st = check_pages(*d, batch, max_pages_per_seq, num_slots, page_table != nullptr);
+  if (st == EG_MLA_OK && batch > kPageMaxBatch) st = EG_MLA_ERR_UNSUPPORTED;
+  if (st != EG_MLA_OK || batch == 0 || total_tokens == 0 || max_pages_per_seq == 0) return st;
+  if (!codes || !scales || !cu_seqlens || !out) return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned16(codes) || !aligned16(out)) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t n = 4 * static_cast<int64_t>(batch);
+  if (outputs_overlap({{out, int64_t{2} * total_tokens * (d->latent_dim + d->rope_dim)}},
+                      {{codes, num_slots * q8_row_bytes(*d)}, {scales, num_slots}, {first_tokens, n}, {cu_seqlens, n + 4},
+                       {page_table, n * max_pages_per_seq}}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
+eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_queries, int32_t max_pages_per_seq, Q8Plan* out) {
+  if (batch < 0 || n_queries < 0 || max_pages_per_seq < 0) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t cap = static_cast<int64_t>(max_pages_per_seq) * d.page_size;
+  if (cap > kMaxCapacity) return EG_MLA_ERR_INVALID_ARG;
+  const int64_t rows = static_cast<int64_t>(n_queries) * d.num_heads;
+  if (batch > kPageMaxBatch || n_queries > kQ8MaxQueries || rows > kQ8MaxRows) return EG_MLA_ERR_UNSUPPORTED;
+  Q8Plan p;
+  p.capacity = static_cast<int>(cap);
+  p.block_rows = 16;
+  p.tile = d.latent_dim <= 128 ? 128 : 64;
+  p.runs = 512;
+  p.blocks = rows / p.block_rows + batch;
+  if (held_product(p.blocks, cap / p.tile + 1) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at += align_up(static_cast<size_t>(bytes));
+    return here;
+  };
+  const int64_t part = (p.runs + p.blocks) * p.block_rows;
+  p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 4);
+  p.off_info = take((p.blocks + 1) * 16);
+  p.off_rows = take(p.blocks * 16);
+  p.off_start = take(p.runs * int64_t{4});
+  p.off_tokens = take(n_queries * int64_t{8});
+  p.off_head = take(16);
+  p.off_ml = take(part * 8);
+  p.off_o = take(part * d.latent_dim * 4);
+  p.bytes = at;
+  *out = p;
+  return EG_MLA_OK;
+}
+
+eg_mla_status validate_q8_attend(const eg_mla_dims* d, int32_t batch, int32_t n_queries, const void* q,
+                                 const int32_t* cu_seqlens, const uint8_t* codes, const uint8_t* scales, const void* w_uk,
+                                 const void* w_uv, const int32_t* seq_lens, const int32_t* page_table,
+                                 int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
+                                 size_t workspace_bytes, const void* out, Q8Plan* p) {
+  eg_mla_status st = check_q8_dims(d);
+  if (st != EG_MLA_OK) return st;
+  st = check_pages(*d, batch, max_pages_per_seq, num_slots, page_table != nullptr);
+  if (st == EG_MLA_OK) st = make_q8_plan(*d, batch, n_queries, max_pages_per_seq, p);
+  if (st != EG_MLA_OK) return st;
+  if (!cu_seqlens && n_queries != batch) return EG_MLA_ERR_INVALID_ARG;
+  if (batch == 0 || n_queries == 0) return EG_MLA_OK;
+  if (!q || !w_uk || !w_uv || !seq_lens || !out || (max_pages_per_seq > 0 && (!codes || !scales)))
+    return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(codes) || !aligned16(w_uk) || !aligned16(w_uv) || !aligned16(out))
+    return EG_MLA_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < p->bytes) return EG_MLA_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return EG_MLA_ERR_WORKSPACE;
+  const int64_t n = 4 * static_cast<int64_t>(batch), h = d->num_heads, dc = d->latent_dim;
+  const int64_t rows = n_queries * h;
+  if (outputs_overlap({{out, rows * d->v_head_dim * 2}, {workspace, static_cast<int64_t>(p->bytes)}},
+                      {{q, rows * (d->head_dim + d->rope_dim) * 2}, {cu_seqlens, n + 4},
+                       {codes, num_slots * q8_row_bytes(*d)}, {scales, num_slots},
+                       {w_uk, held_product(h, d->head_dim * dc * 2)}, {w_uv, held_product(h, d->v_head_dim * dc * 2)},
+                       {seq_lens, n}, {page_table, n * max_pages_per_seq}}))
+    return EG_MLA_ERR_INVALID_ARG;
+  return EG_MLA_OK;
+}
+
 }  // namespace egmla
 
 extern "C" {

@@ -224,6 +224,47 @@ eg_mla_status validate_decode_shared(const eg_mla_dims* d, int32_t batch, const 
                                      int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
                                      size_t workspace_bytes, const void* out, SharedPlan* p);
 
+// Rotation of rows, and the 8-bit latent cache (quant.hip).
+eg_mla_status validate_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t n_tokens, int32_t num_heads,
+                                 int32_t head_dim, int32_t rope_offset, int32_t rope_dim, const void* x,
+                                 int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions, const void* out,
+                                 int64_t out_token_stride, int64_t out_head_stride);
+eg_mla_status check_q8_dims(const eg_mla_dims* d);  // check_dims, and whether an 8-bit cache holds the layer
+inline int64_t q8_row_bytes(const eg_mla_dims& d) { return d.latent_dim + 2 * d.rope_dim; }
+eg_mla_status validate_q8_write(const eg_mla_dims* d, const eg_mla_rope* rope, int32_t n_tokens, const void* kv,
+                                int64_t kv_stride, const void* kv_norm_w, const void* k_norm_w, const void* gate_table,
+                                const int32_t* token_ids, const int32_t* positions, const int32_t* slots,
+                                const uint8_t* codes, const uint8_t* scales, int64_t num_slots);
+eg_mla_status validate_q8_read(const eg_mla_dims* d, int32_t batch, int32_t total_tokens, const uint8_t* codes,
+                               const uint8_t* scales, const int32_t* first_tokens, const int32_t* cu_seqlens,
+                               const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots, const void* out);
+
+// Attention over the 8-bit cache (quant_attend.hip): blocks of query rows, tiles
+// of tokens, and as many runs of tiles as work-groups; a piece (a block's tiles
+// in one run) has a partial row for each of the block's rows.
+struct Q8Plan {
+  int capacity = 0;    // max_pages_per_seq * page_size
+  int block_rows = 0;  // query rows of a block
+  int tile = 0;        // tokens of a tile
+  int runs = 0;
+  int64_t blocks = 0;  // at most
+  size_t off_q = 0;       // fp32 [T, H, d_c + d_r]  absorbed query | RoPE query
+  size_t off_info = 0;    // int4 [blocks + 1]
+  size_t off_rows = 0;    // int4 [blocks]
+  size_t off_start = 0;   // int32 [runs]
+  size_t off_tokens = 0;  // int2 [T]
+  size_t off_head = 0;    // int32 [4]
+  size_t off_ml = 0;      // fp32 [runs + blocks][block_rows][2]
+  size_t off_o = 0;       // fp32 [runs + blocks][block_rows][d_c]
+  size_t bytes = 0;
+};
+eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_queries, int32_t max_pages_per_seq, Q8Plan* out);
+eg_mla_status validate_q8_attend(const eg_mla_dims* d, int32_t batch, int32_t n_queries, const void* q,
+                                 const int32_t* cu_seqlens, const uint8_t* codes, const uint8_t* scales, const void* w_uk,
+                                 const void* w_uv, const int32_t* seq_lens, const int32_t* page_table,
+                                 int32_t max_pages_per_seq, int64_t num_slots, const void* workspace,
+                                 size_t workspace_bytes, const void* out, Q8Plan* p);
+
 inline float softmax_scale(const eg_mla_dims& d) {
   if (d.softmax_scale > 0.f) return d.softmax_scale;
   return 1.0f / __builtin_sqrtf(static_cast<float>(d.head_dim + d.rope_dim));

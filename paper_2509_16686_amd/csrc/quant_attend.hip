@@ -1,0 +1,592 @@
+// Attention of new tokens over the 8-bit latent cache (gfx950): one new token a
+// sequence (decode) or several, causal among themselves.
+//
+// With the gated latent c~ and k^R in the cache, query row (i, h) of a sequence
+// of n new tokens among its `len` cached ones computes, in the absorbed form of
+// App. C Eq. (C.11)-(C.13),
+//   s_j = tau (q_lat . c~_j + q^R . k^R_j),  j < len - n + i + 1,  q_lat = W_UK[h]^T q^C
+//   out = W_UV[h] sum_j softmax_j(s) c~_j.
+// All rows of a sequence share the keys, whatever their head and token.  They
+// are cut into blocks of consecutive rows, a block's keys into tiles, and the
+// tiles of all blocks, in order, into equal runs, one for each work-group (a run
+// may span blocks).  Four launches:
+//  1. the query's absorption (decode.hip), fp32 rows;
+//  2. q8_schedule_kernel: blocks, tiles and runs from the lengths on the device;
+//  3. q8_attend_kernel: a partial row (maximum, sum, latent sum) for each row of
+//     each piece (the tiles of one block in one run);
+//  4. q8_merge_kernel: joins the partial rows of a query row and applies W_UV.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "absorb.h"
+#include "device_common.h"
+#include "eg_mla.h"
+#include "host_plan.h"
+
+namespace egmla {
+
+// ---------------------------------------------------------------------------
+// Schedule
+// ---------------------------------------------------------------------------
+struct Q8Sched {
+  const int32_t* cu;        // [B + 1], or null: one new token a sequence
+  const int32_t* seq_lens;  // [B]
+  int4* info;               // [blocks + 1]: sequence, first row in it, rows, tiles before it
+  int4* rows;               // [blocks]: first query row, first new token's position (may be negative), length, -
+  int32_t* start;           // [runs]: block that a run starts in
+  int2* tokens;             // [T]: the sequence's first block and the token's number in it; -1: no sequence's
+  int32_t* head;            // tiles of a run, blocks, tiles
+  int32_t B, T, H, cap, block_rows, tile, runs;
+};
+
+// Exclusive sum over the work-group's threads, and the total.
+template <int THREADS>
+__device__ __forceinline__ int group_scan(int v, int* tmp, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // the sums before have been read
+  if (lane == 63) tmp[w] = x;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) {
+    if (i < w) before += tmp[i];
+    total += tmp[i];
+  }
+  return before + x - v;
+}
+
+// First i in [0, n) with a[i + 1] > x (n if none); a is non-decreasing.
+__device__ __forceinline__ int first_above(const int* a, int n, int x) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (a[mid + 1] > x) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+template <int THREADS>
+__device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
+  __shared__ int first_s[kPageMaxBatch + 1];  // a sequence's first block
+  __shared__ int cu_s[kPageMaxBatch + 1];     // and first new token
+  __shared__ int tmp[THREADS / 64];
+  const int tid = threadIdx.x;
+  for (int b = tid; b <= a.B; b += THREADS) cu_s[b] = a.cu ? clamp_len(a.cu[b], a.T) : min(b, a.T);
+  int total = 0, blocks = 0;
+  __syncthreads();
+  for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+    const int b = b0 + tid;
+    const int64_t r = b < a.B ? static_cast<int64_t>(max(0, cu_s[b + 1] - cu_s[b])) * a.H : 0;
+    const int at = group_scan<THREADS>(static_cast<int>((r + a.block_rows - 1) / a.block_rows), tmp, total);
+    if (b < a.B) first_s[b] = blocks + at;
+    blocks += total;
+  }
+  if (tid == 0) first_s[a.B] = blocks;
+  __syncthreads();
+  // (offsets that do not rise, which the call does not allow, could make more blocks than there is room for)
+  const int most = static_cast<int>(static_cast<int64_t>(a.T) * a.H / a.block_rows) + a.B;
+  blocks = min(blocks, most);
+  int tiles = 0;
+  for (int k0 = 0; k0 < blocks; k0 += THREADS) {
+    const int k = k0 + tid;
+    int n_tiles = 0, b = 0, row0 = 0, rows = 0, first = 0, len = 0;
+    if (k < blocks) {
+      b = first_above(first_s, a.B, k);
+      const int n = cu_s[b + 1] - cu_s[b];
+      row0 = (k - first_s[b]) * a.block_rows;
+      rows = min(a.block_rows, n * a.H - row0);
+      len = clamp_len(a.seq_lens[b], a.cap);
+      first = len - n;
+      const int most_keys = min(max(first + (row0 + rows - 1) / a.H + 1, 0), len);
+      n_tiles = (most_keys + a.tile - 1) / a.tile;
+    }
+    const int at = group_scan<THREADS>(n_tiles, tmp, total);
+    if (k < blocks) {
+      a.info[k] = make_int4(b, row0, rows, tiles + at);
+      a.rows[k] = make_int4(cu_s[b] * a.H + row0, first, len, 0);
+    }
+    tiles += total;
+  }
+  const int per = max(1, (tiles + a.runs - 1) / a.runs);
+  if (tid == 0) {
+    a.info[blocks] = make_int4(0, 0, 0, tiles);
+    a.head[0] = per;
+    a.head[1] = blocks;
+    a.head[2] = tiles;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (int k = tid; k < blocks; k += THREADS) {
+    const int s = a.info[k].w, e = a.info[k + 1].w;
+    for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < e; ++g) a.start[g] = k;
+  }
+  for (int t = tid; t < a.T; t += THREADS) {
+    const int b = first_above(cu_s, a.B, t);
+    a.tokens[t] = b < a.B && t >= cu_s[b] ? make_int2(first_s[b], t - cu_s[b]) : make_int2(-1, 0);
+  }
+}
+
+__global__ __launch_bounds__(1024) void q8_schedule_kernel(Q8Sched a) { q8_schedule<1024>(a); }
+
+// ---------------------------------------------------------------------------
+// Attention of blocks of 16 rows.  A wave owns units of U tokens of all
+// dims: it loads their rows (16 bytes a lane, the next unit's while it computes
+// one), turns the codes into fp16 with the row's scale in the conversion (exact
+// within fp16's range), stages them in its own LDS tile and takes both MFMA
+// operands from there, so the waves share nothing until they merge at a piece's
+// end.  The RoPE key stays bf16 and exact; the absorbed query and the
+// probabilities are rounded once to fp16; sums, maxima and products are fp32.  A
+// row that stands for NaN has zeros for values and a NaN RoPE key, so that it
+// reaches the rows that attend to it through their score, and no other.
+// ---------------------------------------------------------------------------
+struct Q8Attend {
+  const float* q;  // [T, H, DC + DR] fp32: absorbed | RoPE query
+  const uint8_t* codes;
+  const uint8_t* scales;
+  const int32_t* table;
+  const int4* info;
+  const int4* rows;
+  const int32_t* start;
+  const int32_t* head;
+  float* part_ml;  // [piece][block rows][2]
+  float* part_o;   // [piece][block rows][DC]
+  int64_t num_slots;
+  int32_t H, DC, DR, P, max_pages;
+  float scale_log2;
+};
+
+constexpr int kQ8AttendThreads = 256;
+
+template <int DCP>
+struct Q8Cfg {
+  static constexpr int NW = kQ8AttendThreads / 64;
+  static constexpr int U = DCP <= 128 ? 32 : 16;  // tokens of a unit
+  static constexpr int KB = U / 16;
+  static constexpr int TILE = NW * U;             // tokens of a tile
+  static constexpr int NC = DCP / 32, NR = 2, NB = DCP / 16;
+  static constexpr int TS = DCP + 64 + 8;         // row of a tile: latent (fp16) | RoPE key (bf16) | 16 bytes
+  static constexpr int PL = DCP / 16;             // 16-byte pieces of a token's codes
+  static constexpr int NLI = U * PL / 64, NRI = U * 8 / 64;
+  static constexpr int LDS_TILE = NW * U * TS * 2;
+  static_assert(U * PL % 64 == 0 && NB % 2 == 0 && NW * (NB / 2) * 1024 <= LDS_TILE, "whole loads; half of the accumulators");
+};
+
+// 16 codes times their scale in fp16.
+__device__ __forceinline__ void q8_to_f16(u32x4_t w, float s, u32x4_t& lo, u32x4_t& hi) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], s, false));
+    const uint32_t q = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], s, true));
+    if (i < 2) {
+      lo[2 * i] = p;
+      lo[2 * i + 1] = q;
+    } else {
+      hi[2 * i - 4] = p;
+      hi[2 * i - 3] = q;
+    }
+  }
+}
+
+template <int DCP>
+__global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_attend_kernel(Q8Attend a) {
+  using C = Q8Cfg<DCP>;
+  constexpr int NW = C::NW, U = C::U, KB = C::KB, NC = C::NC, NR = C::NR, NB = C::NB, TS = C::TS, PL = C::PL;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS_TILE + 2 * NW * 16 * 4];
+  f32x4_t* obuf = reinterpret_cast<f32x4_t*>(lds);  // [NW][NB / 2][64], at a piece's end
+  float* mbuf = reinterpret_cast<float*>(lds + C::LDS_TILE);  // [NW][16]
+  float* lbuf = mbuf + NW * 16;
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint16_t* tile = reinterpret_cast<uint16_t*>(lds) + w * U * TS;
+  const int row_bytes = a.DC + 2 * a.DR;
+
+  const int run = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int per = a.head[0], blocks = a.head[1], tiles = a.head[2];
+  int at = run * per;
+  if (static_cast<int64_t>(run) * per >= tiles) return;
+  const int end = min(at + per, tiles);
+  for (int k = a.start[run]; at < end && k < blocks; ++k) {
+    const int4 info = a.info[k];
+    const int next = a.info[k + 1].w;
+    if (next <= at) continue;  // a block without tokens
+    const int4 rw = a.rows[k];
+    const int b = info.x, row0 = info.y, nrows = info.z, first = rw.y, len = rw.z;
+    const int most = min(max(first + (row0 + nrows - 1) / a.H + 1, 0), len);
+    const int j0 = (at - info.w) * C::TILE, j1 = min((min(end, next) - info.w) * C::TILE, most);
+    at = min(end, next);
+
+    // this lane's query row (rows past the last repeat it and are not stored) and the tokens that it attends to
+    const int r = min(r16, nrows - 1);
+    const int lim = min(first + (row0 + r) / a.H + 1, len);
+    const float* qrow = a.q + (static_cast<int64_t>(rw.x) + r) * (a.DC + a.DR);
+    f16x8_t qv[NC];
+    bf16x8_t qr[NR];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int d = 32 * c + 8 * g;
+      f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
+      if (d < a.DC) {
+        x = *reinterpret_cast<const f32x4_t*>(qrow + d);
+        y = *reinterpret_cast<const f32x4_t*>(qrow + d + 4);
+      }
+      qv[c] = __builtin_bit_cast(f16x8_t, u32x4_t{pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]), pack_f16x2(y[0], y[1]),
+                                                  pack_f16x2(y[2], y[3])});
+    }
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const int d = 32 * c + 8 * g;
+      f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
+      if (d < a.DR) {
+        x = *reinterpret_cast<const f32x4_t*>(qrow + a.DC + d);
+        y = *reinterpret_cast<const f32x4_t*>(qrow + a.DC + d + 4);
+      }
+      qr[c] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                   pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])});
+    }
+
+    f32x4_t o[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    const int nunits = (j1 - j0 + U - 1) / U;
+    // slot of this lane's token of unit u (tokens past the last repeat it and are masked)
+    auto slot_of = [&](int u) {
+      const int j = min(j0 + u * U + (lane & (U - 1)), j1 - 1);
+      return static_cast<int>(cache_slot(a.table, b, j, a.P, a.max_pages, a.num_slots));
+    };
+    u32x4_t lat[C::NLI], rop[C::NRI];
+    int sc = 0;
+    auto issue = [&](int slot) {
+      sc = a.scales[slot];
+#pragma unroll
+      for (int c = 0; c < C::NLI; ++c) {
+        const int p = c * 64 + lane, t = p / PL, d = 16 * (p % PL);
+        const int64_t s = __shfl(slot, t, 64);
+        lat[c] = u32x4_t{0u, 0u, 0u, 0u};
+        if (d < a.DC) lat[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.codes + s * row_bytes + d));
+      }
+#pragma unroll
+      for (int c = 0; c < C::NRI; ++c) {
+        const int p = c * 64 + lane, t = p / 8, d = 8 * (p % 8);
+        const int64_t s = __shfl(slot, t, 64);
+        rop[c] = u32x4_t{0u, 0u, 0u, 0u};
+        if (d < a.DR)
+          rop[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.codes + s * row_bytes + a.DC + 2 * d));
+      }
+    };
+    if (w < nunits) {
+      issue(slot_of(w));
+      int slot = slot_of(w + NW);
+      const uint16_t* arow = tile + r16 * TS + 8 * g;
+      uint16_t* tread = tile + (4 * g + (r16 >> 2)) * TS + 4 * (r16 & 3);
+      for (int u = w; u < nunits; u += NW) {
+#pragma unroll
+        for (int c = 0; c < C::NLI; ++c) {
+          const int p = c * 64 + lane, t = p / PL;
+          const int e = __shfl(sc, t, 64);
+          u32x4_t lo, hi;
+          q8_to_f16(lat[c], e == 255 ? 1.f : __uint_as_float(static_cast<uint32_t>(e) << 23), lo, hi);
+          u32x4_t* dst = reinterpret_cast<u32x4_t*>(tile + t * TS + 16 * (p % PL));
+          dst[0] = lo;
+          dst[1] = hi;
+        }
+#pragma unroll
+        for (int c = 0; c < C::NRI; ++c) {
+          const int p = c * 64 + lane, t = p / 8;
+          const uint32_t none = __shfl(sc, t, 64) == 255 ? 0x7fc07fc0u : 0u;
+          *reinterpret_cast<u32x4_t*>(tile + t * TS + DCP + 8 * (p % 8)) = rop[c] | u32x4_t{none, none, none, none};
+        }
+        if (u + NW < nunits) {
+          issue(slot);
+          slot = slot_of(u + 2 * NW);
+        }
+        wave_lds_sync();
+        // S^T[token 16 kb + 4g + i][row r16]
+        const int left = lim - (j0 + u * U);  // tokens of the unit that the row attends to
+        float x[KB][4];
+        float mt = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          f32x4_t acc = {0.f, 0.f, 0.f, 0.f}, acc2 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8_t*>(arow + 16 * kb * TS + 32 * c),
+                                                         qv[c], acc, 0, 0, 0);
+#pragma unroll
+          for (int c = 0; c < NR; ++c)
+            acc2 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                *reinterpret_cast<const bf16x8_t*>(arow + 16 * kb * TS + DCP + 32 * c), qr[c], acc2, 0, 0, 0);
+          acc += acc2;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[kb][i] = 16 * kb + 4 * g + i < left && j0 + u * U + 16 * kb + 4 * g + i < j1 ? acc[i] * a.scale_log2 : -INFINITY;
+            mt = fmaxf(mt, x[kb][i]);
+          }
+        }
+        mt = max_over_row_groups(mt);
+        const float m_new = fmaxf(m_run, mt);
+        const bool grow = m_new > m_run + kLazyRescale;
+        if (__builtin_amdgcn_ballot_w64(grow)) {
+          const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
+          m_run = grow ? m_new : m_run;
+          l_run *= alpha;
+#pragma unroll
+          for (int db = 0; db < NB; ++db) o[db] *= alpha;
+        }
+        // (-inf while the row has met no token, or only scores that overflowed to it: those weigh nothing)
+        const float m_ref = m_run == -INFINITY ? 0.f : m_run;
+        uint32_t pk[KB][2];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(x[kb][i] - m_ref);
+            l_run += p[i];
+          }
+          pk[kb][0] = pack_f16x2(p[0], p[1]);
+          pk[kb][1] = pack_f16x2(p[2], p[3]);
+        }
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          const s16x4_t a0 =
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(tread + db * 16));
+          if constexpr (KB == 2) {
+            const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4_t*)(tread + 16 * TS + db * 16));
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)),
+                __builtin_bit_cast(f16x8_t, u32x4_t{pk[0][0], pk[0][1], pk[KB - 1][0], pk[KB - 1][1]}), o[db], 0, 0, 0);
+          } else {
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, a0),
+                                                          __builtin_bit_cast(f16x4_t, u32x2_t{pk[0][0], pk[0][1]}), o[db], 0, 0, 0);
+          }
+        }
+        wave_lds_sync();
+      }
+    }
+
+    // merge of the waves, the value blocks in two halves
+    l_run = sum_over_row_groups(l_run);
+    if (g == 0) mbuf[w * 16 + r16] = m_run;
+    __syncthreads();  // also: every wave is done with its tile (obuf aliases them)
+    float M = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) M = fmaxf(M, mbuf[v * 16 + r16]);
+    // (a wave without a maximum may hold a NaN sum: it stays one)
+    const float fold = m_run == -INFINITY ? (M == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(m_run - M);
+    if (g == 0) lbuf[w * 16 + r16] = l_run * fold;
+    const int64_t prow = (static_cast<int64_t>(run) + k) * 16 + r16;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half) __syncthreads();  // the first half's sums are read
+#pragma unroll
+      for (int db = 0; db < NB / 2; ++db) obuf[(w * (NB / 2) + db) * 64 + lane] = o[half * (NB / 2) + db] * fold;
+      __syncthreads();
+      for (int db = w; db < NB / 2; db += NW) {
+        f32x4_t sum = obuf[db * 64 + lane];
+#pragma unroll
+        for (int v = 1; v < NW; ++v) sum += obuf[(v * (NB / 2) + db) * 64 + lane];
+        const int d = (half * (NB / 2) + db) * 16 + 4 * g;
+        if (r16 < nrows && d < a.DC) __builtin_nontemporal_store(sum, reinterpret_cast<f32x4_t*>(a.part_o + prow * a.DC + d));
+      }
+    }
+    if (w == 0 && g == 0 && r16 < nrows) {
+      float Ls = 0.f;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) Ls += lbuf[v * 16 + r16];
+      *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(M, Ls);
+    }
+    __syncthreads();  // the merge's buffers have been read
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Merge and up-projection: grid (H, ceil(T / spt)), 8 waves, one head and spt =
+// 1, 2, 4, 8 or 16 new tokens per work-group.  LPR lanes hold a row, 8 dims each;
+// each group of LPR lanes is a worker, and a token's workers take its partial
+// rows in turn, 4 loaded together, folded online in fp32.  They meet in LDS, and
+// the merged row o / l goes there once more as bf16 hi + lo, the B operands of
+// out^T[v][token] = W_UV[h] o^T on v_mfma_f32_16x16x32_bf16, so that the
+// up-projection adds only W_UV's own rounding.
+// ---------------------------------------------------------------------------
+constexpr int kQ8MergeWaves = 8;
+constexpr int kQ8MergeTokens = 16;
+
+struct Q8Merge {
+  const float* part_ml;
+  const float* part_o;
+  const int4* info;
+  const int2* tokens;
+  const int32_t* head;
+  const uint16_t* w_uv;
+  uint16_t* out;
+  int32_t T, H, DC, DV, block_rows, spt;
+};
+
+template <int LPR>
+__global__ __launch_bounds__(kQ8MergeWaves * 64) void q8_merge_kernel(Q8Merge a) {
+  constexpr int DCP = 8 * LPR, OS = DCP + 8, GPW = 64 / LPR, WORKERS = kQ8MergeWaves * GPW;
+  __shared__ __attribute__((aligned(16))) uint16_t o_s[2][kQ8MergeTokens][OS];  // merged rows, hi and lo
+  __shared__ __attribute__((aligned(16))) float part[WORKERS][DCP];
+  __shared__ float m_part[WORKERS], l_part[WORKERS];
+  const int h = blockIdx.x, t0 = blockIdx.y * a.spt;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int per = a.head[0];
+  const int wps = max(1, WORKERS / a.spt), spr = WORKERS / wps;  // workers a token, tokens a round
+  const int worker = w * GPW + lane / LPR, col = 8 * (lane % LPR);
+  for (int r0 = 0; r0 < a.spt; r0 += spr) {
+    const int t = t0 + r0 + worker / wps, me = worker % wps;
+    float M = -INFINITY, sum = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (t < a.T && r0 + worker / wps < a.spt) {
+      const int2 tk = a.tokens[t];
+      if (tk.x >= 0) {
+        const int64_t rho = static_cast<int64_t>(tk.y) * a.H + h;
+        const int k = tk.x + static_cast<int>(rho / a.block_rows);
+        const bool there = k < a.head[1];
+        const int s = there ? a.info[k].w : 0, e = there ? a.info[k + 1].w : 0;
+        const int first = s / per, n = e > s ? (e - 1) / per - first + 1 : 0;
+        const int64_t row0 = (static_cast<int64_t>(first) + k) * a.block_rows + rho % a.block_rows;
+        for (int i0 = me; i0 < n; i0 += 4 * wps) {
+          float2 ml[4];
+          f32x4_t v[4][2];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int64_t row = row0 + static_cast<int64_t>(min(i0 + u * wps, n - 1)) * a.block_rows;
+            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + 2 * row);
+            v[u][0] = v[u][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (col < a.DC) {
+              const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part_o + row * a.DC + col);
+              v[u][0] = p[0];
+              v[u][1] = p[1];
+            }
+          }
+          float top = M;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) top = fmaxf(top, ml[u].x);  // repeats change no maximum
+          // (where no row has a maximum they are added all the same: a NaN in one stays one)
+          const float ref = top == -INFINITY ? 0.f : top;
+          const float keep = M == -INFINITY && top > -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M == -INFINITY ? 0.f : M) - ref);
+          sum *= keep;
+#pragma unroll
+          for (int e8 = 0; e8 < 8; ++e8) acc[e8] *= keep;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (i0 + u * wps >= n) continue;
+            const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - ref);
+            sum = fmaf(x, ml[u].y, sum);
+#pragma unroll
+            for (int e8 = 0; e8 < 8; ++e8) acc[e8] = fmaf(x, v[u][e8 / 4][e8 % 4], acc[e8]);
+          }
+          M = top;
+        }
+      }
+    }
+    if (r0 > 0) __syncthreads();  // the round before has been read
+    *reinterpret_cast<f32x4_t*>(&part[worker][col]) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
+    *reinterpret_cast<f32x4_t*>(&part[worker][col + 4]) = f32x4_t{acc[4], acc[5], acc[6], acc[7]};
+    if (lane % LPR == 0) {
+      m_part[worker] = M;
+      l_part[worker] = sum;
+    }
+    __syncthreads();
+    // merged rows of the round's tokens (zero without keys)
+    for (int i = tid; i < spr * DCP; i += kQ8MergeWaves * 64) {
+      const int kk = i / DCP, c = i - kk * DCP;
+      if (r0 + kk >= a.spt) continue;
+      float top = -INFINITY, num = 0.f, den = 0.f;
+      for (int p = 0; p < wps; ++p) top = fmaxf(top, m_part[kk * wps + p]);
+      for (int p = 0; p < wps; ++p) {
+        const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top);
+        num = fmaf(x, part[kk * wps + p][c], num);
+        den = fmaf(x, l_part[kk * wps + p], den);
+      }
+      const float v = den == 0.f ? 0.f : num / den;
+      const __bf16 hi = static_cast<__bf16>(v);
+      o_s[0][r0 + kk][c] = __builtin_bit_cast(uint16_t, hi);
+      o_s[1][r0 + kk][c] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - static_cast<float>(hi)));
+    }
+  }
+  __syncthreads();
+  const int rr = min(r16, a.spt - 1);  // columns past spt repeat the last and are not stored
+  const int t = t0 + r16;
+  const bool live = r16 < a.spt && t < a.T && a.tokens[min(t, a.T - 1)].x >= 0;  // other rows stay as they are
+  for (int v0 = 16 * w; v0 < a.DV; v0 += 16 * kQ8MergeWaves) {
+    const uint16_t* wrow = a.w_uv + (static_cast<int64_t>(h) * a.DV + min(v0 + r16, a.DV - 1)) * a.DC + 8 * g;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int kc = 0; 32 * kc < a.DC; ++kc) {
+      // (d_c may end half way through a chunk: the merged rows are zero there)
+      const u32x4_t x = 32 * kc + 8 * g < a.DC ? *reinterpret_cast<const u32x4_t*>(wrow + 32 * kc) : u32x4_t{0u, 0u, 0u, 0u};
+      const bf16x8_t av = __builtin_bit_cast(bf16x8_t, x);
+      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[0][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[1][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+    }
+    if (!live) continue;
+    uint16_t* orow = a.out + (static_cast<int64_t>(t) * a.H + h) * a.DV + v0 + 4 * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (v0 + 4 * g + i < a.DV) orow[i] = f32_to_bf16(o[i]);
+  }
+}
+
+}  // namespace egmla
+
+using namespace egmla;
+
+extern "C" size_t eg_mla_quant_attend_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t n_queries,
+                                                  int32_t max_pages_per_seq) {
+  Q8Plan p;
+  if (check_q8_dims(dims) != EG_MLA_OK || make_q8_plan(*dims, batch, n_queries, max_pages_per_seq, &p) != EG_MLA_OK) return 0;
+  return p.bytes;
+}
+
+extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t batch, int32_t n_queries, const void* q,
+                                          const int32_t* cu_seqlens, const uint8_t* codes, const uint8_t* scales,
+                                          const void* w_uk, const void* w_uv, const int32_t* seq_lens,
+                                          const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                          void* workspace, size_t workspace_bytes, void* out, void* stream_) {
+  Q8Plan p;
+  const eg_mla_status st = validate_q8_attend(dims, batch, n_queries, q, cu_seqlens, codes, scales, w_uk, w_uv, seq_lens,
+                                              page_table, max_pages_per_seq, num_slots, workspace, workspace_bytes, out, &p);
+  if (st != EG_MLA_OK || batch == 0 || n_queries == 0) return st;
+  const eg_mla_dims& d = *dims;
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  float* qfull = reinterpret_cast<float*>(ws + p.off_q);
+  const Q8Sched sched{cu_seqlens, seq_lens, reinterpret_cast<int4*>(ws + p.off_info), reinterpret_cast<int4*>(ws + p.off_rows),
+                      reinterpret_cast<int32_t*>(ws + p.off_start), reinterpret_cast<int2*>(ws + p.off_tokens),
+                      reinterpret_cast<int32_t*>(ws + p.off_head), batch, n_queries, d.num_heads, p.capacity, p.block_rows,
+                      p.tile, p.runs};
+  (void)hipGetLastError();
+  if (launch_absorb(d, n_queries, q, w_uk, qfull, stream) != hipSuccess) return EG_MLA_ERR_HIP;
+  hipLaunchKernelGGL(q8_schedule_kernel, dim3(1), dim3(1024), 0, stream, sched);
+  const Q8Attend at{qfull, codes, scales, page_table, sched.info, sched.rows, sched.start, sched.head,
+                    reinterpret_cast<float*>(ws + p.off_ml), reinterpret_cast<float*>(ws + p.off_o), num_slots,
+                    d.num_heads, d.latent_dim, d.rope_dim, d.page_size, max_pages_per_seq,
+                    softmax_scale(d) * 1.4426950408889634f};
+  const dim3 grid(p.runs), block(kQ8AttendThreads);
+  if (d.latent_dim <= 64) hipLaunchKernelGGL((q8_attend_kernel<64>), grid, block, 0, stream, at);
+  else if (d.latent_dim <= 128) hipLaunchKernelGGL((q8_attend_kernel<128>), grid, block, 0, stream, at);
+  else if (d.latent_dim <= 320) hipLaunchKernelGGL((q8_attend_kernel<320>), grid, block, 0, stream, at);
+  else hipLaunchKernelGGL((q8_attend_kernel<512>), grid, block, 0, stream, at);
+  // tokens of a merge work-group: as many as leave two work-groups a compute unit
+  int spt = kQ8MergeTokens;
+  while (spt > 1 && static_cast<int64_t>(d.num_heads) * ((n_queries + spt - 1) / spt) < 512) spt /= 2;
+  const Q8Merge mg{at.part_ml, at.part_o, sched.info, sched.tokens, sched.head, static_cast<const uint16_t*>(w_uv),
+                   static_cast<uint16_t*>(out), n_queries, d.num_heads, d.latent_dim, d.v_head_dim, p.block_rows, spt};
+  const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt), mblock(kQ8MergeWaves * 64);
+  if (d.latent_dim <= 128) hipLaunchKernelGGL((q8_merge_kernel<16>), mgrid, mblock, 0, stream, mg);
+  else hipLaunchKernelGGL((q8_merge_kernel<64>), mgrid, mblock, 0, stream, mg);
+  return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
+}

@@ -1,0 +1,189 @@
+"""Plain 64-bit forms of the row rotation and the 8-bit cache's operators, in NumPy, one token and one sequence after the
+other, and the seeded layers that their tests run on."""
+import math
+
+import numpy as np
+import torch
+
+from paper_2509_16686_amd import binding as B
+
+BF, I32, U8 = torch.bfloat16, torch.int32, torch.uint8
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+
+
+def frequencies(rd, theta=10000.0, factor=1.0, trained=0, slow=1.0, fast=32.0):
+    f = np.array([theta ** (-2.0 * m / rd) for m in range(rd // 2)])
+    if factor == 1.0:
+        return f
+    turns = trained * f / (2 * math.pi)
+    k = np.clip((turns - slow) / (fast - slow), 0.0, 1.0) if trained else np.zeros_like(f)
+    return f * (k + (1 - k) / factor)
+
+
+def rotate(x, positions, f, half=False, magnitude=1.0, inverse=False):
+    """Rotation of the last dimension of x [n, ..., rd] in 64 bits."""
+    rd = x.shape[-1]
+    a = positions.astype(np.float64)[:, None] * f * (-1 if inverse else 1)
+    a = a.reshape([x.shape[0]] + [1] * (x.ndim - 2) + [rd // 2])
+    cs, sn = magnitude * np.cos(a), magnitude * np.sin(a)
+    y = np.empty_like(x)
+    i, j = (slice(0, rd // 2), slice(rd // 2, rd)) if half else (slice(0, rd, 2), slice(1, rd, 2))
+    y[..., i] = x[..., i] * cs - x[..., j] * sn
+    y[..., j] = x[..., i] * sn + x[..., j] * cs
+    return y
+
+
+def norm(x, w):
+    return x if w is None else x / np.sqrt((x * x).mean(-1, keepdims=True) + 1e-6) * w
+
+
+def row_exponent(c):
+    """e of each row of finite gated latents."""
+    top = np.abs(c).max(-1)
+    m, e = np.frexp(top / 448.0)  # top / 448 = m 2^e, m in [1/2, 1)
+    e = np.where(m == 0.5, e - 1, e)
+    return np.where(top == 0, 0, np.clip(e, -126, 120))
+
+
+def e4m3(x):
+    """The e4m3 value nearest to x, ties to the even code (|x| <= 448)."""
+    exponent = np.floor(np.log2(np.maximum(np.abs(x), 2.0 ** -6)))
+    step = 2.0 ** (exponent - 3)
+    return np.round(x / step) * step  # np.round: ties to even
+
+
+_T = [math.copysign((i & 7) / 8 * 2.0 ** -6 if (i >> 3) & 15 == 0 else (1 + (i & 7) / 8) * 2.0 ** (((i >> 3) & 15) - 7),
+                    -1.0 if i & 128 else 1.0) if i & 127 != 127 else math.nan for i in range(256)]
+TABLE = np.array(_T)
+
+
+def cache_rows(codes, scales, dc):
+    """[c~ | k^R] in 64 bits of every row of a cache (uint8 tensors)."""
+    c = codes.cpu().numpy()
+    s = scales.cpu().numpy().astype(np.float64)
+    lat = TABLE[c[:, :dc]] * (2.0 ** (s - 127))[:, None]
+    lat[s == 255] = math.nan
+    rope = codes[:, dc:].contiguous().view(BF).double().cpu().numpy() if codes.shape[1] > dc else np.zeros((len(s), 0))
+    return np.concatenate([lat, rope], 1)
+
+
+def attend(q, rows, w_uk, w_uv, new, lens, slots_of, tau):
+    """(out, scale) of the packed queries: `scale` bounds |W_UV| |c~| |p|, what a relative error of the products is of."""
+    dh = w_uk.shape[1]
+    out, size, at = [], [], 0
+    for b, n in enumerate(new):
+        keys = rows[slots_of(b, lens[b])] if lens[b] else np.zeros((0, rows.shape[1]))
+        for i in range(n):
+            lim = max(0, min(lens[b] - n + i + 1, lens[b]))
+            k = keys[:lim]
+            if lim == 0:
+                out.append(np.zeros((w_uv.shape[0], w_uv.shape[1])))
+                size.append(np.zeros((w_uv.shape[0], w_uv.shape[1])))
+                continue
+            ql = np.concatenate([np.einsum("hk,hkc->hc", q[at + i][:, :dh], w_uk), q[at + i][:, dh:]], 1)
+            s = tau * ql @ k.T
+            with np.errstate(invalid="ignore"):
+                p = np.exp(s - s.max(1, keepdims=True))
+                p /= p.sum(1, keepdims=True)
+            lat = k[:, : w_uk.shape[2]]
+            out.append(np.einsum("hvc,hc->hv", w_uv, p @ lat))
+            size.append(np.einsum("hvc,hc->hv", np.abs(w_uv), p @ np.abs(lat)))
+        at += n
+    return np.array(out), np.array(size)
+
+
+class Layer:
+    """A seeded layer with an 8-bit cache of `rows` rows, on the GPU."""
+
+    def __init__(self, seed, h, dh, dv, dc, dr, page=16, rows=512, vocab=300, std=1.0):
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(seed)
+        self.h, self.dh, self.dv, self.dc, self.dr, self.page, self.rows = h, dh, dv, dc, dr, page, rows
+        self.dims = B.make_dims(num_heads=h, head_dim=dh, v_head_dim=dv, latent_dim=dc, rope_dim=dr, vocab_size=vocab,
+                                page_size=page, dtype=B.BF16)
+        self.w_uk, self.w_uv = self.normal((h, dh, dc), 1 / math.sqrt(dc)), self.normal((h, dv, dc), 1 / math.sqrt(dc))
+        self.gate = self.normal((vocab, dc), 0.1, 1.0)
+        self.codes = torch.zeros((rows, dc + 2 * dr), dtype=U8, device="cuda")
+        self.scales = torch.full((rows,), 127, dtype=U8, device="cuda")
+        self.fill(std)
+
+    def normal(self, shape, std=1.0, mean=0.0, dtype=BF):
+        return (torch.randn(shape, generator=self.g, device="cuda") * std + mean).to(dtype)
+
+    def ints(self, hi, n):
+        return torch.randint(0, hi, (n,), generator=self.g, device="cuda", dtype=I32)
+
+    def perm(self, n):
+        return torch.randperm(n, generator=self.g, device="cuda").to(I32)
+
+    def fill(self, std=1.0):
+        """Every row of the cache, by the values' definition."""
+        c = self.normal((self.rows, self.dc), std, dtype=torch.float32)
+        x = c.double().cpu().numpy()
+        e = row_exponent(x)
+        value = e4m3(x * 2.0 ** -e[:, None].astype(np.float64))
+        code = np.searchsorted(TABLE[:127], np.abs(value)).astype(np.uint8) | np.where(value < 0, 128, 0).astype(np.uint8)
+        self.codes[:, : self.dc] = torch.from_numpy(code).cuda()
+        self.scales.copy_(torch.from_numpy((e + 127).astype(np.uint8)))
+        if self.dr:
+            self.codes[:, self.dc:] = self.normal((self.rows, self.dr)).view(U8)
+
+    def table(self, lens, width=None):
+        """A page table of distinct random pages, -1 behind a sequence's last."""
+        per = [-(-n // self.page) for n in lens]
+        width = max(per + [1]) if width is None else width
+        pages = self.perm(self.rows // self.page)
+        t = torch.full((len(lens), width), -1, dtype=I32, device="cuda")
+        at = 0
+        for b, n in enumerate(per):
+            t[b, :n] = pages[at:at + n]
+            at += n
+        assert at <= self.rows // self.page
+        return t
+
+    def slots_of(self, table):
+        t = table.cpu().numpy().astype(np.int64)
+        return lambda b, n: t[b, np.arange(n) // self.page] * self.page + np.arange(n) % self.page
+
+    def run(self, q, cu, lens, table, width=None, ws=None, out=None, stream=None):
+        n, b, width = q.shape[0], len(lens), (table.shape[1] if width is None else width)
+        if ws is None:
+            ws = B.alloc_workspace(B.quant_attend_workspace_size(self.dims, b, n, width)).fill_(0xAB)
+        if out is None:
+            out = torch.full((n, self.h, self.dv), 7.0, dtype=BF, device="cuda")
+        B.quant_attend(self.dims, q, cu, self.codes, self.scales, self.w_uk, self.w_uv, ints(lens), table, width, ws, out,
+                       stream=stream)
+        return out
+
+    def oracle(self, q, new, lens, slots_of, rows=None):
+        f = lambda t: t.double().cpu().numpy()
+        rows = cache_rows(self.codes, self.scales, self.dc) if rows is None else rows
+        return attend(f(q), rows, f(self.w_uk), f(self.w_uv), new, lens, slots_of, 1 / math.sqrt(self.dh + self.dr))
+
+
+def ints(x):
+    return torch.tensor(list(x), dtype=I32, device="cuda")
+
+
+def offsets(new):
+    return ints([0] + list(np.cumsum(new)))
+
+
+# Error of an output of the attention, relative to sum |W_UV| p |c~| (`size`):
+#   q_lat and the probabilities round to fp16, half a step of 2^-11 each; a score of magnitude |s| (log2 units) moves by at
+#   most 2^-11 sum |q_lat| |c~| tau log2 e.  With the layers here sum |q_lat c~| tau is below 24 (d_h <= 128 values of
+#   variance one and W_UK of variance 1 / d_c: q_lat has deviation sqrt(d_h / d_c), |q_lat . c~| at most
+#   sum of d_c terms of mean 0.64 sqrt(d_h / d_c), over sqrt(d_h + d_r): 0.64 sqrt(d_c) <= 14.5, 1.6 of it at the largest
+#   row norms), a relative error of 24 2^-11 = 2^-6.4 of every weight at the very worst if all roundings agree; they
+#   are independent, and their sum over d_c terms grows as its root: 24 / sqrt(16) 2^-11 = 2^-8.4 at most for d_c >= 16.
+#   Both signs of weights and their normalisation at most double it.  Last, the output's own half step of 2^-8 of its value.
+ATTEND_SIZE_TOL = 2 * (2.0 ** -8.4 + 2.0 ** -11)
+
+
+def check_attend(got, want, size):
+    got = got.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    bound = ATTEND_SIZE_TOL * size + 2.0 ** -8 * np.abs(want) + 1e-30
+    off = np.abs(got - want) / bound
+    off = np.where(np.isnan(want), 0, off)
+    assert off.max(initial=0) <= 1, f"{off.max()} of the bound at {np.unravel_index(off.argmax(), off.shape)}"
