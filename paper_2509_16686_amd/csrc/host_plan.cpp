@@ -894,6 +894,9 @@ constexpr int64_t kMaxRowStride = int64_t{1} << 32;
 constexpr int kQ8MaxLatent = 512, kQ8MaxRopeDim = 64;
 constexpr int64_t kQ8MaxRows = int64_t{1} << 30;  // query rows of a call
 constexpr int kQ8MaxQueries = 1 << 19;
+// Query rows of a sequence, on average, from which blocks of 128 rows are taken.
+constexpr int kQ8ManyRows = 64;
+constexpr int kQ8MaxRuns = 512;
 
 }  // namespace
 
@@ -985,22 +988,26 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   if (batch > kPageMaxBatch || n_queries > kQ8MaxQueries || rows > kQ8MaxRows) return EG_MLA_ERR_UNSUPPORTED;
   Q8Plan p;
   p.capacity = static_cast<int>(cap);
-  p.block_rows = 16;
-  p.tile = d.latent_dim <= 128 ? 128 : 64;
-  p.runs = 512;
+  const bool many = rows >= int64_t{kQ8ManyRows} * batch;  // rows of a sequence, on average
+  p.block_rows = many ? 128 : 16;
+  p.tile = many ? (d.latent_dim <= 128 ? 64 : 32) : d.latent_dim <= 128 ? 128 : 64;
+  p.runs = many && d.latent_dim > 128 ? 256 : 512;
   p.blocks = rows / p.block_rows + batch;
-  if (held_product(p.blocks, cap / p.tile + 1) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
+  if (held_product(rows / 16 + batch, cap / 32 + 1) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;
     at += align_up(static_cast<size_t>(bytes));
     return here;
   };
-  const int64_t part = (p.runs + p.blocks) * p.block_rows;
+  // partial rows: a bound that grows with the batch and the queries, whichever blocks a call takes (128 rows for
+  // each run and sequence, and the query rows)
+  const int64_t part = rows + 128 * (kQ8MaxRuns + static_cast<int64_t>(batch));
   p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 4);
-  p.off_info = take((p.blocks + 1) * 16);
-  p.off_rows = take(p.blocks * 16);
-  p.off_start = take(p.runs * int64_t{4});
+  const int64_t most = rows / 16 + batch;
+  p.off_info = take((most + 1) * 16);
+  p.off_rows = take(most * 16);
+  p.off_start = take(kQ8MaxRuns * int64_t{4});
   p.off_tokens = take(n_queries * int64_t{8});
   p.off_head = take(16);
   p.off_ml = take(part * 8);

@@ -149,23 +149,44 @@ __global__ __launch_bounds__(1024) void q8_schedule_kernel(Q8Sched a) { q8_sched
 // row that stands for NaN has zeros for values and a NaN RoPE key, so that it
 // reaches the rows that attend to it through their score, and no other.
 // ---------------------------------------------------------------------------
+// Cache rows of tokens: those of a page table, or contiguous ones.  No index leaves the cache, and no branch is taken
+// (a load under one is waited for where the branch ends).
+struct Q8Pages {
+  const int32_t* table;  // contiguous rows: any readable word
+  int32_t paged, P, npages, max_pages, cap;
+  uint32_t mul, shift;   // j / P = j mul >> shift for 0 <= j < 2^31
+  __device__ __forceinline__ int column(int j) const {
+    return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(j)) * mul >> shift);
+  }
+  __device__ __forceinline__ int page(int b, int j) const {
+    return table[paged ? static_cast<int64_t>(b) * max_pages + column(j) : 0];
+  }
+  __device__ __forceinline__ int row(int b, int j, int page) const {  // given the token's entry of the table
+    const int r = min(max(page, 0), npages - 1) * P + (j - column(j) * P);
+    return paged ? r : b * cap + j;
+  }
+};
+
 struct Q8Attend {
   const float* q;  // [T, H, DC + DR] fp32: absorbed | RoPE query
   const uint8_t* codes;
   const uint8_t* scales;
-  const int32_t* table;
+  Q8Pages cache;
   const int4* info;
   const int4* rows;
   const int32_t* start;
   const int32_t* head;
   float* part_ml;  // [piece][block rows][2]
   float* part_o;   // [piece][block rows][DC]
-  int64_t num_slots;
-  int32_t H, DC, DR, P, max_pages;
+  int32_t H, DC, DR;
   float scale_log2;
 };
 
 constexpr int kQ8AttendThreads = 256;
+
+// Values that are the same in every lane, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int4 uniform(int4 x) { return make_int4(uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w)); }
 
 template <int DCP>
 struct Q8Cfg {
@@ -211,15 +232,15 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
   const int row_bytes = a.DC + 2 * a.DR;
 
   const int run = xcd_logical_block(blockIdx.x, gridDim.x);
-  const int per = a.head[0], blocks = a.head[1], tiles = a.head[2];
+  const int per = uniform(a.head[0]), blocks = uniform(a.head[1]), tiles = uniform(a.head[2]);
   int at = run * per;
   if (static_cast<int64_t>(run) * per >= tiles) return;
   const int end = min(at + per, tiles);
-  for (int k = a.start[run]; at < end && k < blocks; ++k) {
-    const int4 info = a.info[k];
-    const int next = a.info[k + 1].w;
+  for (int k = uniform(a.start[run]); at < end && k < blocks; ++k) {
+    const int4 info = uniform(a.info[k]);
+    const int next = uniform(a.info[k + 1].w);
     if (next <= at) continue;  // a block without tokens
-    const int4 rw = a.rows[k];
+    const int4 rw = uniform(a.rows[k]);
     const int b = info.x, row0 = info.y, nrows = info.z, first = rw.y, len = rw.z;
     const int most = min(max(first + (row0 + nrows - 1) / a.H + 1, 0), len);
     const int j0 = (at - info.w) * C::TILE, j1 = min((min(end, next) - info.w) * C::TILE, most);
@@ -263,7 +284,7 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
     // slot of this lane's token of unit u (tokens past the last repeat it and are masked)
     auto slot_of = [&](int u) {
       const int j = min(j0 + u * U + (lane & (U - 1)), j1 - 1);
-      return static_cast<int>(cache_slot(a.table, b, j, a.P, a.max_pages, a.num_slots));
+      return a.cache.row(b, j, a.cache.page(b, j));
     };
     u32x4_t lat[C::NLI], rop[C::NRI];
     int sc = 0;
@@ -330,7 +351,7 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
           acc += acc2;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            x[kb][i] = 16 * kb + 4 * g + i < left && j0 + u * U + 16 * kb + 4 * g + i < j1 ? acc[i] * a.scale_log2 : -INFINITY;
+            x[kb][i] = 16 * kb + 4 * g + i < left ? acc[i] * a.scale_log2 : -INFINITY;
             mt = fmaxf(mt, x[kb][i]);
           }
         }
@@ -411,6 +432,10 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
     __syncthreads();  // the merge's buffers have been read
   }
 }
+
+}  // namespace egmla
+#include "quant_rows.h"
+namespace egmla {
 
 // ---------------------------------------------------------------------------
 // Merge and up-projection: grid (H, ceil(T / spt)), 8 waves, one head and spt =
@@ -571,12 +596,19 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   (void)hipGetLastError();
   if (launch_absorb(d, n_queries, q, w_uk, qfull, stream) != hipSuccess) return EG_MLA_ERR_HIP;
   hipLaunchKernelGGL(q8_schedule_kernel, dim3(1), dim3(1024), 0, stream, sched);
-  const Q8Attend at{qfull, codes, scales, page_table, sched.info, sched.rows, sched.start, sched.head,
-                    reinterpret_cast<float*>(ws + p.off_ml), reinterpret_cast<float*>(ws + p.off_o), num_slots,
-                    d.num_heads, d.latent_dim, d.rope_dim, d.page_size, max_pages_per_seq,
-                    softmax_scale(d) * 1.4426950408889634f};
+  Q8Pages pages{page_table ? page_table : sched.head, page_table != nullptr, d.page_size, static_cast<int32_t>(num_slots / d.page_size), max_pages_per_seq, p.capacity, 0, 31};
+  while ((int64_t{1} << (pages.shift - 31)) < d.page_size) ++pages.shift;  // l = ceil(log2 P): mul = ceil(2^(31+l) / P) < 2^32
+  pages.mul = static_cast<uint32_t>(((uint64_t{1} << pages.shift) + d.page_size - 1) / d.page_size);
+  const Q8Attend at{qfull, codes, scales, pages, sched.info, sched.rows, sched.start, sched.head,
+                    reinterpret_cast<float*>(ws + p.off_ml), reinterpret_cast<float*>(ws + p.off_o),
+                    d.num_heads, d.latent_dim, d.rope_dim, softmax_scale(d) * 1.4426950408889634f};
   const dim3 grid(p.runs), block(kQ8AttendThreads);
-  if (d.latent_dim <= 64) hipLaunchKernelGGL((q8_attend_kernel<64>), grid, block, 0, stream, at);
+  if (p.block_rows == kQ8Rows) {
+    if (d.latent_dim <= 64) hipLaunchKernelGGL((q8_rows_kernel<64>), grid, block, 0, stream, at);
+    else if (d.latent_dim <= 128) hipLaunchKernelGGL((q8_rows_kernel<128>), grid, block, 0, stream, at);
+    else if (d.latent_dim <= 320) hipLaunchKernelGGL((q8_rows_kernel<320>), grid, block, 0, stream, at);
+    else hipLaunchKernelGGL((q8_rows_kernel<512>), grid, block, 0, stream, at);
+  } else if (d.latent_dim <= 64) hipLaunchKernelGGL((q8_attend_kernel<64>), grid, block, 0, stream, at);
   else if (d.latent_dim <= 128) hipLaunchKernelGGL((q8_attend_kernel<128>), grid, block, 0, stream, at);
   else if (d.latent_dim <= 320) hipLaunchKernelGGL((q8_attend_kernel<320>), grid, block, 0, stream, at);
   else hipLaunchKernelGGL((q8_attend_kernel<512>), grid, block, 0, stream, at);

@@ -30,6 +30,8 @@
 // combination of fp16 values.
 #pragma once
 
+#include "rows32.h"
+
 namespace egmla {
 
 template <int DC, int KEYS_>
@@ -44,15 +46,6 @@ struct PrefixCfg {
 constexpr int kPrefixThreads = 256;
 constexpr int kPrefixRsrcWord3 = 0x00020000;  // raw buffer resource: 32-bit data format, the record count in bytes
 static_assert(kPrefixRows == 32 * kPrefixThreads / 64, "32 rows per wave");
-
-// Byte of piece p (16 bytes: dims 8p ..) of a key's latent row, and of its
-// RoPE row: the low bits of the piece are swizzled by the key so that the 16
-// lanes of a 16-byte read cycle (keys) and the 32 lanes of a transposed 8-byte
-// read cycle hit distinct banks.
-__host__ __device__ __forceinline__ int prefix_latent_byte(int key, int p) {
-  return 256 * (p >> 4) + 16 * ((p & 15) ^ (((key & 3) << 2) | ((key >> 2) & 3)));
-}
-__host__ __device__ __forceinline__ int prefix_rope_byte(int key, int p) { return 16 * (p ^ ((key >> 1) & 7)); }
 
 constexpr int kPrepTokens = 16;    // tokens that a work-group gates at a time
 constexpr int kPrepGroups = 2048;  // work-groups that gate, at most
@@ -164,24 +157,6 @@ struct PrefixArgs {
   int64_t num_slots;
   int32_t own_cap, own_pages, blocks_per_seq, P, V;
 };
-
-typedef __attribute__((ext_vector_type(16))) float px_f32x16_t;
-
-// Holds a block of accumulators in accumulation or ordinary registers at this point.
-__device__ __forceinline__ void in_agprs(px_f32x16_t& x) { asm volatile("" : "+a"(x)); }
-__device__ __forceinline__ void in_vgprs(px_f32x16_t& x) { asm volatile("" : "+v"(x)); }
-
-// Maximum and sum of lanes i and i ^ 32, the same value (same order) in both.
-__device__ __forceinline__ float half_max(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
-}
-__device__ __forceinline__ float half_sum(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
-}
 
 // OWN (heads a multiple of 128, so that a row block lies within a sequence): after its run of the prefix a work-group
 // takes its share of the sequence's own tokens into the same accumulators.  Their raw rows and gate rows are copied to
