@@ -40,10 +40,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kAbsorbRows = 16;
 constexpr int kAbsorbCols = 64;
 
-template <bool BF16>
+// HALF: 16-bit rows [q_lat fp16 | q^R bf16] in their place.
+template <bool BF16, bool HALF = false>
 __global__ __launch_bounds__(256) void absorb_kernel(const void* __restrict__ q, const void* __restrict__ w_uk,
                                                      float* __restrict__ qfull, int B, int H, int DH, int DC,
                                                      int DR) {
+  [[maybe_unused]] uint16_t* qhalf = reinterpret_cast<uint16_t*>(qfull);
   extern __shared__ float smem[];  // q rows [kAbsorbRows][DH], partial sums [4][kAbsorbRows][kAbsorbCols]
   float* q_s = smem;
   float* red = smem + kAbsorbRows * DH;
@@ -85,13 +87,18 @@ __global__ __launch_bounds__(256) void absorb_kernel(const void* __restrict__ q,
       float v = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) v += red[(j * kAbsorbRows + bb) * kAbsorbCols + cc];
-      qfull[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + c0 + cc] = v;
+      const int64_t at = (static_cast<int64_t>(b0 + bb) * H + h) * DQ + c0 + cc;
+      if constexpr (HALF) qhalf[at] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
+      else qfull[at] = v;
     }
   }
   if (blockIdx.y == 0) {
     for (int i = tid; i < nb * DR; i += 256) {
       const int bb = i / DR, r = i % DR;
-      qfull[(static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r] = ld<BF16>(q, (static_cast<int64_t>(b0 + bb) * H + h) * DQin + DH + r);
+      const int64_t at = (static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r;
+      const float v = ld<BF16>(q, (static_cast<int64_t>(b0 + bb) * H + h) * DQin + DH + r);
+      if constexpr (HALF) qhalf[at] = f32_to_bf16(v);
+      else qfull[at] = v;
     }
   }
 }
@@ -615,6 +622,18 @@ hipError_t launch_absorb_parts(const eg_mla_dims& d, int32_t batch, const void* 
   return hipGetLastError();
 }
 
+template <typename K>
+static hipError_t launch_absorb_any(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* rows,
+                                    K kern, hipStream_t stream) {
+  const dim3 grid(d.num_heads, (d.latent_dim + kAbsorbCols - 1) / kAbsorbCols, (batch + kAbsorbRows - 1) / kAbsorbRows);
+  const size_t lds = sizeof(float) * (kAbsorbRows * d.head_dim + 4 * kAbsorbRows * kAbsorbCols);
+  const hipError_t e = set_lds(kern, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, grid, dim3(256), lds, stream, q, w_uk, rows, batch, d.num_heads, d.head_dim, d.latent_dim,
+                     d.rope_dim);
+  return hipGetLastError();
+}
+
 hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* qfull,
                          hipStream_t stream) {
   const bool bf = d.dtype == EG_MLA_BF16;
@@ -630,14 +649,12 @@ hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, con
                        SchedArgs{});
     return hipGetLastError();
   }
-  const dim3 grid(d.num_heads, (d.latent_dim + kAbsorbCols - 1) / kAbsorbCols, (batch + kAbsorbRows - 1) / kAbsorbRows);
-  const size_t lds = sizeof(float) * (kAbsorbRows * d.head_dim + 4 * kAbsorbRows * kAbsorbCols);
-  auto kern = bf ? absorb_kernel<true> : absorb_kernel<false>;
-  hipError_t e = set_lds(kern, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, grid, dim3(256), lds, stream, q, w_uk, qfull, batch, d.num_heads, d.head_dim, d.latent_dim,
-                     d.rope_dim);
-  return hipGetLastError();
+  return launch_absorb_any(d, batch, q, w_uk, qfull, bf ? absorb_kernel<true> : absorb_kernel<false>, stream);
+}
+
+hipError_t launch_absorb_half(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, uint16_t* rows,
+                              hipStream_t stream) {
+  return launch_absorb_any(d, batch, q, w_uk, reinterpret_cast<float*>(rows), absorb_kernel<true, true>, stream);
 }
 
 namespace {

@@ -1003,7 +1003,7 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   // partial rows: a bound that grows with the batch and the queries, whichever blocks a call takes (128 rows for
   // each run and sequence, and the query rows)
   const int64_t part = rows + 128 * (kQ8MaxRuns + static_cast<int64_t>(batch));
-  p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 4);
+  p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 2);
   const int64_t most = rows / 16 + batch;
   p.off_info = take((most + 1) * 16);
   p.off_rows = take(most * 16);

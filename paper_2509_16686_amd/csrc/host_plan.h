@@ -248,7 +248,7 @@ struct Q8Plan {
   int tile = 0;        // tokens of a tile
   int runs = 0;
   int64_t blocks = 0;  // at most
-  size_t off_q = 0;       // fp32 [T, H, d_c + d_r]  absorbed query | RoPE query
+  size_t off_q = 0;       // 16-bit [T, H, d_c + d_r]  q_lat fp16 | q^R bf16
   size_t off_info = 0;    // int4 [blocks + 1]
   size_t off_rows = 0;    // int4 [blocks]
   size_t off_start = 0;   // int32 [runs]

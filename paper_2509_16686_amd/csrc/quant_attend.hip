@@ -9,18 +9,19 @@
 // All rows of a sequence share the keys, whatever their head and token.  They
 // are cut into blocks of consecutive rows, a block's keys into tiles, and the
 // tiles of all blocks, in order, into equal runs, one for each work-group (a run
-// may span blocks).  Four launches:
-//  1. the query's absorption (decode.hip), fp32 rows;
-//  2. q8_schedule_kernel: blocks, tiles and runs from the lengths on the device;
-//  3. q8_attend_kernel: a partial row (maximum, sum, latent sum) for each row of
-//     each piece (the tiles of one block in one run);
-//  4. q8_merge_kernel: joins the partial rows of a query row and applies W_UV.
+// may span blocks).  Three launches:
+//  1. q8_prep_kernel: the query's absorption, 16-bit rows, and (one work-group) blocks, tiles and runs from the lengths
+//     on the device (d_h other than 64 and 128: two launches);
+//  2. q8_attend_kernel or, for blocks of 128 rows, q8_rows_kernel (quant_rows.h): a partial row (maximum, sum, latent
+//     sum) for each row of each piece (the tiles of one block in one run);
+//  3. q8_merge_kernel: joins the partial rows of a query row and applies W_UV.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 
 #include "absorb.h"
+#include "absorb_tile.h"
 #include "device_common.h"
 #include "eg_mla.h"
 #include "host_plan.h"
@@ -78,15 +79,14 @@ __device__ __forceinline__ int first_above(const int* a, int n, int x) {
 template <int THREADS>
 __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   __shared__ int first_s[kPageMaxBatch + 1];  // a sequence's first block
-  __shared__ int cu_s[kPageMaxBatch + 1];     // and first new token
   __shared__ int tmp[THREADS / 64];
   const int tid = threadIdx.x;
-  for (int b = tid; b <= a.B; b += THREADS) cu_s[b] = a.cu ? clamp_len(a.cu[b], a.T) : min(b, a.T);
+  auto first_token = [&](int b) { return a.cu ? clamp_len(a.cu[b], a.T) : min(b, a.T); };
+  for (int t = tid; t < a.T; t += THREADS) a.tokens[t] = make_int2(-1, 0);
   int total = 0, blocks = 0;
-  __syncthreads();
   for (int b0 = 0; b0 < a.B; b0 += THREADS) {
     const int b = b0 + tid;
-    const int64_t r = b < a.B ? static_cast<int64_t>(max(0, cu_s[b + 1] - cu_s[b])) * a.H : 0;
+    const int64_t r = b < a.B ? static_cast<int64_t>(max(0, first_token(b + 1) - first_token(b))) * a.H : 0;
     const int at = group_scan<THREADS>(static_cast<int>((r + a.block_rows - 1) / a.block_rows), tmp, total);
     if (b < a.B) first_s[b] = blocks + at;
     blocks += total;
@@ -99,21 +99,24 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   int tiles = 0;
   for (int k0 = 0; k0 < blocks; k0 += THREADS) {
     const int k = k0 + tid;
-    int n_tiles = 0, b = 0, row0 = 0, rows = 0, first = 0, len = 0;
+    int n_tiles = 0, b = 0, row0 = 0, rows = 0, first = 0, len = 0, cu = 0;
     if (k < blocks) {
       b = first_above(first_s, a.B, k);
-      const int n = cu_s[b + 1] - cu_s[b];
+      cu = first_token(b);
+      const int n = first_token(b + 1) - cu;
       row0 = (k - first_s[b]) * a.block_rows;
       rows = min(a.block_rows, n * a.H - row0);
       len = clamp_len(a.seq_lens[b], a.cap);
       first = len - n;
       const int most_keys = min(max(first + (row0 + rows - 1) / a.H + 1, 0), len);
       n_tiles = (most_keys + a.tile - 1) / a.tile;
+      // the tokens whose first row is in this block
+      for (int i = (row0 + a.H - 1) / a.H; i * a.H < row0 + rows; ++i) a.tokens[cu + i] = make_int2(first_s[b], i);
     }
     const int at = group_scan<THREADS>(n_tiles, tmp, total);
     if (k < blocks) {
       a.info[k] = make_int4(b, row0, rows, tiles + at);
-      a.rows[k] = make_int4(cu_s[b] * a.H + row0, first, len, 0);
+      a.rows[k] = make_int4(cu * a.H + row0, first, len, 0);
     }
     tiles += total;
   }
@@ -130,13 +133,27 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
     const int s = a.info[k].w, e = a.info[k + 1].w;
     for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < e; ++g) a.start[g] = k;
   }
-  for (int t = tid; t < a.T; t += THREADS) {
-    const int b = first_above(cu_s, a.B, t);
-    a.tokens[t] = b < a.B && t >= cu_s[b] ? make_int2(first_s[b], t - cu_s[b]) : make_int2(-1, 0);
-  }
 }
 
 __global__ __launch_bounds__(1024) void q8_schedule_kernel(Q8Sched a) { q8_schedule<1024>(a); }
+
+// Schedule (work-group 0) and absorption in one launch: 16-bit rows [q_lat fp16 | q^R bf16].
+struct Q8Prep {
+  const uint16_t* q;
+  const uint16_t* w_uk;
+  uint16_t* rows;
+  int32_t T, H, DC, DR, row_blocks;
+};
+template <int DH, int BLOCKS, int COLS>
+__global__ __launch_bounds__(256) void q8_prep_kernel(Q8Prep p, Q8Sched a) {
+  if (blockIdx.x == 0) {
+    q8_schedule<256>(a);
+    return;
+  }
+  const int wg = blockIdx.x - 1, h = wg % p.H, rest = wg / p.H;
+  absorb_tile<DH, BLOCKS, COLS, AbsorbRows::kHalf>(p.q, p.w_uk, nullptr, p.rows, p.T, p.H, p.DC, p.DR, h,
+                                                   rest % p.row_blocks, rest / p.row_blocks);
+}
 
 // ---------------------------------------------------------------------------
 // Attention of blocks of 16 rows.  A wave owns units of U tokens of all
@@ -168,7 +185,7 @@ struct Q8Pages {
 };
 
 struct Q8Attend {
-  const float* q;  // [T, H, DC + DR] fp32: absorbed | RoPE query
+  const uint16_t* q;  // [T, H, DC + DR]: q_lat fp16 | q^R bf16
   const uint8_t* codes;
   const uint8_t* scales;
   Q8Pages cache;
@@ -177,7 +194,7 @@ struct Q8Attend {
   const int32_t* start;
   const int32_t* head;
   float* part_ml;  // [piece][block rows][2]
-  float* part_o;   // [piece][block rows][DC]
+  void* part_o;    // [piece][block rows][DC]: fp32 sums O, or (blocks of 128 rows) O / l in fp16
   int32_t H, DC, DR;
   float scale_log2;
 };
@@ -218,6 +235,11 @@ __device__ __forceinline__ void q8_to_f16(u32x4_t w, float s, u32x4_t& lo, u32x4
   }
 }
 
+// Eight values of a query row's part of n, zero behind its end.
+__device__ __forceinline__ u32x4_t q8_query(const uint16_t* part, int d, int n) {
+  return d < n ? *reinterpret_cast<const u32x4_t*>(part + d) : u32x4_t{0u, 0u, 0u, 0u};
+}
+
 template <int DCP>
 __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_attend_kernel(Q8Attend a) {
   using C = Q8Cfg<DCP>;
@@ -249,31 +271,13 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
     // this lane's query row (rows past the last repeat it and are not stored) and the tokens that it attends to
     const int r = min(r16, nrows - 1);
     const int lim = min(first + (row0 + r) / a.H + 1, len);
-    const float* qrow = a.q + (static_cast<int64_t>(rw.x) + r) * (a.DC + a.DR);
+    const uint16_t* qrow = a.q + (static_cast<int64_t>(rw.x) + r) * (a.DC + a.DR);
     f16x8_t qv[NC];
     bf16x8_t qr[NR];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int d = 32 * c + 8 * g;
-      f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
-      if (d < a.DC) {
-        x = *reinterpret_cast<const f32x4_t*>(qrow + d);
-        y = *reinterpret_cast<const f32x4_t*>(qrow + d + 4);
-      }
-      qv[c] = __builtin_bit_cast(f16x8_t, u32x4_t{pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]), pack_f16x2(y[0], y[1]),
-                                                  pack_f16x2(y[2], y[3])});
-    }
+    for (int c = 0; c < NC; ++c) qv[c] = __builtin_bit_cast(f16x8_t, q8_query(qrow, 32 * c + 8 * g, a.DC));
 #pragma unroll
-    for (int c = 0; c < NR; ++c) {
-      const int d = 32 * c + 8 * g;
-      f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
-      if (d < a.DR) {
-        x = *reinterpret_cast<const f32x4_t*>(qrow + a.DC + d);
-        y = *reinterpret_cast<const f32x4_t*>(qrow + a.DC + d + 4);
-      }
-      qr[c] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                   pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])});
-    }
+    for (int c = 0; c < NR; ++c) qr[c] = __builtin_bit_cast(bf16x8_t, q8_query(qrow + a.DC, 32 * c + 8 * g, a.DR));
 
     f32x4_t o[NB];
 #pragma unroll
@@ -420,7 +424,7 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
 #pragma unroll
         for (int v = 1; v < NW; ++v) sum += obuf[(v * (NB / 2) + db) * 64 + lane];
         const int d = (half * (NB / 2) + db) * 16 + 4 * g;
-        if (r16 < nrows && d < a.DC) __builtin_nontemporal_store(sum, reinterpret_cast<f32x4_t*>(a.part_o + prow * a.DC + d));
+        if (r16 < nrows && d < a.DC) __builtin_nontemporal_store(sum, reinterpret_cast<f32x4_t*>(static_cast<float*>(a.part_o) + prow * a.DC + d));
       }
     }
     if (w == 0 && g == 0 && r16 < nrows) {
@@ -438,20 +442,19 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
 namespace egmla {
 
 // ---------------------------------------------------------------------------
-// Merge and up-projection: grid (H, ceil(T / spt)), 8 waves, one head and spt =
-// 1, 2, 4, 8 or 16 new tokens per work-group.  LPR lanes hold a row, 8 dims each;
-// each group of LPR lanes is a worker, and a token's workers take its partial
-// rows in turn, 4 loaded together, folded online in fp32.  They meet in LDS, and
-// the merged row o / l goes there once more as bf16 hi + lo, the B operands of
-// out^T[v][token] = W_UV[h] o^T on v_mfma_f32_16x16x32_bf16, so that the
-// up-projection adds only W_UV's own rounding.
+// Merge and up-projection: grid (H, ceil(T / spt)), one head and spt = 1, 2, 4, ..
+// new tokens per work-group (up to 16, or 32 of wide rows).  LPR lanes hold a row, 8 dims each; each group
+// of LPR lanes is a worker.  With at least as many tokens as workers a worker takes
+// its tokens (up to TPW) side by side, else a token's workers take its partial rows
+// in turn and meet in LDS.  Rows are folded online in fp32, two loaded together; the
+// merged row o / l goes to LDS as bf16 hi + lo, the B operands of out^T[v][token] =
+// W_UV[h] o^T on v_mfma_f32_16x16x32_bf16, so that the up-projection adds only
+// W_UV's own rounding.  Bound by its chain of loads (token, block, rows), behind
+// which W_UV's rows arrive.
 // ---------------------------------------------------------------------------
-constexpr int kQ8MergeWaves = 8;
-constexpr int kQ8MergeTokens = 16;
-
 struct Q8Merge {
   const float* part_ml;
-  const float* part_o;
+  const void* part_o;
   const int4* info;
   const int2* tokens;
   const int32_t* head;
@@ -461,113 +464,216 @@ struct Q8Merge {
 };
 
 template <int LPR>
-__global__ __launch_bounds__(kQ8MergeWaves * 64) void q8_merge_kernel(Q8Merge a) {
-  constexpr int DCP = 8 * LPR, OS = DCP + 8, GPW = 64 / LPR, WORKERS = kQ8MergeWaves * GPW;
-  __shared__ __attribute__((aligned(16))) uint16_t o_s[2][kQ8MergeTokens][OS];  // merged rows, hi and lo
-  __shared__ __attribute__((aligned(16))) float part[WORKERS][DCP];
-  __shared__ float m_part[WORKERS], l_part[WORKERS];
+struct Q8MergeCfg {
+  static constexpr int WAVES = LPR == 64 ? 8 : 4, WORKERS = WAVES * 64 / LPR;
+  static constexpr int TOKENS = LPR == 64 ? 32 : 16;  // of a work-group, at most
+  static constexpr int TPW = TOKENS / WORKERS;        // of a worker
+  static_assert(TOKENS % WORKERS == 0, "whole rounds");
+};
+
+template <int LPR, bool HALF>
+__global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) void q8_merge_kernel(Q8Merge a) {
+  using C = Q8MergeCfg<LPR>;
+  constexpr int DCP = 8 * LPR, NKC = DCP / 32, OS = DCP + 8, GPW = 64 / LPR, TPW = C::TPW, U = 2;
+  __shared__ __attribute__((aligned(16))) uint16_t o_s[2][C::TOKENS][OS];  // merged rows, hi and lo
+  __shared__ __attribute__((aligned(16))) float part[C::WORKERS][DCP];
+  __shared__ float m_part[C::WORKERS], l_part[C::WORKERS];
   const int h = blockIdx.x, t0 = blockIdx.y * a.spt;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
-  const int per = a.head[0];
-  const int wps = max(1, WORKERS / a.spt), spr = WORKERS / wps;  // workers a token, tokens a round
-  const int worker = w * GPW + lane / LPR, col = 8 * (lane % LPR);
-  for (int r0 = 0; r0 < a.spt; r0 += spr) {
-    const int t = t0 + r0 + worker / wps, me = worker % wps;
+  const int per = a.head[0], blocks = a.head[1];
+  const int wps = max(1, C::WORKERS / a.spt);  // workers a token
+  const int worker = w * GPW + lane / LPR, me = worker % wps, col = 8 * (lane % LPR);
+  // this worker's tokens worker / wps + j WORKERS: how many partial rows they have, and the first
+  int n[TPW];
+  int64_t row0[TPW];
+  {
+    int2 tk[TPW];
+    int k[TPW], s[TPW], e[TPW];
+#pragma unroll
+    for (int j = 0; j < TPW; ++j) {
+      const int i = worker / wps + j * C::WORKERS;
+      tk[j] = i < a.spt && t0 + i < a.T ? a.tokens[t0 + i] : make_int2(-1, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < TPW; ++j) {
+      row0[j] = static_cast<int64_t>(tk[j].y) * a.H + h;
+      k[j] = tk[j].x + static_cast<int>(row0[j] / a.block_rows);
+      const bool there = tk[j].x >= 0 && k[j] < blocks;
+      s[j] = there ? a.info[k[j]].w : 0;
+      e[j] = there ? a.info[k[j] + 1].w : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < TPW; ++j) {
+      const int first = s[j] / per;
+      n[j] = e[j] > s[j] ? (e[j] - 1) / per - first + 1 : 0;
+      row0[j] = (static_cast<int64_t>(first) + k[j]) * a.block_rows + row0[j] % a.block_rows;
+    }
+  }
+  // rows i, i + wps of a token (repeats of the last past its end)
+  struct Rows {
+    float2 ml[U];
+    u32x4_t x[U][HALF ? 1 : 2];
+  };
+  auto load = [&](Rows& r, int64_t first, int i, int n) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = first + static_cast<int64_t>(min(i + u * wps, n - 1)) * a.block_rows;
+      r.ml[u] = *reinterpret_cast<const float2*>(a.part_ml + 2 * row);
+#pragma unroll
+      for (int q = 0; q < (HALF ? 1 : 2); ++q) {
+        r.x[u][q] = u32x4_t{0u, 0u, 0u, 0u};
+        if (col < a.DC)
+          r.x[u][q] = *reinterpret_cast<const u32x4_t*>(static_cast<const unsigned char*>(a.part_o) +
+                                                        (row * a.DC + col) * (HALF ? 2 : 4) + 16 * q);
+      }
+    }
+  };
+  Rows rows[TPW];
+#pragma unroll
+  for (int j = 0; j < TPW; ++j)
+    if (me < n[j]) load(rows[j], row0[j], me, n[j]);
+  // W_UV rows v0 + r16 (columns 32 kc + 8 g ..; zero past d_c, as the merged rows are)
+  u32x4_t wa[NKC];
+  auto load_w = [&](int v0) {
+    const uint16_t* wrow = a.w_uv + (static_cast<int64_t>(h) * a.DV + min(v0 + r16, a.DV - 1)) * a.DC + 8 * g;
+#pragma unroll
+    for (int kc = 0; kc < NKC; ++kc)
+      wa[kc] = 32 * kc + 8 * g < a.DC ? *reinterpret_cast<const u32x4_t*>(wrow + 32 * kc) : u32x4_t{0u, 0u, 0u, 0u};
+  };
+  load_w(16 * w);
+
+  auto put = [&](int i, int c, const float (&v)[8]) {  // merged values c .. of token i
+    bf16x8_t hi, lo;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      hi[q] = static_cast<__bf16>(v[q]);
+      lo[q] = static_cast<__bf16>(v[q] - static_cast<float>(hi[q]));
+    }
+    *reinterpret_cast<bf16x8_t*>(&o_s[0][i][c]) = hi;
+    *reinterpret_cast<bf16x8_t*>(&o_s[1][i][c]) = lo;
+  };
+#pragma unroll
+  for (int j = 0; j < TPW; ++j) {
     float M = -INFINITY, sum = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (t < a.T && r0 + worker / wps < a.spt) {
-      const int2 tk = a.tokens[t];
-      if (tk.x >= 0) {
-        const int64_t rho = static_cast<int64_t>(tk.y) * a.H + h;
-        const int k = tk.x + static_cast<int>(rho / a.block_rows);
-        const bool there = k < a.head[1];
-        const int s = there ? a.info[k].w : 0, e = there ? a.info[k + 1].w : 0;
-        const int first = s / per, n = e > s ? (e - 1) / per - first + 1 : 0;
-        const int64_t row0 = (static_cast<int64_t>(first) + k) * a.block_rows + rho % a.block_rows;
-        for (int i0 = me; i0 < n; i0 += 4 * wps) {
-          float2 ml[4];
-          f32x4_t v[4][2];
+    for (int i = me; i < n[j]; i += U * wps) {
+      const Rows r = rows[j];
+      if (i + U * wps < n[j]) load(rows[j], row0[j], i + U * wps, n[j]);
+      float top = M;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int64_t row = row0 + static_cast<int64_t>(min(i0 + u * wps, n - 1)) * a.block_rows;
-            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + 2 * row);
-            v[u][0] = v[u][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            if (col < a.DC) {
-              const f32x4_t* p = reinterpret_cast<const f32x4_t*>(a.part_o + row * a.DC + col);
-              v[u][0] = p[0];
-              v[u][1] = p[1];
-            }
-          }
-          float top = M;
+      for (int u = 0; u < U; ++u) top = fmaxf(top, r.ml[u].x);  // repeats change no maximum
+      // (where no row has a maximum they are added all the same: a NaN in one stays one)
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float keep = M == -INFINITY && top > -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M == -INFINITY ? 0.f : M) - ref);
+      sum *= keep;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) top = fmaxf(top, ml[u].x);  // repeats change no maximum
-          // (where no row has a maximum they are added all the same: a NaN in one stays one)
-          const float ref = top == -INFINITY ? 0.f : top;
-          const float keep = M == -INFINITY && top > -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M == -INFINITY ? 0.f : M) - ref);
-          sum *= keep;
+      for (int q = 0; q < 8; ++q) acc[q] *= keep;
 #pragma unroll
-          for (int e8 = 0; e8 < 8; ++e8) acc[e8] *= keep;
+      for (int u = 0; u < U; ++u) {
+        if (i + u * wps >= n[j]) continue;
+        const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r.ml[u].x - ref);
+        sum = fmaf(x, r.ml[u].y, sum);
+        if constexpr (HALF) {
+          const f16x8_t v = __builtin_bit_cast(f16x8_t, r.x[u][0]);
+          const float y = x * r.ml[u].y;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (i0 + u * wps >= n) continue;
-            const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - ref);
-            sum = fmaf(x, ml[u].y, sum);
+          for (int q = 0; q < 8; ++q) acc[q] = fmaf(y, static_cast<float>(v[q]), acc[q]);
+        } else {
 #pragma unroll
-            for (int e8 = 0; e8 < 8; ++e8) acc[e8] = fmaf(x, v[u][e8 / 4][e8 % 4], acc[e8]);
-          }
-          M = top;
+          for (int q = 0; q < 8; ++q) acc[q] = fmaf(x, __uint_as_float(r.x[u][q / 4][q % 4]), acc[q]);
         }
       }
+      M = top;
     }
-    if (r0 > 0) __syncthreads();  // the round before has been read
-    *reinterpret_cast<f32x4_t*>(&part[worker][col]) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
-    *reinterpret_cast<f32x4_t*>(&part[worker][col + 4]) = f32x4_t{acc[4], acc[5], acc[6], acc[7]};
-    if (lane % LPR == 0) {
-      m_part[worker] = M;
-      l_part[worker] = sum;
-    }
-    __syncthreads();
-    // merged rows of the round's tokens (zero without keys)
-    for (int i = tid; i < spr * DCP; i += kQ8MergeWaves * 64) {
-      const int kk = i / DCP, c = i - kk * DCP;
-      if (r0 + kk >= a.spt) continue;
-      float top = -INFINITY, num = 0.f, den = 0.f;
-      for (int p = 0; p < wps; ++p) top = fmaxf(top, m_part[kk * wps + p]);
-      for (int p = 0; p < wps; ++p) {
-        const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top);
-        num = fmaf(x, part[kk * wps + p][c], num);
-        den = fmaf(x, l_part[kk * wps + p], den);
+    if (wps == 1) {
+      const int i = worker + j * C::WORKERS;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc[q] = sum == 0.f ? 0.f : acc[q] / sum;  // (zero without keys)
+      if (i < C::TOKENS) put(i, col, acc);
+    } else {  // (one token a worker: j is 0)
+      *reinterpret_cast<f32x4_t*>(&part[worker][col]) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
+      *reinterpret_cast<f32x4_t*>(&part[worker][col + 4]) = f32x4_t{acc[4], acc[5], acc[6], acc[7]};
+      if (lane % LPR == 0) {
+        m_part[worker] = M;
+        l_part[worker] = sum;
       }
-      const float v = den == 0.f ? 0.f : num / den;
-      const __bf16 hi = static_cast<__bf16>(v);
-      o_s[0][r0 + kk][c] = __builtin_bit_cast(uint16_t, hi);
-      o_s[1][r0 + kk][c] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - static_cast<float>(hi)));
+      break;
     }
   }
   __syncthreads();
-  const int rr = min(r16, a.spt - 1);  // columns past spt repeat the last and are not stored
-  const int t = t0 + r16;
-  const bool live = r16 < a.spt && t < a.T && a.tokens[min(t, a.T - 1)].x >= 0;  // other rows stay as they are
-  for (int v0 = 16 * w; v0 < a.DV; v0 += 16 * kQ8MergeWaves) {
-    const uint16_t* wrow = a.w_uv + (static_cast<int64_t>(h) * a.DV + min(v0 + r16, a.DV - 1)) * a.DC + 8 * g;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int kc = 0; 32 * kc < a.DC; ++kc) {
-      // (d_c may end half way through a chunk: the merged rows are zero there)
-      const u32x4_t x = 32 * kc + 8 * g < a.DC ? *reinterpret_cast<const u32x4_t*>(wrow + 32 * kc) : u32x4_t{0u, 0u, 0u, 0u};
-      const bf16x8_t av = __builtin_bit_cast(bf16x8_t, x);
-      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[0][rr][32 * kc + 8 * g]), o, 0, 0, 0);
-      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[1][rr][32 * kc + 8 * g]), o, 0, 0, 0);
-    }
-    if (!live) continue;
-    uint16_t* orow = a.out + (static_cast<int64_t>(t) * a.H + h) * a.DV + v0 + 4 * g;
+  if (wps > 1) {
+    for (int i = tid; i < a.spt * LPR; i += C::WAVES * 64) {
+      const int kk = i / LPR, c = 8 * (i % LPR);
+      float top = -INFINITY, den = 0.f, num[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p < wps; ++p) top = fmaxf(top, m_part[kk * wps + p]);
+      for (int p = 0; p < wps; ++p) {
+        const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_part[kk * wps + p] - top);
+        den = fmaf(x, l_part[kk * wps + p], den);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (v0 + 4 * g + i < a.DV) orow[i] = f32_to_bf16(o[i]);
+        for (int q = 0; q < 8; ++q) num[q] = fmaf(x, part[kk * wps + p][c + q], num[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) num[q] = den == 0.f ? 0.f : num[q] / den;
+      put(kk, c, num);
+    }
+    __syncthreads();
+  }
+  for (int v0 = 16 * w; v0 < a.DV; v0 += 16 * C::WAVES) {
+    if (v0 != 16 * w) load_w(v0);
+#pragma unroll
+    for (int i0 = 0; i0 < C::TOKENS; i0 += 16) {
+      if (i0 >= a.spt) continue;
+      const int i = i0 + r16, rr = min(i, a.spt - 1);  // columns past spt repeat the last and are not stored
+      f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kc = 0; kc < NKC; ++kc) {
+        const bf16x8_t av = __builtin_bit_cast(bf16x8_t, wa[kc]);
+        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[0][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[1][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+      }
+      const int t = t0 + i;
+      if (i >= a.spt || t >= a.T || a.tokens[t].x < 0) continue;  // other rows stay as they are
+      uint16_t* orow = a.out + (static_cast<int64_t>(t) * a.H + h) * a.DV + v0 + 4 * g;
+      if (a.DV % 4 == 0) {
+        if (v0 + 4 * g < a.DV) *reinterpret_cast<u32x2_t*>(orow) = u32x2_t{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v0 + 4 * g + e < a.DV) orow[e] = f32_to_bf16(o[e]);
+    }
   }
 }
 
 }  // namespace egmla
 
 using namespace egmla;
+
+namespace {
+
+hipError_t launch_q8_prep(const eg_mla_dims& d, int32_t n, const void* q, const void* w_uk, uint16_t* rows,
+                          const Q8Sched& sched, hipStream_t stream) {
+  if (d.head_dim != 64 && d.head_dim != 128) {
+    hipLaunchKernelGGL(q8_schedule_kernel, dim3(1), dim3(1024), 0, stream, sched);
+    return launch_absorb_half(d, n, q, w_uk, rows, stream);
+  }
+  // 64 queries a work-group where those of 16 would be many; narrow column slices where few
+  const int64_t tiles = static_cast<int64_t>(d.num_heads) * ((n + kAbsRows - 1) / kAbsRows);
+  const bool grouped = tiles >= 512, narrow = tiles < kAbsMinWorkGroups;
+  const int cols = narrow ? kAbsColsNarrow : kAbsCols, block = kAbsRows * (grouped ? kAbsBlocks : 1);
+  const Q8Prep p{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(w_uk), rows, n, d.num_heads, d.latent_dim,
+                 d.rope_dim, (n + block - 1) / block};
+  const int64_t wgs = int64_t{d.num_heads} * p.row_blocks * ((d.latent_dim + cols - 1) / cols) + 1;
+  auto kern = d.head_dim == 64 ? (grouped  ? q8_prep_kernel<64, kAbsBlocks, kAbsCols>
+                                  : narrow ? q8_prep_kernel<64, 1, kAbsColsNarrow>
+                                           : q8_prep_kernel<64, 1, kAbsCols>)
+              : grouped ? q8_prep_kernel<128, kAbsBlocks, kAbsCols>
+              : narrow  ? q8_prep_kernel<128, 1, kAbsColsNarrow>
+                        : q8_prep_kernel<128, 1, kAbsCols>;
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, stream, p, sched);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 extern "C" size_t eg_mla_quant_attend_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t n_queries,
                                                   int32_t max_pages_per_seq) {
@@ -588,19 +694,18 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   const eg_mla_dims& d = *dims;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
-  float* qfull = reinterpret_cast<float*>(ws + p.off_q);
+  uint16_t* qrows = reinterpret_cast<uint16_t*>(ws + p.off_q);
   const Q8Sched sched{cu_seqlens, seq_lens, reinterpret_cast<int4*>(ws + p.off_info), reinterpret_cast<int4*>(ws + p.off_rows),
                       reinterpret_cast<int32_t*>(ws + p.off_start), reinterpret_cast<int2*>(ws + p.off_tokens),
                       reinterpret_cast<int32_t*>(ws + p.off_head), batch, n_queries, d.num_heads, p.capacity, p.block_rows,
                       p.tile, p.runs};
   (void)hipGetLastError();
-  if (launch_absorb(d, n_queries, q, w_uk, qfull, stream) != hipSuccess) return EG_MLA_ERR_HIP;
-  hipLaunchKernelGGL(q8_schedule_kernel, dim3(1), dim3(1024), 0, stream, sched);
+  if (launch_q8_prep(d, n_queries, q, w_uk, qrows, sched, stream) != hipSuccess) return EG_MLA_ERR_HIP;
   Q8Pages pages{page_table ? page_table : sched.head, page_table != nullptr, d.page_size, static_cast<int32_t>(num_slots / d.page_size), max_pages_per_seq, p.capacity, 0, 31};
   while ((int64_t{1} << (pages.shift - 31)) < d.page_size) ++pages.shift;  // l = ceil(log2 P): mul = ceil(2^(31+l) / P) < 2^32
   pages.mul = static_cast<uint32_t>(((uint64_t{1} << pages.shift) + d.page_size - 1) / d.page_size);
-  const Q8Attend at{qfull, codes, scales, pages, sched.info, sched.rows, sched.start, sched.head,
-                    reinterpret_cast<float*>(ws + p.off_ml), reinterpret_cast<float*>(ws + p.off_o),
+  const Q8Attend at{qrows, codes, scales, pages, sched.info, sched.rows, sched.start, sched.head,
+                    reinterpret_cast<float*>(ws + p.off_ml), ws + p.off_o,
                     d.num_heads, d.latent_dim, d.rope_dim, softmax_scale(d) * 1.4426950408889634f};
   const dim3 grid(p.runs), block(kQ8AttendThreads);
   if (p.block_rows == kQ8Rows) {
@@ -612,13 +717,16 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   else if (d.latent_dim <= 128) hipLaunchKernelGGL((q8_attend_kernel<128>), grid, block, 0, stream, at);
   else if (d.latent_dim <= 320) hipLaunchKernelGGL((q8_attend_kernel<320>), grid, block, 0, stream, at);
   else hipLaunchKernelGGL((q8_attend_kernel<512>), grid, block, 0, stream, at);
-  // tokens of a merge work-group: as many as leave two work-groups a compute unit
-  int spt = kQ8MergeTokens;
-  while (spt > 1 && static_cast<int64_t>(d.num_heads) * ((n_queries + spt - 1) / spt) < 512) spt /= 2;
+  // tokens of a merge work-group: as many as leave two work-groups a compute unit (of wide rows one: 8 waves)
+  const bool wide = d.latent_dim > 128;
+  int spt = wide ? Q8MergeCfg<64>::TOKENS : Q8MergeCfg<16>::TOKENS;
+  while (spt > 1 && static_cast<int64_t>(d.num_heads) * ((n_queries + spt - 1) / spt) < (wide ? 256 : 512)) spt /= 2;
   const Q8Merge mg{at.part_ml, at.part_o, sched.info, sched.tokens, sched.head, static_cast<const uint16_t*>(w_uv),
                    static_cast<uint16_t*>(out), n_queries, d.num_heads, d.latent_dim, d.v_head_dim, p.block_rows, spt};
-  const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt), mblock(kQ8MergeWaves * 64);
-  if (d.latent_dim <= 128) hipLaunchKernelGGL((q8_merge_kernel<16>), mgrid, mblock, 0, stream, mg);
-  else hipLaunchKernelGGL((q8_merge_kernel<64>), mgrid, mblock, 0, stream, mg);
+  const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt), mblock(64 * (wide ? Q8MergeCfg<64>::WAVES : Q8MergeCfg<16>::WAVES));
+  const bool half = p.block_rows == kQ8Rows;
+  auto merge = wide ? (half ? q8_merge_kernel<64, true> : q8_merge_kernel<64, false>)
+                    : (half ? q8_merge_kernel<16, true> : q8_merge_kernel<16, false>);
+  hipLaunchKernelGGL(merge, mgrid, mblock, 0, stream, mg);
   return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
 }

@@ -28,7 +28,7 @@ struct Q8RowsCfg {
   static constexpr int PL = DC / 16;                     // pieces (16 codes) of a key
   static constexpr int NLI = (KW * PL + 63) / 64, NRI = KW * 8 / 64;
   static constexpr int NC = DC / 16, NR = 4, KB = KEYS / 32, NDB = DC / 32;
-  static constexpr int QL = DC == 512 ? 10 : 0;           // query chunks that wait in LDS beside q^R
+  static constexpr int QL = DC == 512 ? 4 : 0;           // query chunks that wait in LDS beside q^R
   static constexpr int Q_LDS = QL ? (NR + QL) * kQ8RowsThreads * 16 : 16;
   static_assert(2 * TILE + Q_LDS + 4 * KEYS * 8 <= 160 * 1024 && (KEYS & (KEYS - 1)) == 0, "LDS");
 };
@@ -73,31 +73,13 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
     // this lane's query row (rows past the last repeat it and are not stored) and the tokens that it attends to
     const int r = min(32 * w + r32, nrows - 1);
     const int lim = min(first + (row0 + r) / a.H + 1, len);
-    const float* qrow = a.q + (static_cast<int64_t>(rw.x) + r) * (a.DC + a.DR);
+    const uint16_t* qrow = a.q + (static_cast<int64_t>(rw.x) + r) * (a.DC + a.DR);
     f16x8_t qv[NC];
     bf16x8_t qr[NR];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int d = 16 * c + 8 * h;
-      f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
-      if (d < a.DC) {
-        x = *reinterpret_cast<const f32x4_t*>(qrow + d);
-        y = *reinterpret_cast<const f32x4_t*>(qrow + d + 4);
-      }
-      qv[c] = __builtin_bit_cast(f16x8_t, u32x4_t{pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]), pack_f16x2(y[0], y[1]),
-                                                  pack_f16x2(y[2], y[3])});
-    }
+    for (int c = 0; c < NC; ++c) qv[c] = __builtin_bit_cast(f16x8_t, q8_query(qrow, 16 * c + 8 * h, a.DC));
 #pragma unroll
-    for (int c = 0; c < NR; ++c) {
-      const int d = 16 * c + 8 * h;
-      f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
-      if (d < a.DR) {
-        x = *reinterpret_cast<const f32x4_t*>(qrow + a.DC + d);
-        y = *reinterpret_cast<const f32x4_t*>(qrow + a.DC + d + 4);
-      }
-      qr[c] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                   pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])});
-    }
+    for (int c = 0; c < NR; ++c) qr[c] = __builtin_bit_cast(bf16x8_t, q8_query(qrow + a.DC, 16 * c + 8 * h, a.DR));
     if constexpr (QL > 0) {
 #pragma unroll
       for (int c = 0; c < NR; ++c) q_s[c * kQ8RowsThreads + tid] = __builtin_bit_cast(u32x4_t, qr[c]);
@@ -347,21 +329,22 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
 
     // lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row that met no token (or whose scores
     // all overflowed to -inf) weighs nothing; a NaN among them stays one
-    const float l = half_sum(l_run);
-    int lane_e = tid & 63;  // (the row is formed anew: nothing of it is kept over the loops)
-    asm volatile("" : "+v"(lane_e));
-    const int he = lane_e >> 5, re = 32 * w + (lane_e & 31);
+    const float l = half_sum(l_run), inv = l == 0.f ? 0.f : 1.0f / l;
+    const int ln = lane_anew(n), he = ln >> 5, re = 32 * w + (ln & 31);
     if (re < nrows) {
       const int64_t prow = (static_cast<int64_t>(run) + k) * kQ8Rows + re;
       if (he == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(l == 0.f ? -INFINITY : m_run, l);
-      float* orow = a.part_o + prow * a.DC + 8 * he;
+      uint16_t* orow = static_cast<uint16_t*>(a.part_o) + prow * a.DC + 8 * he;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (32 * db + 16 * (j >> 1) < a.DC)
-            *reinterpret_cast<f32x4_t*>(orow + 32 * db + 16 * (j >> 1) + 4 * (j & 1)) =
-                f32x4_t{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+        for (int j = 0; j < 2; ++j)
+          if (32 * db + 16 * j < a.DC)
+            *reinterpret_cast<u32x4_t*>(orow + 32 * db + 16 * j) =
+                u32x4_t{pack_f16x2(o[db][8 * j] * inv, o[db][8 * j + 1] * inv),
+                        pack_f16x2(o[db][8 * j + 2] * inv, o[db][8 * j + 3] * inv),
+                        pack_f16x2(o[db][8 * j + 4] * inv, o[db][8 * j + 5] * inv),
+                        pack_f16x2(o[db][8 * j + 6] * inv, o[db][8 * j + 7] * inv)};
     }
   }
 #endif
