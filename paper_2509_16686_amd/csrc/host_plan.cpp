@@ -992,8 +992,9 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   p.block_rows = many ? 128 : 16;
   p.tile = many ? (d.latent_dim <= 128 ? 64 : 32) : d.latent_dim <= 128 ? 128 : 64;
   p.runs = many && d.latent_dim > 128 ? 256 : 512;
+  p.lead = many ? 4 : 0;
   p.blocks = rows / p.block_rows + batch;
-  if (held_product(rows / 16 + batch, cap / 32 + 1) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
+  if (held_product(rows / 16 + batch, cap / 32 + 5) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;
@@ -1005,7 +1006,7 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   const int64_t part = rows + 128 * (kQ8MaxRuns + static_cast<int64_t>(batch));
   p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 2);
   const int64_t most = rows / 16 + batch;
-  p.off_info = take((most + 1) * 16);
+  p.off_info = take(most * 16);
   p.off_rows = take(most * 16);
   p.off_start = take(kQ8MaxRuns * int64_t{4});
   p.off_tokens = take(n_queries * int64_t{8});

@@ -247,9 +247,10 @@ struct Q8Plan {
   int block_rows = 0;  // query rows of a block
   int tile = 0;        // tokens of a tile
   int runs = 0;
+  int lead = 0;        // tiles that a block's start costs, in the sharing out of the runs
   int64_t blocks = 0;  // at most
   size_t off_q = 0;       // 16-bit [T, H, d_c + d_r]  q_lat fp16 | q^R bf16
-  size_t off_info = 0;    // int4 [blocks + 1]
+  size_t off_info = 0;    // int4 [blocks]
   size_t off_rows = 0;    // int4 [blocks]
   size_t off_start = 0;   // int32 [runs]
   size_t off_tokens = 0;  // int2 [T]

@@ -34,12 +34,14 @@ namespace egmla {
 struct Q8Sched {
   const int32_t* cu;        // [B + 1], or null: one new token a sequence
   const int32_t* seq_lens;  // [B]
-  int4* info;               // [blocks + 1]: sequence, first row in it, rows, tiles before it
-  int4* rows;               // [blocks]: first query row, first new token's position (may be negative), length, -
-  int32_t* start;           // [runs]: block that a run starts in
+  // Places: the tiles of all blocks in order, `lead` places left free before each block's (a piece costs about as much
+  // as that many tiles before its first and after its last).
+  int4* info;               // [blocks]: sequence, first row in it, rows, place of the first tile
+  int4* rows;               // [blocks]: first query row, first new token's position (may be negative), length, place behind the last tile
+  int32_t* start;           // [runs]: the first block with tiles from a run's first place on
   int2* tokens;             // [T]: the sequence's first block and the token's number in it; -1: no sequence's
-  int32_t* head;            // tiles of a run, blocks, tiles
-  int32_t B, T, H, cap, block_rows, tile, runs;
+  int32_t* head;            // places of a run, blocks, places
+  int32_t B, T, H, cap, block_rows, tile, runs, lead;
 };
 
 // Exclusive sum over the work-group's threads, and the total.
@@ -113,16 +115,16 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
       // the tokens whose first row is in this block
       for (int i = (row0 + a.H - 1) / a.H; i * a.H < row0 + rows; ++i) a.tokens[cu + i] = make_int2(first_s[b], i);
     }
-    const int at = group_scan<THREADS>(n_tiles, tmp, total);
+    const int lead = n_tiles ? a.lead : 0;
+    const int at = group_scan<THREADS>(n_tiles + lead, tmp, total);
     if (k < blocks) {
-      a.info[k] = make_int4(b, row0, rows, tiles + at);
-      a.rows[k] = make_int4(cu * a.H + row0, first, len, 0);
+      a.info[k] = make_int4(b, row0, rows, tiles + at + lead);
+      a.rows[k] = make_int4(cu * a.H + row0, first, len, tiles + at + lead + n_tiles);
     }
     tiles += total;
   }
   const int per = max(1, (tiles + a.runs - 1) / a.runs);
   if (tid == 0) {
-    a.info[blocks] = make_int4(0, 0, 0, tiles);
     a.head[0] = per;
     a.head[1] = blocks;
     a.head[2] = tiles;
@@ -130,7 +132,7 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   __threadfence_block();
   __syncthreads();
   for (int k = tid; k < blocks; k += THREADS) {
-    const int s = a.info[k].w, e = a.info[k + 1].w;
+    const int e = a.rows[k].w, s = e == a.info[k].w ? e : a.info[k].w - a.lead;
     for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < e; ++g) a.start[g] = k;
   }
 }
@@ -258,11 +260,12 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
   int at = run * per;
   if (static_cast<int64_t>(run) * per >= tiles) return;
   const int end = min(at + per, tiles);
-  for (int k = uniform(a.start[run]); at < end && k < blocks; ++k) {
-    const int4 info = uniform(a.info[k]);
-    const int next = uniform(a.info[k + 1].w);
+  for (int k = uniform(a.start[run]); k < blocks; ++k) {
+    const int4 info = uniform(a.info[k]), rw = uniform(a.rows[k]);
+    at = max(at, info.w);
+    if (at >= end) break;
+    const int next = rw.w;
     if (next <= at) continue;  // a block without tokens
-    const int4 rw = uniform(a.rows[k]);
     const int b = info.x, row0 = info.y, nrows = info.z, first = rw.y, len = rw.z;
     const int most = min(max(first + (row0 + nrows - 1) / a.H + 1, 0), len);
     const int j0 = (at - info.w) * C::TILE, j1 = min((min(end, next) - info.w) * C::TILE, most);
@@ -456,6 +459,7 @@ struct Q8Merge {
   const float* part_ml;
   const void* part_o;
   const int4* info;
+  const int4* rows;
   const int2* tokens;
   const int32_t* head;
   const uint16_t* w_uv;
@@ -500,7 +504,7 @@ __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) voi
       k[j] = tk[j].x + static_cast<int>(row0[j] / a.block_rows);
       const bool there = tk[j].x >= 0 && k[j] < blocks;
       s[j] = there ? a.info[k[j]].w : 0;
-      e[j] = there ? a.info[k[j] + 1].w : 0;
+      e[j] = there ? a.rows[k[j]].w : 0;
     }
 #pragma unroll
     for (int j = 0; j < TPW; ++j) {
@@ -698,7 +702,7 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   const Q8Sched sched{cu_seqlens, seq_lens, reinterpret_cast<int4*>(ws + p.off_info), reinterpret_cast<int4*>(ws + p.off_rows),
                       reinterpret_cast<int32_t*>(ws + p.off_start), reinterpret_cast<int2*>(ws + p.off_tokens),
                       reinterpret_cast<int32_t*>(ws + p.off_head), batch, n_queries, d.num_heads, p.capacity, p.block_rows,
-                      p.tile, p.runs};
+                      p.tile, p.runs, p.lead};
   (void)hipGetLastError();
   if (launch_q8_prep(d, n_queries, q, w_uk, qrows, sched, stream) != hipSuccess) return EG_MLA_ERR_HIP;
   Q8Pages pages{page_table ? page_table : sched.head, page_table != nullptr, d.page_size, static_cast<int32_t>(num_slots / d.page_size), max_pages_per_seq, p.capacity, 0, 31};
@@ -721,7 +725,7 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   const bool wide = d.latent_dim > 128;
   int spt = wide ? Q8MergeCfg<64>::TOKENS : Q8MergeCfg<16>::TOKENS;
   while (spt > 1 && static_cast<int64_t>(d.num_heads) * ((n_queries + spt - 1) / spt) < (wide ? 256 : 512)) spt /= 2;
-  const Q8Merge mg{at.part_ml, at.part_o, sched.info, sched.tokens, sched.head, static_cast<const uint16_t*>(w_uv),
+  const Q8Merge mg{at.part_ml, at.part_o, sched.info, sched.rows, sched.tokens, sched.head, static_cast<const uint16_t*>(w_uv),
                    static_cast<uint16_t*>(out), n_queries, d.num_heads, d.latent_dim, d.v_head_dim, p.block_rows, spt};
   const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt), mblock(64 * (wide ? Q8MergeCfg<64>::WAVES : Q8MergeCfg<16>::WAVES));
   const bool half = p.block_rows == kQ8Rows;

@@ -36,9 +36,9 @@ struct Q8RowsCfg {
 // The lane's number, formed anew for each i: nothing that follows from it is kept in between (where registers are full it
 // would go to scratch memory, and a reload waits for every load before it, the rows of the next tile among them).
 __device__ __forceinline__ int lane_anew(int i) {
-  int zero = 0;
+  uint32_t zero = 0;
   asm("" : "+s"(zero) : "s"(i));
-  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero)) & 63u;
 }
 
 template <int DC>
@@ -60,11 +60,12 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
   if (static_cast<int64_t>(run) * per >= tiles) return;
   int at = run * per;
   const int end = min(at + per, tiles);
-  for (int k = uniform(a.start[run]); at < end && k < blocks; ++k) {
-    const int4 info = uniform(a.info[k]);
-    const int next = uniform(a.info[k + 1].w);
+  for (int k = uniform(a.start[run]); k < blocks; ++k) {
+    const int4 info = uniform(a.info[k]), rw = uniform(a.rows[k]);
+    at = max(at, info.w);
+    if (at >= end) break;
+    const int next = rw.w;
     if (next <= at) continue;  // a block without tokens
-    const int4 rw = uniform(a.rows[k]);
     const int b = info.x, row0 = info.y, nrows = info.z, first = rw.y, len = rw.z;
     const int most = min(max(first + (row0 + nrows - 1) / a.H + 1, 0), len);
     const int j0 = (at - info.w) * C::KEYS, j1 = min((min(end, next) - info.w) * C::KEYS, most);
@@ -110,11 +111,17 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
       const int r32 = ln & 31, h = ln >> 5, r16 = ln & 15, R1 = (ln >> 4) & 1;
       const int swz_l = ((r32 & 3) << 2) | ((r32 >> 2) & 3), swz_r = (r32 >> 1) & 7;
       const int off_l = r32 * C::LROW, off_r = C::ROPE + r32 * C::RROW;
-      px_f32x16_t s[KB];
+      // d_c 512: the compiler has products write accumulation registers, which the values fill, and would move a block of
+      // them out and back for each tile; the scores' products are written to ordinary ones by hand, and to two
+      // accumulators in turn (a product does not wait for the one before it)
+      constexpr bool HAND = QL > 0;
+      constexpr int NS = HAND ? 2 * KB : KB;
+      px_f32x16_t s[NS];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+      for (int kb = 0; kb < NS; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+      if constexpr (HAND) asm("s_nop 1" : "+v"(s[0]), "+v"(s[1]));  // a vector result feeds no product for 2 wait states
       // chunks of 16 values, the RoPE key's first; operands are read QA chunks ahead of their products
       u32x4_t sa[QA + 1][KB], sq[QA + 1];
       auto read_chunk = [&](int c) __attribute__((always_inline)) {
@@ -132,18 +139,29 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
       for (int c = 0; c < NC + NR; ++c) {
         if (c + QA < NC + NR) read_chunk(c + QA);
         __builtin_amdgcn_sched_barrier(0);
+        const u32x4_t bv = QL > 0 && c < NR + QL ? sq[c % (QA + 1)]
+                           : c < NR              ? __builtin_bit_cast(u32x4_t, qr[c < NR ? c : 0])
+                                                 : __builtin_bit_cast(u32x4_t, qv[c < NR ? 0 : c - NR]);
+        if constexpr (HAND) {
+          if (c < NR) asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s[c % 2]) : "v"(sa[c % (QA + 1)][0]), "v"(bv));
+          else asm("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s[c % 2]) : "v"(sa[c % (QA + 1)][0]), "v"(bv));
+        } else {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const u32x4_t av = sa[c % (QA + 1)][kb];
-          if (c < NR)
-            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8_t, av), QL > 0 ? __builtin_bit_cast(bf16x8_t, sq[c % (QA + 1)]) : qr[c], s[kb], 0, 0, 0);
-          else
-            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                __builtin_bit_cast(f16x8_t, av),
-                c < NR + QL ? __builtin_bit_cast(f16x8_t, sq[c % (QA + 1)]) : qv[c - NR], s[kb], 0, 0, 0);
+          for (int kb = 0; kb < KB; ++kb) {
+            const u32x4_t av = sa[c % (QA + 1)][kb];
+            if (c < NR)
+              s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av),
+                                                              __builtin_bit_cast(bf16x8_t, bv), s[kb], 0, 0, 0);
+            else
+              s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, av),
+                                                             __builtin_bit_cast(f16x8_t, bv), s[kb], 0, 0, 0);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (HAND) {  // a product's result is read by a vector instruction 18 wait states behind it at the earliest
+        asm("s_nop 15\n\ts_nop 7" : "+v"(s[0]), "+v"(s[1]));
+        s[0] += s[1];
       }
       if (__builtin_amdgcn_ballot_w64(valid < C::KEYS)) {  // some row's tokens end inside this tile
 #pragma unroll
