@@ -37,8 +37,9 @@ __device__ __forceinline__ void turn_of(uint64_t freq, int32_t position, float& 
 
 // ---------------------------------------------------------------------------
 // Rotation of rows [n, H, D]: a work-group takes one token and `hpu` of its
-// heads; a thread takes one item of a head's row (VEC pairs, or VEC values to
-// copy) for every hpar-th of them, so that its sines are formed once.
+// heads; a thread takes two pieces of VEC values of a head's row, those of VEC
+// pairs or two to copy, for every hpar-th of them, so that its sines are formed
+// once, and several heads' loads are in flight.
 // ---------------------------------------------------------------------------
 struct RopeArgs {
   const void* x;
@@ -79,48 +80,60 @@ __global__ __launch_bounds__(kQ8Threads) void rope_rows_kernel(RopeArgs a) {
   const int u = static_cast<int>(blockIdx.x - t * a.upt);
   const int h0 = u * a.hpu, h1 = min(h0 + a.hpu, a.H);
   const int32_t position = a.positions[t];
-  const int turns = a.rd / (2 * VEC), front = a.off / VEC;
-  const int items = turns + (a.copy ? (a.D - a.rd) / VEC : 0);
+  const int turns = a.rd / (2 * VEC), others = a.copy ? (a.D - a.rd) / VEC : 0;  // items that turn; pieces to copy
+  const int items = turns + (others + 1) / 2;
   const int span = min(items, kQ8Threads), hpar = kQ8Threads / span;
   const int hp = threadIdx.x / span;
   if (hp >= hpar) return;
+  const int64_t x0 = t * a.xt, o0 = t * a.ot;
   for (int item = threadIdx.x % span; item < items; item += span) {
-    const int64_t x0 = t * a.xt, o0 = t * a.ot;
-    if (item < turns) {
-      const int p = a.off + (HALF ? item * VEC : 2 * item * VEC), q = HALF ? p + a.rd / 2 : p + VEC;
-      float sn[VEC], cs[VEC];
+    const bool turn = item < turns;
+    int p, q;
+    float sn[VEC], cs[VEC];
+    if (turn) {
+      p = a.off + (HALF ? item * VEC : 2 * item * VEC);
+      q = HALF ? p + a.rd / 2 : p + VEC;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         turn_of(a.freq[item * VEC + e], position, sn[e], cs[e]);
         sn[e] *= a.sign * a.magnitude;
         cs[e] *= a.magnitude;
       }
-#pragma unroll 2
-      for (int h = h0 + hp; h < h1; h += hpar) {
-        V x, y, r, s;
-        x.load(a.x, x0 + h * a.xh + p);
-        y.load(a.x, x0 + h * a.xh + q);
+    } else {  // (of an odd number the last one twice)
+      const int c = 2 * (item - turns), d = min(c + 1, others - 1);
+      p = c * VEC + (c * VEC < a.off ? 0 : a.rd);
+      q = d * VEC + (d * VEC < a.off ? 0 : a.rd);
+    }
+    constexpr int UNROLL = 4;
+    for (int h = h0 + hp; h < h1; h += UNROLL * hpar) {
+      V x[UNROLL], y[UNROLL];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          // pair e: values e of x and y, or values 2e and 2e + 1 of the two side by side
-          const int i = HALF ? e : 2 * e, j = HALF ? e + VEC : 2 * e + 1;
-          const float f = i < VEC ? x.get(i) : y.get(i - VEC), g = j < VEC ? x.get(j) : y.get(j - VEC);
-          const float rf = f * cs[e] - g * sn[e], rg = f * sn[e] + g * cs[e];
-          if (i < VEC) r.set(i, rf);
-          else s.set(i - VEC, rf);
-          if (j < VEC) r.set(j, rg);
-          else s.set(j - VEC, rg);
-        }
-        r.store(a.out, o0 + h * a.oh + p);
-        s.store(a.out, o0 + h * a.oh + q);
+      for (int u = 0; u < UNROLL; ++u) {  // (heads past the last repeat it and are not stored)
+        const int64_t at = x0 + min(h + u * hpar, h1 - 1) * a.xh;
+        x[u].load(a.x, at + p);
+        y[u].load(a.x, at + q);
       }
-    } else {
-      const int c = item - turns, p = c < front ? c * VEC : c * VEC + a.rd;
-#pragma unroll 4
-      for (int h = h0 + hp; h < h1; h += hpar) {
-        V x;
-        x.load(a.x, x0 + h * a.xh + p);
-        x.store(a.out, o0 + h * a.oh + p);
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        V r = x[u], s = y[u];
+        if (turn) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            // pair e: values e of x and y, or values 2e and 2e + 1 of the two side by side
+            const int i = HALF ? e : 2 * e, j = HALF ? e + VEC : 2 * e + 1;
+            const float f = i < VEC ? x[u].get(i) : y[u].get(i - VEC), g = j < VEC ? x[u].get(j) : y[u].get(j - VEC);
+            const float rf = f * cs[e] - g * sn[e], rg = f * sn[e] + g * cs[e];
+            if (i < VEC) r.set(i, rf);
+            else s.set(i - VEC, rf);
+            if (j < VEC) r.set(j, rg);
+            else s.set(j - VEC, rg);
+          }
+        }
+        if (h + u * hpar < h1) {
+          const int64_t at = o0 + (h + u * hpar) * a.oh;
+          r.store(a.out, at + p);
+          s.store(a.out, at + q);
+        }
       }
     }
   }
@@ -420,12 +433,12 @@ extern "C" eg_mla_status eg_mla_rope_rows(const eg_mla_rope* rope, int32_t dtype
   };
   while (vec > 1 && !fits(vec)) vec /= 2;
   // heads of a work-group: whole passes, up to 8 of them while there are work-groups enough
-  const int items = std::max(1, rope_dim / (2 * vec) + (a.copy ? (head_dim - rope_dim) / vec : 0));
+  const int items = std::max(1, rope_dim / (2 * vec) + (a.copy ? ((head_dim - rope_dim) / vec + 1) / 2 : 0));
   const int hpar = std::max(1, kQ8Threads / items);
   int passes = 1;
   while (passes < 8 && static_cast<int64_t>(n_tokens) * num_heads >= int64_t{2048} * hpar * passes * 2) passes *= 2;
-  a.hpu = hpar * passes;
-  a.upt = (num_heads + a.hpu - 1) / a.hpu;
+  a.upt = (num_heads + hpar * passes - 1) / (hpar * passes);
+  a.hpu = (num_heads + a.upt - 1) / a.upt;  // (as many in each)
   const int64_t wgs = static_cast<int64_t>(n_tokens) * a.upt;
   if (wgs > 0x7fffffff) return EG_MLA_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(wgs));
