@@ -894,8 +894,17 @@ constexpr int64_t kMaxRowStride = int64_t{1} << 32;
 constexpr int kQ8MaxLatent = 512, kQ8MaxRopeDim = 64;
 constexpr int64_t kQ8MaxRows = int64_t{1} << 30;  // query rows of a call
 constexpr int kQ8MaxQueries = 1 << 19;
-// Query rows of a sequence, on average, from which blocks of 128 rows are taken.
-constexpr int kQ8ManyRows = 64;
+// Blocks of 128 query rows instead of 16: from so many rows a sequence on average, and so many products (rows x capacity
+// x (2 d_c + d_r)), below which their longer start is the time.  us a call with blocks of 16 / 128, tokens of each
+// sequence in brackets:
+//   16 heads d_c 128, 32 x 4096:  [2] 28.7 / 35.2  [3] 38.1 / 37.0  [4] 36.3 / 36.4  [6] 48.9 / 40.6  [16] 83.6 / 53.5
+//   16 heads d_c 128, 8 x 500:    [4] 21.6 / 23.3  [16] 21.6 / 26.1;  4 x 32768:  [4] 38.7 / 41.8  [8] 53.7 / 48.4
+//   12 heads d_c 64, 32 x 4096:   [2] 25.3 / 28.4  [3] 32.0 / 28.0  [16] 62.5 / 38.3
+//   16 heads d_c 320, 32 x 4096:  [1] 34.2 / 49.4  [2] 44.9 / 52.8  [3] 67.5 / 61.7  [16] 161 / 93.7
+//   128 heads d_c 512, 8 x 4096:  [1] 80.4 / 55.4  [16] 761 / 213;  1 x 30000:  [1] 95.1 / 69.0
+//   5 heads d_c 48, 16 x 3000:    [16] 28.5 / 29.6
+constexpr int kQ8ManyRows = 48;
+constexpr int64_t kQ8ManyProducts = 600000000;
 constexpr int kQ8MaxRuns = 512;
 
 }  // namespace
@@ -988,10 +997,14 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   if (batch > kPageMaxBatch || n_queries > kQ8MaxQueries || rows > kQ8MaxRows) return EG_MLA_ERR_UNSUPPORTED;
   Q8Plan p;
   p.capacity = static_cast<int>(cap);
-  const bool many = rows >= int64_t{kQ8ManyRows} * batch;  // rows of a sequence, on average
+  const bool many = rows >= int64_t{kQ8ManyRows} * batch &&
+                    held_product(held_product(rows, cap), 2 * d.latent_dim + d.rope_dim) >= kQ8ManyProducts;
   p.block_rows = many ? 128 : 16;
   p.tile = many ? (d.latent_dim <= 128 ? 64 : 32) : d.latent_dim <= 128 ? 128 : 64;
-  p.runs = many && d.latent_dim > 128 ? 256 : 512;
+  // one work-group a compute unit where registers or LDS leave room for one, else two
+  p.runs = many && d.latent_dim > 128 ? 256 : kQ8MaxRuns;
+  // (us a call at lead 0, 4, 8, 12: 64 x 512-16384 x 128 heads 226, 214, 216, 216; chunks of 200-600 tokens x 16 heads
+  // 245, 201, 205, 209; blocks of 16, 256 x 250-8192: 71.4, 71.2, 71.3, 76.2)
   p.lead = many ? 4 : 0;
   p.blocks = rows / p.block_rows + batch;
   if (held_product(rows / 16 + batch, cap / 32 + 5) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
@@ -1001,9 +1014,10 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
     at += align_up(static_cast<size_t>(bytes));
     return here;
   };
-  // partial rows: a bound that grows with the batch and the queries, whichever blocks a call takes (128 rows for
-  // each run and sequence, and the query rows)
-  const int64_t part = rows + 128 * (kQ8MaxRuns + static_cast<int64_t>(batch));
+  // partial rows: bounds that grow with the batch and the queries, of either size of block (fp32 rows of blocks of 16,
+  // fp16 of 128), so that a workspace serves every smaller call
+  const int64_t small = 16 * (kQ8MaxRuns + rows / 16 + batch);
+  const int64_t large = 128 * ((d.latent_dim > 128 ? 256 : kQ8MaxRuns) + rows / 128 + batch);
   p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 2);
   const int64_t most = rows / 16 + batch;
   p.off_info = take(most * 16);
@@ -1011,8 +1025,8 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   p.off_start = take(kQ8MaxRuns * int64_t{4});
   p.off_tokens = take(n_queries * int64_t{8});
   p.off_head = take(16);
-  p.off_ml = take(part * 8);
-  p.off_o = take(part * d.latent_dim * 4);
+  p.off_ml = take(std::max(small, large) * 8);
+  p.off_o = take(std::max(4 * small, 2 * large) * d.latent_dim);
   p.bytes = at;
   *out = p;
   return EG_MLA_OK;

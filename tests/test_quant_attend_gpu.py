@@ -39,6 +39,22 @@ def test_new_tokens(gpu, shape, new, lens):
     assert bool((out[sum(new):] == 7).all())  # rows of no sequence
 
 
+WIDE = 1 << 20  # tokens of capacity: enough for blocks of 128 rows wherever there are 48 rows a sequence
+
+
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s not in ("one", "d496")])
+@pytest.mark.parametrize("new,lens", [([130, 1], [131, 1]), ([17, 70, 33], [17, 260, 70]), ([64, 0, 90], [500, 9, 60]),
+                                      ([26], [63]), ([128, 128], [128, 129])])
+def test_blocks_of_128_rows(gpu, shape, new, lens):
+    """The same calls with a table wide enough that many rows are taken together."""
+    L = Layer(len(lens) + 20, *SHAPES[shape], page=16, rows=16 * (sum(-(-n // 16) for n in lens) + 2))
+    table = L.table(lens, WIDE // 16)
+    q = L.normal((sum(new) + 3, L.h, L.dh + L.dr))
+    out = L.run(q, offsets(new), lens, table)
+    check_attend(out[: sum(new)], *L.oracle(q, new, lens, L.slots_of(table)))
+    assert bool((out[sum(new):] == 7).all())
+
+
 @pytest.mark.parametrize("shape", ["kv64", "h16", "mla320", "h128"])
 @pytest.mark.parametrize("new,lens", [([1], [40000]), ([1] * 3, [9000, 17, 12345]), ([9, 2], [9000, 5000])])
 def test_long_contexts(gpu, shape, new, lens):
@@ -81,31 +97,35 @@ def test_contiguous_rows_and_clamped_lengths(gpu, shape):
     assert bool((out == 0).all())  # a capacity of nothing
 
 
+@pytest.mark.parametrize("new", [1, 30])
 @pytest.mark.parametrize("shape", ["odd", "h16", "mla320", "h128"])
-def test_bad_pages_stay_in_the_cache(gpu, shape):
+def test_bad_pages_stay_in_the_cache(gpu, shape, new):
     L = Layer(34, *SHAPES[shape], page=16, rows=16 * 6)
-    table = ints([-7, 6, 2 ** 31 - 1, -2 ** 31]).reshape(2, 2)
-    q = L.normal((2, L.h, L.dh + L.dr))
+    table = torch.full((2, WIDE // 16), 3, dtype=I32, device="cuda")
+    table[:, :2] = ints([-7, 6, 2 ** 31 - 1, -2 ** 31]).reshape(2, 2)
+    q = L.normal((2 * new, L.h, L.dh + L.dr))
     held = np.array([[0, 5], [5, 0]])
     at = lambda b, n: held[b, np.arange(n) // 16] * 16 + np.arange(n) % 16
-    check_attend(L.run(q, None, [30, 32], table), *L.oracle(q, [1, 1], [30, 32], at))
+    check_attend(L.run(q, offsets([new, new]), [30, 32], table), *L.oracle(q, [new, new], [30, 32], at))
 
 
+@pytest.mark.parametrize("wide", [0, WIDE])
 @pytest.mark.parametrize("shape", ["odd", "h16", "h128"])
-def test_offsets_out_of_order_stay_in_bounds(gpu, shape):
+def test_offsets_out_of_order_stay_in_bounds(gpu, shape, wide):
     L = Layer(35, *SHAPES[shape], page=16, rows=16 * 6)
-    table = L.table([30, 30, 20])
+    table = L.table([30, 30, 20], wide // 16 if wide else None)
     q = L.normal((40, L.h, L.dh + L.dr))
     for cu in ([0, 30, 10, 40], [5, 2 ** 31 - 1, -3, 20], [40, 0, 40, 0], [-2 ** 31, -1, 0, 2 ** 31 - 1], [0, 0, 0, 0]):
         L.run(q, ints(cu), [30, 30, 20], table)
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("wide", [0, WIDE])
 @pytest.mark.parametrize("shape", ["odd", "h16", "mla320", "h128"])
-def test_rows_that_stand_for_nan_reach_only_those_that_attend_to_them(gpu, shape):
+def test_rows_that_stand_for_nan_reach_only_those_that_attend_to_them(gpu, shape, wide):
     L = Layer(36, *SHAPES[shape], page=16, rows=16 * 20)
     lens, new = [40, 100, 33], [6, 20, 1]
-    table = L.table(lens)
+    table = L.table(lens, wide // 16 if wide else None)
     at = L.slots_of(table)
     for b, j in ((0, 37), (1, 85), (2, 32)):
         slot = int(at(b, lens[b])[j])
@@ -124,13 +144,14 @@ def test_rows_that_stand_for_nan_reach_only_those_that_attend_to_them(gpu, shape
     check_attend(out, want, size)
 
 
+@pytest.mark.parametrize("wide", [0, WIDE])
 @pytest.mark.parametrize("shape", ["odd", "h16", "mla320", "h128"])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
-def test_not_finite_keys(gpu, shape, value):
+def test_not_finite_keys(gpu, shape, value, wide):
     """A RoPE key that is not finite reaches only the rows that attend to it."""
     L = Layer(37, *SHAPES[shape], page=16, rows=16 * 20)
     lens, new = [50, 30], [10, 4]
-    table = L.table(lens)
+    table = L.table(lens, wide // 16 if wide else None)
     slot = int(L.slots_of(table)(0, 50)[44])  # seen by the new tokens 4 .. 9 of the first
     L.codes[slot, L.dc: L.dc + 2] = torch.tensor([value], dtype=BF).view(U8).cuda()
     q = L.normal((14, L.h, L.dh + L.dr))
@@ -146,14 +167,15 @@ def test_not_finite_keys(gpu, shape, value):
     assert np.array_equal(np.isnan(got), np.isnan(want[seen]))
 
 
+@pytest.mark.parametrize("wide", [0, WIDE])
 @pytest.mark.parametrize("shape", ["kv64", "h16", "mla320", "h128"])
-def test_scales_of_any_size(gpu, shape):
+def test_scales_of_any_size(gpu, shape, wide):
     """Rows of magnitudes from 2^-20 to 2^9 side by side; scores far apart."""
     L = Layer(38, *SHAPES[shape], page=16, rows=16 * 30)
     L.scales.copy_((127 + torch.randint(-20, 2, (L.rows,), generator=L.g, device="cuda")).to(U8))
-    lens, new = [300, 50], [3, 1]
-    table = L.table(lens)
-    q = L.normal((4, L.h, L.dh + L.dr), 0.02)
+    lens, new = [300, 50], [3, 11]
+    table = L.table(lens, wide // 16 if wide else None)
+    q = L.normal((14, L.h, L.dh + L.dr), 0.02)
     check_attend(L.run(q, offsets(new), lens, table), *L.oracle(q, new, lens, L.slots_of(table)))
 
 

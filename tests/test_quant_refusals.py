@@ -9,7 +9,7 @@ import torch
 from paper_2509_16686_amd import binding as B
 
 OK, ARG, UNSUP, WS = B.OK, B.ERR_INVALID_ARG, B.ERR_UNSUPPORTED, B.ERR_WORKSPACE
-BIG = 1 << 24  # made-up addresses, 16 MiB apart
+BIG = 1 << 28  # made-up addresses, 256 MiB apart
 
 
 def at(i, off=0):
@@ -113,7 +113,7 @@ def test_read(layer, change, expect):
 
 
 ATTEND = dict(dims=None, batch=4, n=4, q=at(0), cu=at(1), codes=at(2), scales=at(3), w_uk=at(4), w_uv=at(5), lens=at(6),
-              table=at(7), pages=8, num_slots=1024, ws=at(10), ws_bytes=1 << 24, out=at(8), stream=None)
+              table=at(7), pages=8, num_slots=1024, ws=at(10), ws_bytes=1 << 28, out=at(8), stream=None)
 
 
 @pytest.mark.parametrize("layer,change,expect", [
