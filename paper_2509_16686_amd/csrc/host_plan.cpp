@@ -1022,7 +1022,7 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   const int64_t most = rows / 16 + batch;
   p.off_info = take(most * 16);
   p.off_rows = take(most * 16);
-  p.off_start = take(kQ8MaxRuns * int64_t{4});
+  p.off_start = take(kQ8MaxRuns * int64_t{48});
   p.off_tokens = take(n_queries * int64_t{8});
   p.off_head = take(16);
   p.off_ml = take(std::max(small, large) * 8);

@@ -252,7 +252,7 @@ struct Q8Plan {
   size_t off_q = 0;       // 16-bit [T, H, d_c + d_r]  q_lat fp16 | q^R bf16
   size_t off_info = 0;    // int4 [blocks]
   size_t off_rows = 0;    // int4 [blocks]
-  size_t off_start = 0;   // int32 [runs]
+  size_t off_start = 0;   // int4 [runs][3]
   size_t off_tokens = 0;  // int2 [T]
   size_t off_head = 0;    // int32 [4]
   size_t off_ml = 0;      // fp32 [runs + blocks][block_rows][2]

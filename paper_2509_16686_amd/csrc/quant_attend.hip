@@ -38,9 +38,10 @@ struct Q8Sched {
   // as that many tiles before its first and after its last).
   int4* info;               // [blocks]: sequence, first row in it, rows, place of the first tile
   int4* rows;               // [blocks]: first query row, first new token's position (may be negative), length, place behind the last tile
-  int32_t* start;           // [runs]: the first block with tiles from a run's first place on
+  int4* start;              // [runs][3]: the first block with tiles from a run's first place on (its number, places of a
+                            // run, blocks, places in all; its info; its rows): what a run starts with, in one load
   int2* tokens;             // [T]: the sequence's first block and the token's number in it; -1: no sequence's
-  int32_t* head;            // places of a run, blocks, places
+  int32_t* head;            // places of a run, blocks
   int32_t B, T, H, cap, block_rows, tile, runs, lead;
 };
 
@@ -85,6 +86,7 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   const int tid = threadIdx.x;
   auto first_token = [&](int b) { return a.cu ? clamp_len(a.cu[b], a.T) : min(b, a.T); };
   for (int t = tid; t < a.T; t += THREADS) a.tokens[t] = make_int2(-1, 0);
+  for (int g = tid; g < a.runs; g += THREADS) a.start[3 * g] = make_int4(0, 0, 0, 0);  // no places
   int total = 0, blocks = 0;
   for (int b0 = 0; b0 < a.B; b0 += THREADS) {
     const int b = b0 + tid;
@@ -99,6 +101,7 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   const int most = static_cast<int>(static_cast<int64_t>(a.T) * a.H / a.block_rows) + a.B;
   blocks = min(blocks, most);
   int tiles = 0;
+  int4 info = make_int4(0, 0, 0, 0), rows_of = info;  // of this thread's last block
   for (int k0 = 0; k0 < blocks; k0 += THREADS) {
     const int k = k0 + tid;
     int n_tiles = 0, b = 0, row0 = 0, rows = 0, first = 0, len = 0, cu = 0;
@@ -118,8 +121,8 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
     const int lead = n_tiles ? a.lead : 0;
     const int at = group_scan<THREADS>(n_tiles + lead, tmp, total);
     if (k < blocks) {
-      a.info[k] = make_int4(b, row0, rows, tiles + at + lead);
-      a.rows[k] = make_int4(cu * a.H + row0, first, len, tiles + at + lead + n_tiles);
+      a.info[k] = info = make_int4(b, row0, rows, tiles + at + lead);
+      a.rows[k] = rows_of = make_int4(cu * a.H + row0, first, len, tiles + at + lead + n_tiles);
     }
     tiles += total;
   }
@@ -127,13 +130,20 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   if (tid == 0) {
     a.head[0] = per;
     a.head[1] = blocks;
-    a.head[2] = tiles;
   }
   __threadfence_block();
   __syncthreads();
   for (int k = tid; k < blocks; k += THREADS) {
-    const int e = a.rows[k].w, s = e == a.info[k].w ? e : a.info[k].w - a.lead;
-    for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < e; ++g) a.start[g] = k;
+    if (blocks > THREADS) {
+      info = a.info[k];
+      rows_of = a.rows[k];
+    }
+    const int e = rows_of.w, s = e == info.w ? e : info.w - a.lead;
+    for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < e; ++g) {
+      a.start[3 * g] = make_int4(k, per, blocks, tiles);
+      a.start[3 * g + 1] = info;
+      a.start[3 * g + 2] = rows_of;
+    }
   }
 }
 
@@ -193,8 +203,7 @@ struct Q8Attend {
   Q8Pages cache;
   const int4* info;
   const int4* rows;
-  const int32_t* start;
-  const int32_t* head;
+  const int4* start;
   float* part_ml;  // [piece][block rows][2]
   void* part_o;    // [piece][block rows][DC]: fp32 sums O, or (blocks of 128 rows) O / l in fp16
   int32_t H, DC, DR;
@@ -256,12 +265,17 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
   const int row_bytes = a.DC + 2 * a.DR;
 
   const int run = xcd_logical_block(blockIdx.x, gridDim.x);
-  const int per = uniform(a.head[0]), blocks = uniform(a.head[1]), tiles = uniform(a.head[2]);
+  const int4 mine = uniform(a.start[3 * run]);
+  int4 info = uniform(a.start[3 * run + 1]), rw = uniform(a.start[3 * run + 2]);
+  const int per = mine.y, blocks = mine.z, tiles = mine.w;
   int at = run * per;
   if (static_cast<int64_t>(run) * per >= tiles) return;
   const int end = min(at + per, tiles);
-  for (int k = uniform(a.start[run]); k < blocks; ++k) {
-    const int4 info = uniform(a.info[k]), rw = uniform(a.rows[k]);
+  for (int k = mine.x; k < blocks; ++k) {
+    if (k != mine.x) {
+      info = uniform(a.info[k]);
+      rw = uniform(a.rows[k]);
+    }
     at = max(at, info.w);
     if (at >= end) break;
     const int next = rw.w;
@@ -700,7 +714,7 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   uint16_t* qrows = reinterpret_cast<uint16_t*>(ws + p.off_q);
   const Q8Sched sched{cu_seqlens, seq_lens, reinterpret_cast<int4*>(ws + p.off_info), reinterpret_cast<int4*>(ws + p.off_rows),
-                      reinterpret_cast<int32_t*>(ws + p.off_start), reinterpret_cast<int2*>(ws + p.off_tokens),
+                      reinterpret_cast<int4*>(ws + p.off_start), reinterpret_cast<int2*>(ws + p.off_tokens),
                       reinterpret_cast<int32_t*>(ws + p.off_head), batch, n_queries, d.num_heads, p.capacity, p.block_rows,
                       p.tile, p.runs, p.lead};
   (void)hipGetLastError();
@@ -708,7 +722,7 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   Q8Pages pages{page_table ? page_table : sched.head, page_table != nullptr, d.page_size, static_cast<int32_t>(num_slots / d.page_size), max_pages_per_seq, p.capacity, 0, 31};
   while ((int64_t{1} << (pages.shift - 31)) < d.page_size) ++pages.shift;  // l = ceil(log2 P): mul = ceil(2^(31+l) / P) < 2^32
   pages.mul = static_cast<uint32_t>(((uint64_t{1} << pages.shift) + d.page_size - 1) / d.page_size);
-  const Q8Attend at{qrows, codes, scales, pages, sched.info, sched.rows, sched.start, sched.head,
+  const Q8Attend at{qrows, codes, scales, pages, sched.info, sched.rows, sched.start,
                     reinterpret_cast<float*>(ws + p.off_ml), ws + p.off_o,
                     d.num_heads, d.latent_dim, d.rope_dim, softmax_scale(d) * 1.4426950408889634f};
   const dim3 grid(p.runs), block(kQ8AttendThreads);

@@ -56,12 +56,17 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
   const int row_bytes = a.DC + 2 * a.DR;
 
   const int run = xcd_logical_block(blockIdx.x, gridDim.x);
-  const int per = uniform(a.head[0]), blocks = uniform(a.head[1]), tiles = uniform(a.head[2]);
+  const int4 mine = uniform(a.start[3 * run]);
+  int4 info = uniform(a.start[3 * run + 1]), rw = uniform(a.start[3 * run + 2]);
+  const int per = mine.y, blocks = mine.z, tiles = mine.w;
   if (static_cast<int64_t>(run) * per >= tiles) return;
   int at = run * per;
   const int end = min(at + per, tiles);
-  for (int k = uniform(a.start[run]); k < blocks; ++k) {
-    const int4 info = uniform(a.info[k]), rw = uniform(a.rows[k]);
+  for (int k = mine.x; k < blocks; ++k) {
+    if (k != mine.x) {
+      info = uniform(a.info[k]);
+      rw = uniform(a.rows[k]);
+    }
     at = max(at, info.w);
     if (at >= end) break;
     const int next = rw.w;
