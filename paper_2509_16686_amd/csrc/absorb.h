@@ -12,10 +12,6 @@ namespace egmla {
 hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* qfull,
                          hipStream_t stream);
 
-// The same into 16-bit rows [q_lat fp16 | q^R bf16], for any shape of bf16 storage (the vector kernel).
-hipError_t launch_absorb_half(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, uint16_t* rows,
-                              hipStream_t stream);
-
 // Absorbed query in three bf16 parts that together hold the fp32 q_lat, in the
 // order of the A operands of v_mfma_f32_16x16x32_bf16: per sequence and block
 // of 16 heads, one run of 1 KB per 32 values of [first part | q^R], then of the

@@ -1,10 +1,83 @@
-// One tile of the query absorption on MFMA (bf16 storage).
+// Tiles of the query absorption: for any shape, and on MFMA (bf16 storage).
 #pragma once
 
 #include "absorb.h"
 #include "device_common.h"
 
 namespace egmla {
+
+// ---------------------------------------------------------------------------
+// Absorption for any shape: qfull[b,h,:] = [W_UK[h]^T q^C[b,h] | q^R[b,h]]   (fp32)
+// grid (H, ceil(DC / 64), ceil(B / 16)), 256 threads = 64 latent columns x
+// 4 slices of the head dim.  Each W_UK row segment is read once per 16
+// sequences with 128-byte coalesced loads; the 4 slices are summed in LDS.
+// ---------------------------------------------------------------------------
+constexpr int kAbsorbRows = 16;
+constexpr int kAbsorbCols = 64;
+
+inline size_t absorb_any_lds(int DH) { return sizeof(float) * (kAbsorbRows * DH + 4 * kAbsorbRows * kAbsorbCols); }
+
+// Tile (h, by, bz) of it, in `smem`: q rows [kAbsorbRows][DH], partial sums [4][kAbsorbRows][kAbsorbCols].  HALF: 16-bit rows
+// [q_lat fp16 | q^R bf16] in the fp32 ones' place.
+template <bool BF16, bool HALF>
+__device__ __forceinline__ void absorb_any_tile(const void* __restrict__ q, const void* __restrict__ w_uk,
+                                                float* __restrict__ qfull, int B, int H, int DH, int DC, int DR, int h,
+                                                int by, int bz, float* smem) {
+  [[maybe_unused]] uint16_t* qhalf = reinterpret_cast<uint16_t*>(qfull);
+  float* q_s = smem;
+  float* red = smem + kAbsorbRows * DH;
+  const int c0 = by * kAbsorbCols;
+  const int b0 = bz * kAbsorbRows;
+  const int nb = min(kAbsorbRows, B - b0);
+  const int DQin = DH + DR;
+  const int DQ = DC + DR;
+  const int tid = threadIdx.x;
+  for (int i = tid; i < kAbsorbRows * DH; i += 256) {
+    const int bb = i / DH, k = i % DH;
+    q_s[i] = bb < nb ? ld<BF16>(q, (static_cast<int64_t>(b0 + bb) * H + h) * DQin + k) : 0.f;
+  }
+  __syncthreads();
+  const int cl = tid & (kAbsorbCols - 1);
+  const int kq = tid / kAbsorbCols;  // 0..3
+  const int c = c0 + cl;
+  const int kper = (DH + 3) / 4;
+  const int k_lo = kq * kper, k_hi = min(DH, k_lo + kper);
+  float acc[kAbsorbRows];
+#pragma unroll
+  for (int bb = 0; bb < kAbsorbRows; ++bb) acc[bb] = 0.f;
+  if (c < DC) {
+    const int64_t wbase = static_cast<int64_t>(h) * DH * DC + c;
+#pragma unroll 4
+    for (int k = k_lo; k < k_hi; ++k) {
+      const float wv = ld<BF16>(w_uk, wbase + static_cast<int64_t>(k) * DC);
+#pragma unroll
+      for (int bb = 0; bb < kAbsorbRows; ++bb) acc[bb] = fmaf(wv, q_s[bb * DH + k], acc[bb]);
+    }
+  }
+#pragma unroll
+  for (int bb = 0; bb < kAbsorbRows; ++bb) red[(kq * kAbsorbRows + bb) * kAbsorbCols + cl] = acc[bb];
+  __syncthreads();
+  for (int i = tid; i < kAbsorbRows * kAbsorbCols; i += 256) {
+    const int bb = i / kAbsorbCols, cc = i % kAbsorbCols;
+    if (bb < nb && c0 + cc < DC) {
+      float v = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v += red[(j * kAbsorbRows + bb) * kAbsorbCols + cc];
+      const int64_t at = (static_cast<int64_t>(b0 + bb) * H + h) * DQ + c0 + cc;
+      if constexpr (HALF) qhalf[at] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
+      else qfull[at] = v;
+    }
+  }
+  if (by == 0) {
+    for (int i = tid; i < nb * DR; i += 256) {
+      const int bb = i / DR, r = i % DR;
+      const int64_t at = (static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r;
+      const float v = ld<BF16>(q, (static_cast<int64_t>(b0 + bb) * H + h) * DQin + DH + r);
+      if constexpr (HALF) qhalf[at] = f32_to_bf16(v);
+      else qfull[at] = v;
+    }
+  }
+}
 
 // ---------------------------------------------------------------------------
 // Absorption on MFMA: qfull[b, h, c] = sum_k q^C[b, h, k] W_UK[h, k, c] for

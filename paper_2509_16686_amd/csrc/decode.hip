@@ -23,6 +23,7 @@
 #include <mutex>
 
 #include "absorb.h"
+#include "absorb_tile.h"
 #include "device_common.h"
 #include "eg_mla.h"
 #include "host_plan.h"
@@ -31,76 +32,13 @@ namespace egmla {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// ---------------------------------------------------------------------------
-// 1. absorption: qfull[b,h,:] = [W_UK[h]^T q^C[b,h] | q^R[b,h]]   (fp32)
-// grid (H, ceil(DC / 64), ceil(B / 16)), 256 threads = 64 latent columns x
-// 4 slices of the head dim.  Each W_UK row segment is read once per 16
-// sequences with 128-byte coalesced loads; the 4 slices are summed in LDS.
-// ---------------------------------------------------------------------------
-constexpr int kAbsorbRows = 16;
-constexpr int kAbsorbCols = 64;
-
-// HALF: 16-bit rows [q_lat fp16 | q^R bf16] in their place.
-template <bool BF16, bool HALF = false>
+// 1. absorption for any shape (absorb_tile.h)
+template <bool BF16>
 __global__ __launch_bounds__(256) void absorb_kernel(const void* __restrict__ q, const void* __restrict__ w_uk,
                                                      float* __restrict__ qfull, int B, int H, int DH, int DC,
                                                      int DR) {
-  [[maybe_unused]] uint16_t* qhalf = reinterpret_cast<uint16_t*>(qfull);
-  extern __shared__ float smem[];  // q rows [kAbsorbRows][DH], partial sums [4][kAbsorbRows][kAbsorbCols]
-  float* q_s = smem;
-  float* red = smem + kAbsorbRows * DH;
-  const int h = blockIdx.x;
-  const int c0 = blockIdx.y * kAbsorbCols;
-  const int b0 = blockIdx.z * kAbsorbRows;
-  const int nb = min(kAbsorbRows, B - b0);
-  const int DQin = DH + DR;
-  const int DQ = DC + DR;
-  const int tid = threadIdx.x;
-  for (int i = tid; i < kAbsorbRows * DH; i += 256) {
-    const int bb = i / DH, k = i % DH;
-    q_s[i] = bb < nb ? ld<BF16>(q, (static_cast<int64_t>(b0 + bb) * H + h) * DQin + k) : 0.f;
-  }
-  __syncthreads();
-  const int cl = tid & (kAbsorbCols - 1);
-  const int kq = tid / kAbsorbCols;  // 0..3
-  const int c = c0 + cl;
-  const int kper = (DH + 3) / 4;
-  const int k_lo = kq * kper, k_hi = min(DH, k_lo + kper);
-  float acc[kAbsorbRows];
-#pragma unroll
-  for (int bb = 0; bb < kAbsorbRows; ++bb) acc[bb] = 0.f;
-  if (c < DC) {
-    const int64_t wbase = static_cast<int64_t>(h) * DH * DC + c;
-#pragma unroll 4
-    for (int k = k_lo; k < k_hi; ++k) {
-      const float wv = ld<BF16>(w_uk, wbase + static_cast<int64_t>(k) * DC);
-#pragma unroll
-      for (int bb = 0; bb < kAbsorbRows; ++bb) acc[bb] = fmaf(wv, q_s[bb * DH + k], acc[bb]);
-    }
-  }
-#pragma unroll
-  for (int bb = 0; bb < kAbsorbRows; ++bb) red[(kq * kAbsorbRows + bb) * kAbsorbCols + cl] = acc[bb];
-  __syncthreads();
-  for (int i = tid; i < kAbsorbRows * kAbsorbCols; i += 256) {
-    const int bb = i / kAbsorbCols, cc = i % kAbsorbCols;
-    if (bb < nb && c0 + cc < DC) {
-      float v = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v += red[(j * kAbsorbRows + bb) * kAbsorbCols + cc];
-      const int64_t at = (static_cast<int64_t>(b0 + bb) * H + h) * DQ + c0 + cc;
-      if constexpr (HALF) qhalf[at] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
-      else qfull[at] = v;
-    }
-  }
-  if (blockIdx.y == 0) {
-    for (int i = tid; i < nb * DR; i += 256) {
-      const int bb = i / DR, r = i % DR;
-      const int64_t at = (static_cast<int64_t>(b0 + bb) * H + h) * DQ + DC + r;
-      const float v = ld<BF16>(q, (static_cast<int64_t>(b0 + bb) * H + h) * DQin + DH + r);
-      if constexpr (HALF) qhalf[at] = f32_to_bf16(v);
-      else qfull[at] = v;
-    }
-  }
+  extern __shared__ float smem[];
+  absorb_any_tile<BF16, false>(q, w_uk, qfull, B, H, DH, DC, DR, blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
 
 // Split-K bookkeeping shared by the split kernels.
@@ -622,18 +560,6 @@ hipError_t launch_absorb_parts(const eg_mla_dims& d, int32_t batch, const void* 
   return hipGetLastError();
 }
 
-template <typename K>
-static hipError_t launch_absorb_any(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* rows,
-                                    K kern, hipStream_t stream) {
-  const dim3 grid(d.num_heads, (d.latent_dim + kAbsorbCols - 1) / kAbsorbCols, (batch + kAbsorbRows - 1) / kAbsorbRows);
-  const size_t lds = sizeof(float) * (kAbsorbRows * d.head_dim + 4 * kAbsorbRows * kAbsorbCols);
-  const hipError_t e = set_lds(kern, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, grid, dim3(256), lds, stream, q, w_uk, rows, batch, d.num_heads, d.head_dim, d.latent_dim,
-                     d.rope_dim);
-  return hipGetLastError();
-}
-
 hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, float* qfull,
                          hipStream_t stream) {
   const bool bf = d.dtype == EG_MLA_BF16;
@@ -649,12 +575,14 @@ hipError_t launch_absorb(const eg_mla_dims& d, int32_t batch, const void* q, con
                        SchedArgs{});
     return hipGetLastError();
   }
-  return launch_absorb_any(d, batch, q, w_uk, qfull, bf ? absorb_kernel<true> : absorb_kernel<false>, stream);
-}
-
-hipError_t launch_absorb_half(const eg_mla_dims& d, int32_t batch, const void* q, const void* w_uk, uint16_t* rows,
-                              hipStream_t stream) {
-  return launch_absorb_any(d, batch, q, w_uk, reinterpret_cast<float*>(rows), absorb_kernel<true, true>, stream);
+  const dim3 grid(d.num_heads, (d.latent_dim + kAbsorbCols - 1) / kAbsorbCols, (batch + kAbsorbRows - 1) / kAbsorbRows);
+  const size_t lds = absorb_any_lds(d.head_dim);
+  auto kern = bf ? absorb_kernel<true> : absorb_kernel<false>;
+  hipError_t e = set_lds(kern, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, grid, dim3(256), lds, stream, q, w_uk, qfull, batch, d.num_heads, d.head_dim, d.latent_dim,
+                     d.rope_dim);
+  return hipGetLastError();
 }
 
 namespace {

@@ -11,7 +11,7 @@
 // tiles of all blocks, in order, into equal runs, one for each work-group (a run
 // may span blocks).  Three launches:
 //  1. q8_prep_kernel: the query's absorption, 16-bit rows, and (one work-group) blocks, tiles and runs from the lengths
-//     on the device (d_h other than 64 and 128: two launches);
+//     on the device;
 //  2. q8_attend_kernel or, for blocks of 128 rows, q8_rows_kernel (quant_rows.h): a partial row (maximum, sum, latent
 //     sum) for each row of each piece (the tiles of one block in one run);
 //  3. q8_merge_kernel: joins the partial rows of a query row and applies W_UV.
@@ -147,14 +147,12 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   }
 }
 
-__global__ __launch_bounds__(1024) void q8_schedule_kernel(Q8Sched a) { q8_schedule<1024>(a); }
-
 // Schedule (work-group 0) and absorption in one launch: 16-bit rows [q_lat fp16 | q^R bf16].
 struct Q8Prep {
   const uint16_t* q;
   const uint16_t* w_uk;
   uint16_t* rows;
-  int32_t T, H, DC, DR, row_blocks;
+  int32_t T, H, DH, DC, DR, row_blocks;
 };
 template <int DH, int BLOCKS, int COLS>
 __global__ __launch_bounds__(256) void q8_prep_kernel(Q8Prep p, Q8Sched a) {
@@ -165,6 +163,17 @@ __global__ __launch_bounds__(256) void q8_prep_kernel(Q8Prep p, Q8Sched a) {
   const int wg = blockIdx.x - 1, h = wg % p.H, rest = wg / p.H;
   absorb_tile<DH, BLOCKS, COLS, AbsorbRows::kHalf>(p.q, p.w_uk, nullptr, p.rows, p.T, p.H, p.DC, p.DR, h,
                                                    rest % p.row_blocks, rest / p.row_blocks);
+}
+
+__global__ __launch_bounds__(256) void q8_prep_any_kernel(Q8Prep p, Q8Sched a) {  // (for any d_h)
+  extern __shared__ float smem[];
+  if (blockIdx.x == 0) {
+    q8_schedule<256>(a);
+    return;
+  }
+  const int wg = blockIdx.x - 1, h = wg % p.H, rest = wg / p.H;
+  absorb_any_tile<true, true>(p.q, p.w_uk, reinterpret_cast<float*>(p.rows), p.T, p.H, p.DH, p.DC, p.DR, h,
+                              rest / p.row_blocks, rest % p.row_blocks, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -670,16 +679,13 @@ namespace {
 
 hipError_t launch_q8_prep(const eg_mla_dims& d, int32_t n, const void* q, const void* w_uk, uint16_t* rows,
                           const Q8Sched& sched, hipStream_t stream) {
-  if (d.head_dim != 64 && d.head_dim != 128) {
-    hipLaunchKernelGGL(q8_schedule_kernel, dim3(1), dim3(1024), 0, stream, sched);
-    return launch_absorb_half(d, n, q, w_uk, rows, stream);
-  }
   // 64 queries a work-group where those of 16 would be many; narrow column slices where few
   const int64_t tiles = static_cast<int64_t>(d.num_heads) * ((n + kAbsRows - 1) / kAbsRows);
-  const bool grouped = tiles >= 512, narrow = tiles < kAbsMinWorkGroups;
-  const int cols = narrow ? kAbsColsNarrow : kAbsCols, block = kAbsRows * (grouped ? kAbsBlocks : 1);
-  const Q8Prep p{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(w_uk), rows, n, d.num_heads, d.latent_dim,
-                 d.rope_dim, (n + block - 1) / block};
+  const bool any = d.head_dim != 64 && d.head_dim != 128, grouped = !any && tiles >= 512, narrow = tiles < kAbsMinWorkGroups;
+  const int cols = any ? kAbsorbCols : narrow ? kAbsColsNarrow : kAbsCols;
+  const int block = any ? kAbsorbRows : kAbsRows * (grouped ? kAbsBlocks : 1);
+  const Q8Prep p{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(w_uk), rows, n, d.num_heads, d.head_dim,
+                 d.latent_dim, d.rope_dim, (n + block - 1) / block};
   const int64_t wgs = int64_t{d.num_heads} * p.row_blocks * ((d.latent_dim + cols - 1) / cols) + 1;
   auto kern = d.head_dim == 64 ? (grouped  ? q8_prep_kernel<64, kAbsBlocks, kAbsCols>
                                   : narrow ? q8_prep_kernel<64, 1, kAbsColsNarrow>
@@ -687,7 +693,17 @@ hipError_t launch_q8_prep(const eg_mla_dims& d, int32_t n, const void* q, const 
               : grouped ? q8_prep_kernel<128, kAbsBlocks, kAbsCols>
               : narrow  ? q8_prep_kernel<128, 1, kAbsColsNarrow>
                         : q8_prep_kernel<128, 1, kAbsCols>;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, stream, p, sched);
+  size_t lds = 0;
+  if (any) {
+    kern = q8_prep_any_kernel;
+    lds = absorb_any_lds(d.head_dim);  // up to 80 KB
+    if (lds > 32768) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(lds));
+      if (e != hipSuccess) return e;
+    }
+  }
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(256), lds, stream, p, sched);
   return hipGetLastError();
 }
 

@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 #         h   dh   dv   dc   dr
 SHAPES = {"one": (1, 8, 8, 16, 0), "odd": (5, 40, 56, 48, 24), "kv64": (12, 64, 64, 64, 64), "h16": (16, 128, 128, 128, 64),
           "h20": (20, 128, 96, 128, 32), "d144": (16, 64, 136, 144, 64), "mla320": (16, 128, 128, 320, 64),
-          "h24": (24, 128, 128, 512, 64), "h128": (128, 128, 128, 512, 64), "h130": (130, 16, 8, 64, 8), "d496": (3, 24, 24, 496, 16)}
+          "h24": (24, 128, 128, 512, 64), "h128": (128, 128, 128, 512, 64), "h130": (130, 16, 8, 64, 8), "d496": (3, 24, 24, 496, 16),
+          "tall": (2, 1024, 1024, 64, 64)}
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -42,7 +43,7 @@ def test_new_tokens(gpu, shape, new, lens):
 WIDE = 1 << 20  # tokens of capacity: enough for blocks of 128 rows wherever there are 48 rows a sequence
 
 
-@pytest.mark.parametrize("shape", [s for s in SHAPES if s not in ("one", "d496")])
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s not in ("one", "d496", "tall")])
 @pytest.mark.parametrize("new,lens", [([130, 1], [131, 1]), ([17, 70, 33], [17, 260, 70]), ([64, 0, 90], [500, 9, 60]),
                                       ([26], [63]), ([128, 128], [128, 129])])
 def test_blocks_of_128_rows(gpu, shape, new, lens):
