@@ -101,7 +101,6 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   const int most = static_cast<int>(static_cast<int64_t>(a.T) * a.H / a.block_rows) + a.B;
   blocks = min(blocks, most);
   int tiles = 0;
-  int4 info = make_int4(0, 0, 0, 0), rows_of = info;  // of this thread's last block
   for (int k0 = 0; k0 < blocks; k0 += THREADS) {
     const int k = k0 + tid;
     int n_tiles = 0, b = 0, row0 = 0, rows = 0, first = 0, len = 0, cu = 0;
@@ -121,8 +120,8 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
     const int lead = n_tiles ? a.lead : 0;
     const int at = group_scan<THREADS>(n_tiles + lead, tmp, total);
     if (k < blocks) {
-      a.info[k] = info = make_int4(b, row0, rows, tiles + at + lead);
-      a.rows[k] = rows_of = make_int4(cu * a.H + row0, first, len, tiles + at + lead + n_tiles);
+      a.info[k] = make_int4(b, row0, rows, tiles + at + lead);
+      a.rows[k] = make_int4(cu * a.H + row0, first, len, tiles + at + lead + n_tiles);
     }
     tiles += total;
   }
@@ -131,18 +130,25 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
     a.head[0] = per;
     a.head[1] = blocks;
   }
+  auto put = [&](int g, int k, int4 info, int4 rows) {
+    a.start[3 * g] = make_int4(k, per, blocks, tiles);
+    a.start[3 * g + 1] = info;
+    a.start[3 * g + 2] = rows;
+  };
   __threadfence_block();
   __syncthreads();
-  for (int k = tid; k < blocks; k += THREADS) {
-    if (blocks > THREADS) {
-      info = a.info[k];
-      rows_of = a.rows[k];
+  if (blocks <= kPageMaxBatch) {  // a thread a run: the first block that ends behind the run's first place
+    for (int k = tid; k <= blocks; k += THREADS) first_s[k] = k ? a.rows[k - 1].w : 0;
+    __syncthreads();
+    for (int g = tid; g < a.runs && static_cast<int64_t>(g) * per < tiles; g += THREADS) {
+      const int k = first_above(first_s, blocks, g * per);
+      put(g, k, a.info[k], a.rows[k]);
     }
-    const int e = rows_of.w, s = e == info.w ? e : info.w - a.lead;
-    for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < e; ++g) {
-      a.start[3 * g] = make_int4(k, per, blocks, tiles);
-      a.start[3 * g + 1] = info;
-      a.start[3 * g + 2] = rows_of;
+  } else {  // more blocks than runs: few runs start in one
+    for (int k = tid; k < blocks; k += THREADS) {
+      const int4 info = a.info[k], rows = a.rows[k];
+      const int s = rows.w == info.w ? rows.w : info.w - a.lead;
+      for (int g = (s + per - 1) / per; g < a.runs && static_cast<int64_t>(g) * per < rows.w; ++g) put(g, k, info, rows);
     }
   }
 }
@@ -472,8 +478,8 @@ namespace egmla {
 // new tokens per work-group (up to 16, or 32 of wide rows).  LPR lanes hold a row, 8 dims each; each group
 // of LPR lanes is a worker.  With at least as many tokens as workers a worker takes
 // its tokens (up to TPW) side by side, else a token's workers take its partial rows
-// in turn and meet in LDS.  Rows are folded online in fp32, two loaded together; the
-// merged row o / l goes to LDS as bf16 hi + lo, the B operands of out^T[v][token] =
+// in turn and meet in LDS.  Rows are folded online in fp32, two or four loaded together;
+// the merged row o / l goes to LDS as bf16 hi + lo, the B operands of out^T[v][token] =
 // W_UV[h] o^T on v_mfma_f32_16x16x32_bf16, so that the up-projection adds only
 // W_UV's own rounding.  Bound by its chain of loads (token, block, rows), behind
 // which W_UV's rows arrive.
@@ -501,7 +507,7 @@ struct Q8MergeCfg {
 template <int LPR, bool HALF>
 __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) void q8_merge_kernel(Q8Merge a) {
   using C = Q8MergeCfg<LPR>;
-  constexpr int DCP = 8 * LPR, NKC = DCP / 32, OS = DCP + 8, GPW = 64 / LPR, TPW = C::TPW, U = 2;
+  constexpr int DCP = 8 * LPR, NKC = DCP / 32, OS = DCP + 8, GPW = 64 / LPR, TPW = C::TPW, U = LPR == 64 ? 2 : 4;
   __shared__ __attribute__((aligned(16))) uint16_t o_s[2][C::TOKENS][OS];  // merged rows, hi and lo
   __shared__ __attribute__((aligned(16))) float part[C::WORKERS][DCP];
   __shared__ float m_part[C::WORKERS], l_part[C::WORKERS];
