@@ -702,7 +702,8 @@ eg_mla_status eg_mla_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t n
  * (magnitudes below 65504), q^R and k^R in bf16; sums are fp32.  Which tokens a row
  * does not attend to does not matter to it, whatever they hold.
  *
- * Batch above 4096, n_queries above 2^19 or n_queries * H above 2^30:
+ * Batch above 4096, n_queries above 2^19, ceil(n_queries / 16) H ceil(d_c / 64)
+ * above 2^23, or query rows times capacity past what 32 bits count in tiles:
  * EG_MLA_ERR_UNSUPPORTED.  Lengths, ids, pages and offsets on the device are made
  * safe, not checked.  No output or workspace overlaps an input or another output
  * (EG_MLA_ERR_INVALID_ARG).

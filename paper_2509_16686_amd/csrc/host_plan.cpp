@@ -892,7 +892,7 @@ eg_mla_status check_rope(const eg_mla_rope* r, int32_t rope_dim) {
 constexpr int kMaxRopeDim = 640;
 constexpr int64_t kMaxRowStride = int64_t{1} << 32;
 constexpr int kQ8MaxLatent = 512, kQ8MaxRopeDim = 64;
-constexpr int64_t kQ8MaxRows = int64_t{1} << 30;  // query rows of a call
+constexpr int64_t kQ8MaxTiles = int64_t{1} << 23;  // tiles of 16 queries, a head and 64 latent values (work-groups of the absorption)
 constexpr int kQ8MaxQueries = 1 << 19;
 // Blocks of 128 query rows instead of 16: from so many rows a sequence on average, and so many products (rows x capacity
 // x (2 d_c + d_r)), below which their longer start is the time.  us a call with blocks of 16 / 128, tokens of each
@@ -994,7 +994,9 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   const int64_t cap = static_cast<int64_t>(max_pages_per_seq) * d.page_size;
   if (cap > kMaxCapacity) return EG_MLA_ERR_INVALID_ARG;
   const int64_t rows = static_cast<int64_t>(n_queries) * d.num_heads;
-  if (batch > kPageMaxBatch || n_queries > kQ8MaxQueries || rows > kQ8MaxRows) return EG_MLA_ERR_UNSUPPORTED;
+  if (batch > kPageMaxBatch || n_queries > kQ8MaxQueries ||
+      held_product(ceil_div(n_queries, 16) * int64_t{d.num_heads}, ceil_div(d.latent_dim, 64)) > kQ8MaxTiles)
+    return EG_MLA_ERR_UNSUPPORTED;
   Q8Plan p;
   p.capacity = static_cast<int>(cap);
   const bool many = rows >= int64_t{kQ8ManyRows} * batch &&
@@ -1007,7 +1009,7 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   // 245, 201, 205, 209; blocks of 16, 256 x 250-8192: 71.4, 71.2, 71.3, 76.2)
   p.lead = many ? 4 : 0;
   p.blocks = rows / p.block_rows + batch;
-  if (held_product(rows / 16 + batch, cap / 32 + 5) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
+  if (held_product(p.blocks, cap / p.tile + 1 + p.lead) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;

@@ -118,7 +118,8 @@ ATTEND = dict(dims=None, batch=4, n=4, q=at(0), cu=at(1), codes=at(2), scales=at
 
 @pytest.mark.parametrize("layer,change,expect", [
     ({}, dict(batch=0, n=0), OK), ({}, dict(n=0), OK), ({}, dict(batch=-1), ARG), ({}, dict(n=-1), ARG),
-    ({}, dict(batch=4097), UNSUP), ({}, dict(n=(1 << 19) + 1), UNSUP), (dict(num_heads=1 << 12), dict(n=1 << 19), UNSUP),
+    ({}, dict(batch=4097), UNSUP), ({}, dict(n=(1 << 19) + 1), UNSUP), (dict(num_heads=1 << 12), dict(n=1 << 19), UNSUP), (dict(num_heads=1 << 23), {}, UNSUP),
+    (dict(), dict(n=1 << 19, pages=1 << 24, num_slots=1 << 20), UNSUP),
     ({}, dict(pages=-1), ARG), ({}, dict(pages=1 << 25), ARG), ({}, dict(cu=None, n=5), ARG), ({}, dict(table=None), ARG),
     ({}, dict(num_slots=63), ARG), ({}, dict(num_slots=1 << 31), UNSUP), (dict(dtype=B.FP32), {}, UNSUP),
     (dict(latent_dim=136), {}, UNSUP), (dict(rope_dim=72), {}, UNSUP),

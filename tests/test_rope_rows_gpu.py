@@ -143,3 +143,16 @@ def test_not_finite_values_stay_with_their_pair(gpu):
     for i, h, m in ((0, 1, 2), (1, 0, 20), (1, 1, 0)):
         want[i, h, 2 * m: 2 * m + 2] = True
     assert torch.equal(bad, want)
+
+
+def test_more_work_groups_than_one_dimension_takes(gpu):
+    n = (1 << 24) + 1001
+    x = rows(11, (n, 1, 8), BF)
+    positions = torch.arange(n, device="cuda", dtype=I32)
+    out = torch.empty_like(x)
+    B.rope_rows(B.make_rope(), x, positions, out, rope_dim=4)
+    at = torch.tensor([0, 1, 12345, (1 << 20) - 1, 1 << 20, (1 << 24) - 1, 1 << 24, n - 2, n - 1], device="cuda")
+    check(out[at], x[at], 4, 4, positions[at], frequencies(4), False)
+    B.rope_rows(B.make_rope(), out, positions, out, rope_dim=4, inverse=True)
+    # there and back, a value is rounded twice, and each of a pair takes part of the other's rounding
+    assert (out.float() - x.float()).abs().max() <= 4 * 2.0 ** -8 * x.float().abs().max()
