@@ -478,10 +478,10 @@ extern "C" int64_t eg_mla_quant_row_bytes(const eg_mla_dims* dims) {
 }
 
 extern "C" eg_mla_status eg_mla_quant_write(const eg_mla_dims* dims, const eg_mla_rope* rope, int32_t n_tokens, const void* kv,
-                                         int64_t kv_stride, const void* kv_norm_w, const void* k_norm_w,
-                                         const void* gate_table, const int32_t* token_ids, const int32_t* positions,
-                                         const int32_t* slots, uint8_t* codes, uint8_t* scales, int64_t num_slots,
-                                         void* stream_) {
+                                            int64_t kv_stride, const void* kv_norm_w, const void* k_norm_w,
+                                            const void* gate_table, const int32_t* token_ids, const int32_t* positions,
+                                            const int32_t* slots, uint8_t* codes, uint8_t* scales, int64_t num_slots,
+                                            void* stream_) {
   const eg_mla_status st = validate_q8_write(dims, rope, n_tokens, kv, kv_stride, kv_norm_w, k_norm_w, gate_table,
                                              token_ids, positions, slots, codes, scales, num_slots);
   if (st != EG_MLA_OK || n_tokens == 0) return st;
@@ -516,9 +516,9 @@ extern "C" eg_mla_status eg_mla_quant_write(const eg_mla_dims* dims, const eg_ml
 }
 
 extern "C" eg_mla_status eg_mla_quant_read(const eg_mla_dims* dims, int32_t batch, int32_t total_tokens, const uint8_t* codes,
-                                        const uint8_t* scales, const int32_t* first_tokens, const int32_t* cu_seqlens,
-                                        const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
-                                        void* out, void* stream_) {
+                                           const uint8_t* scales, const int32_t* first_tokens, const int32_t* cu_seqlens,
+                                           const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                           void* out, void* stream_) {
   const eg_mla_status st = validate_q8_read(dims, batch, total_tokens, codes, scales, first_tokens, cu_seqlens,
                                             page_table, max_pages_per_seq, num_slots, out);
   if (st != EG_MLA_OK || batch == 0 || total_tokens == 0 || max_pages_per_seq == 0) return st;

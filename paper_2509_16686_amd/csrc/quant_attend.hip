@@ -37,7 +37,8 @@ struct Q8Sched {
   // Places: the tiles of all blocks in order, `lead` places left free before each block's (a piece costs about as much
   // as that many tiles before its first and after its last).
   int4* info;               // [blocks]: sequence, first row in it, rows, place of the first tile
-  int4* rows;               // [blocks]: first query row, first new token's position (may be negative), length, place behind the last tile
+  int4* rows;               // [blocks]: first query row, first new token's position (may be negative), length, place
+                            // behind the last tile
   int4* start;              // [runs][3]: the first block with tiles from a run's first place on (its number, places of a
                             // run, blocks, places in all; its info; its rows): what a run starts with, in one load
   int2* tokens;             // [T]: the sequence's first block and the token's number in it; -1: no sequence's
@@ -428,8 +429,8 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
                 __builtin_bit_cast(f16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)),
                 __builtin_bit_cast(f16x8_t, u32x4_t{pk[0][0], pk[0][1], pk[KB - 1][0], pk[KB - 1][1]}), o[db], 0, 0, 0);
           } else {
-            o[db] = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, a0),
-                                                          __builtin_bit_cast(f16x4_t, u32x2_t{pk[0][0], pk[0][1]}), o[db], 0, 0, 0);
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x16f16(
+                __builtin_bit_cast(f16x4_t, a0), __builtin_bit_cast(f16x4_t, u32x2_t{pk[0][0], pk[0][1]}), o[db], 0, 0, 0);
           }
         }
         wave_lds_sync();
@@ -599,7 +600,7 @@ __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) voi
       for (int u = 0; u < U; ++u) top = fmaxf(top, r.ml[u].x);  // repeats change no maximum
       // (where no row has a maximum they are added all the same: a NaN in one stays one)
       const float ref = top == -INFINITY ? 0.f : top;
-      const float keep = M == -INFINITY && top > -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M == -INFINITY ? 0.f : M) - ref);
+      const float keep = M > -INFINITY ? __builtin_amdgcn_exp2f(M - ref) : top > -INFINITY ? 0.f : 1.f;
       sum *= keep;
 #pragma unroll
       for (int q = 0; q < 8; ++q) acc[q] *= keep;
@@ -663,8 +664,10 @@ __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) voi
 #pragma unroll
       for (int kc = 0; kc < NKC; ++kc) {
         const bf16x8_t av = __builtin_bit_cast(bf16x8_t, wa[kc]);
-        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[0][rr][32 * kc + 8 * g]), o, 0, 0, 0);
-        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, *reinterpret_cast<const bf16x8_t*>(&o_s[1][rr][32 * kc + 8 * g]), o, 0, 0, 0);
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              av, *reinterpret_cast<const bf16x8_t*>(&o_s[part][rr][32 * kc + 8 * g]), o, 0, 0, 0);
       }
       const int t = t0 + i;
       if (i >= a.spt || t >= a.T || a.tokens[t].x < 0) continue;  // other rows stay as they are
@@ -719,17 +722,17 @@ hipError_t launch_q8_prep(const eg_mla_dims& d, int32_t n, const void* q, const 
 }  // namespace
 
 extern "C" size_t eg_mla_quant_attend_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t n_queries,
-                                                  int32_t max_pages_per_seq) {
+                                                     int32_t max_pages_per_seq) {
   Q8Plan p;
   if (check_q8_dims(dims) != EG_MLA_OK || make_q8_plan(*dims, batch, n_queries, max_pages_per_seq, &p) != EG_MLA_OK) return 0;
   return p.bytes;
 }
 
 extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t batch, int32_t n_queries, const void* q,
-                                          const int32_t* cu_seqlens, const uint8_t* codes, const uint8_t* scales,
-                                          const void* w_uk, const void* w_uv, const int32_t* seq_lens,
-                                          const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
-                                          void* workspace, size_t workspace_bytes, void* out, void* stream_) {
+                                             const int32_t* cu_seqlens, const uint8_t* codes, const uint8_t* scales,
+                                             const void* w_uk, const void* w_uv, const int32_t* seq_lens,
+                                             const int32_t* page_table, int32_t max_pages_per_seq, int64_t num_slots,
+                                             void* workspace, size_t workspace_bytes, void* out, void* stream_) {
   Q8Plan p;
   const eg_mla_status st = validate_q8_attend(dims, batch, n_queries, q, cu_seqlens, codes, scales, w_uk, w_uv, seq_lens,
                                               page_table, max_pages_per_seq, num_slots, workspace, workspace_bytes, out, &p);
@@ -744,7 +747,8 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
                       p.tile, p.runs, p.lead};
   (void)hipGetLastError();
   if (launch_q8_prep(d, n_queries, q, w_uk, qrows, sched, stream) != hipSuccess) return EG_MLA_ERR_HIP;
-  Q8Pages pages{page_table ? page_table : sched.head, page_table != nullptr, d.page_size, static_cast<int32_t>(num_slots / d.page_size), max_pages_per_seq, p.capacity, 0, 31};
+  Q8Pages pages{page_table ? page_table : sched.head, page_table != nullptr, d.page_size,
+                static_cast<int32_t>(num_slots / d.page_size), max_pages_per_seq, p.capacity, 0, 31};
   while ((int64_t{1} << (pages.shift - 31)) < d.page_size) ++pages.shift;  // l = ceil(log2 P): mul = ceil(2^(31+l) / P) < 2^32
   pages.mul = static_cast<uint32_t>(((uint64_t{1} << pages.shift) + d.page_size - 1) / d.page_size);
   const Q8Attend at{qrows, codes, scales, pages, sched.info, sched.rows, sched.start,
@@ -766,7 +770,8 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   while (spt > 1 && static_cast<int64_t>(d.num_heads) * ((n_queries + spt - 1) / spt) < (wide ? 256 : 512)) spt /= 2;
   const Q8Merge mg{at.part_ml, at.part_o, sched.info, sched.rows, sched.tokens, sched.head, static_cast<const uint16_t*>(w_uv),
                    static_cast<uint16_t*>(out), n_queries, d.num_heads, d.latent_dim, d.v_head_dim, p.block_rows, spt};
-  const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt), mblock(64 * (wide ? Q8MergeCfg<64>::WAVES : Q8MergeCfg<16>::WAVES));
+  const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt);
+  const dim3 mblock(64 * (wide ? Q8MergeCfg<64>::WAVES : Q8MergeCfg<16>::WAVES));
   const bool half = p.block_rows == kQ8Rows;
   auto merge = wide ? (half ? q8_merge_kernel<64, true> : q8_merge_kernel<64, false>)
                     : (half ? q8_merge_kernel<16, true> : q8_merge_kernel<16, false>);

@@ -1,14 +1,19 @@
 // Attention over the 8-bit cache for blocks of 128 query rows (gfx950 MFMA).
 // Included by quant_attend.hip.
 //
-// Bound by the matrix cores once a few dozen rows share a key.  A work-group of 4
-// waves holds 128 rows, 32 a wave, in registers, and takes its keys in tiles of
-// 64 (32 from d_c 320 on).  Rows are loaded into registers a tile ahead; the wave that
-// loaded a row turns it into fp16 with its scale (once for 128 rows) and writes it into one of two tile buffers; scores S^T[key][row] on v_mfma_f32_32x32x16 (A: 32 keys from LDS, B: the wave's rows), online softmax per row
-// in the log2 domain with lazy rescale, and values O^T[dim][row] += C~^T P^T with the probabilities as the B
-// operand as they lie in the score accumulators and transposed LDS reads as the A operand: each LDS byte feeds 32 rows.
-// 64 sequences of 512-16384 tokens x 128 heads of d_c 512: about 190 us (0.8 PFLOP/s); 8 chunks of 200-600 tokens x 16
-// heads of d_c 128 over 600-8192: about 150 us (0.9).
+// Bound by the matrix cores, and at d_c up to 128 by the softmax's vector
+// instructions, once a few dozen rows share a key.  A work-group of 4 waves holds
+// 128 rows, 32 a wave, in registers, and takes its keys in tiles of 64 (32 from
+// d_c 320 on).  Rows are loaded into registers a tile ahead (through the caches:
+// blocks of a sequence share them; chunks 202 -> 195 us a call); the wave that loaded
+// a row turns it into fp16 with its scale, once for 128 rows, and writes it into one
+// of two tile buffers; scores S^T[key][row] on v_mfma_f32_32x32x16 (A: 32 keys from LDS,
+// B: the wave's rows), online softmax per row in the log2 domain with lazy rescale,
+// and values O^T[dim][row] += C~^T P^T with the probabilities as the B operand as
+// they lie in the score accumulators and transposed LDS reads as the A operand: each
+// LDS byte feeds 32 rows.
+// 64 sequences of 512-16384 tokens x 128 heads of d_c 512: about 190 us (0.8 PFLOP/s);
+// 8 chunks of 200-600 tokens x 16 heads of d_c 128 over 600-8192: 150-165 us (0.9).
 #pragma once
 
 #include "rows32.h"
@@ -120,7 +125,8 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
       const int off_l = r32 * C::LROW, off_r = C::ROPE + r32 * C::RROW;
       // d_c 512: the compiler has products write accumulation registers, which the values fill, and would move a block of
       // them out and back for each tile; the scores' products are written to ordinary ones by hand, and to two
-      // accumulators in turn (a product does not wait for the one before it)
+      // accumulators in turn (a product does not wait for the one before it).  The compiler does not know them for
+      // products: each is 2 wait states behind any vector instruction that may have written an operand
       constexpr bool HAND = QL > 0;
       constexpr int NS = HAND ? 2 * KB : KB;
       px_f32x16_t s[NS];
@@ -128,7 +134,6 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
       for (int kb = 0; kb < NS; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-      if constexpr (HAND) asm("s_nop 1" : "+v"(s[0]), "+v"(s[1]));  // a vector result feeds no product for 2 wait states
       // chunks of 16 values, the RoPE key's first; operands are read QA chunks ahead of their products
       u32x4_t sa[QA + 1][KB], sq[QA + 1];
       auto read_chunk = [&](int c) __attribute__((always_inline)) {
@@ -150,8 +155,9 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
                            : c < NR              ? __builtin_bit_cast(u32x4_t, qr[c < NR ? c : 0])
                                                  : __builtin_bit_cast(u32x4_t, qv[c < NR ? 0 : c - NR]);
         if constexpr (HAND) {
-          if (c < NR) asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s[c % 2]) : "v"(sa[c % (QA + 1)][0]), "v"(bv));
-          else asm("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s[c % 2]) : "v"(sa[c % (QA + 1)][0]), "v"(bv));
+          const u32x4_t av = sa[c % (QA + 1)][0];
+          if (c < NR) asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s[c % 2]) : "v"(av), "v"(bv));
+          else asm("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s[c % 2]) : "v"(av), "v"(bv));
         } else {
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) {
@@ -292,8 +298,9 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint32_t x = lat[c][2 * half + i];
-            v[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, __int_as_float(sc[c]), false));
-            v[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, __int_as_float(sc[c]), true));
+            const float f = __int_as_float(sc[c]);
+            v[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, f, false));
+            v[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, f, true));
           }
           *reinterpret_cast<u32x4_t*>(to[half]) = v;
         }

@@ -34,7 +34,7 @@ def rotate(x, positions, f, half=False, magnitude=1.0, inverse=False):
 
 
 def norm(x, w):
-    return x if w is None else x / np.sqrt((x * x).mean(-1, keepdims=True) + 1e-6) * w
+    return x if w is None or x.shape[-1] == 0 else x / np.sqrt((x * x).mean(-1, keepdims=True) + 1e-6) * w
 
 
 def row_exponent(c):
