@@ -28,16 +28,13 @@ constexpr int kQ8None = 0x3f800001;
 __device__ __forceinline__ int q8_scale(int byte) { return byte == 255 ? kQ8None : byte << 23; }
 
 template <int DC_>
-struct Q8RowsCfg {
-  static constexpr int DC = DC_, KEYS = DC <= 128 ? 64 : 32, KW = KEYS / 4;  // keys of a tile, of a wave's copies
-  static constexpr int LROW = prefix_latent_row(DC), RROW = 128;             // bytes of a key: latent, RoPE key
-  static constexpr int ROPE = KEYS * LROW, TILE = KEYS * (LROW + RROW);
-  static constexpr int PL = DC / 16;                     // pieces (16 codes) of a key
-  static constexpr int NLI = (KW * PL + 63) / 64, NRI = KW * 8 / 64;
+struct Q8RowsCfg : Q8Tile<DC_> {
+  using T = Q8Tile<DC_>;
+  static constexpr int DC = DC_, KEYS = T::KEYS;
   static constexpr int NC = DC / 16, NR = 4, KB = KEYS / 32, NDB = DC / 32;
   static constexpr int QL = DC == 512 ? 4 : 0;           // query chunks that wait in LDS beside q^R
   static constexpr int Q_LDS = QL ? (NR + QL) * kQ8RowsThreads * 16 : 16;
-  static_assert(2 * TILE + Q_LDS + 4 * KEYS * 8 <= 160 * 1024 && (KEYS & (KEYS - 1)) == 0, "LDS");
+  static_assert(T::SPARE + 16 + Q_LDS + 4 * KEYS * 8 <= 160 * 1024 && (KEYS & (KEYS - 1)) == 0, "LDS");
 };
 
 // The lane's number, formed anew for each i: nothing that follows from it is kept in between (where registers are full it
@@ -55,7 +52,7 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
   constexpr int NC = C::NC, NR = C::NR, KB = C::KB, NDB = C::NDB, KW = C::KW, PL = C::PL, QL = C::QL;
   constexpr bool ACC = DC > 128;  // the accumulators are held in the accumulation registers (see shared_prefix.h)
   constexpr int QA = DC == 512 ? 3 : 2, PA = DC <= 128 ? 2 : 4;  // how far LDS reads run ahead of the products
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * C::TILE + 16];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::SPARE + 16];
   __shared__ __attribute__((aligned(16))) u32x4_t q_s[C::Q_LDS / 16];
   __shared__ int2 list[4][C::KEYS];  // (cache row, scale) of the tokens of four tiles
   const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, h = lane >> 5;
@@ -281,17 +278,16 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
             reinterpret_cast<const u32x4_t*>(a.codes + static_cast<int64_t>(e.x) * row_bytes + (d < 2 * a.DR ? a.DC + d : 0)));
       }
     };
-    // turns them into fp16 in `tb`, in SLOTS short pieces (a piece of codes: place, half, half; one of the RoPE key: place,
+    // turns them into fp16 in the tile at byte `base`, in SLOTS short pieces (a piece of codes: place, half, half; one of the RoPE key: place,
     // value).  Columns past d_c hold values that no query and no output has.
     constexpr int SLOTS = 3 * C::NLI + 2 * C::NRI;
     unsigned char* to[2];
-    auto convert = [&](unsigned char* tb, int ln, int slot) __attribute__((always_inline)) {
+    auto convert = [&](int base, int ln, int slot) __attribute__((always_inline)) {
       if (slot < 3 * C::NLI) {
-        const int c = slot / 3, p = c * 64 + ln, key = min(KW * w + p / PL, KW * w + KW - 1), pc = p % PL;
+        const int c = slot / 3, p = c * 64 + ln;
         if (slot % 3 == 0) {
-          to[0] = tb + key * C::LROW + prefix_latent_byte(key, 2 * pc);
-          to[1] = tb + key * C::LROW + prefix_latent_byte(key, 2 * pc + 1);
-          if (KW * PL % 64 != 0 && p >= KW * PL) to[0] = to[1] = tb + C::TILE;  // (behind the last piece: nowhere)
+          to[0] = lds + q8_latent_store<C>(base, w, p, 0);
+          to[1] = lds + q8_latent_store<C>(base, w, p, 1);
         } else {
           const int half = slot % 3 - 1;
           u32x4_t v;
@@ -307,7 +303,7 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
       } else {
         const int c = (slot - 3 * C::NLI) / 2, p = c * 64 + ln, key = KW * w + p / 8, pc = p % 8;
         if ((slot - 3 * C::NLI) % 2 == 0) {
-          to[0] = tb + C::ROPE + key * C::RROW + prefix_rope_byte(key, pc);
+          to[0] = lds + base + C::ROPE + key * C::RROW + prefix_rope_byte(key, pc);
         } else {
           u32x4_t v = rop[c];
           if (8 * pc >= a.DR) v = u32x4_t{0u, 0u, 0u, 0u};
@@ -316,9 +312,9 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
         }
       }
     };
-    auto convert_all = [&](unsigned char* tb) __attribute__((always_inline)) {
+    auto convert_all = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < SLOTS; ++i) convert(tb, threadIdx.x & 63, i);
+      for (int i = 0; i < SLOTS; ++i) convert(base, threadIdx.x & 63, i);
     };
 
     // a tile's tokens (those past the last repeat it and are masked) are listed a tile ahead of their rows' loads: page,
@@ -337,10 +333,11 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
     int page_next = a.cache.page(b, j_next);
     __syncthreads();
     issue(0);
-    convert_all(lds);
+    convert_all(0);
     issue(1);
-    // tile i of the piece from `tb`; the next one's rows go to `nb` (last read in step i - 1), the one's after are loaded
-    auto step = [&](int i, const unsigned char* tb, unsigned char* nb) __attribute__((always_inline)) {
+    // tile i of the piece from `tb`; the next one's rows go to byte `next` on (last read in step i - 1), the one's after
+    // are loaded
+    auto step = [&](int i, const unsigned char* tb, int next) __attribute__((always_inline)) {
       __syncthreads();
       const int ln = lane_anew(i);
       if (w == 0 && ln < C::KEYS) list[(i + 3) & 3][ln] = make_int2(slot_next, q8_scale(scale_next));
@@ -351,12 +348,12 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
       attend(tb, i, [&](int product, int products) __attribute__((always_inline)) {
 #pragma unroll
         for (int slot = 0; slot < SLOTS; ++slot)
-          if (slot * products / SLOTS == product) convert(nb, ln, slot);
+          if (slot * products / SLOTS == product) convert(next, ln, slot);
       });
       issue(i + 2);
     };
     const int n = (j1 - j0 + C::KEYS - 1) / C::KEYS;
-    for (int i = 0; i < n; ++i) step(i, lds + (i & 1) * C::TILE, lds + (~i & 1) * C::TILE);
+    for (int i = 0; i < n; ++i) step(i, lds + (i & 1) * C::TILE, (~i & 1) * C::TILE);
     __syncthreads();  // the lists and tiles have been read
 
     // lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row that met no token (or whose scores

@@ -1,19 +1,11 @@
 // What the attention kernels of 32 query rows a wave share: the layout of a key
-// tile in LDS, and lane operations on the accumulators of v_mfma_f32_32x32x16.
+// tile in LDS (key_tile.h), and lane operations on the accumulators of v_mfma_f32_32x32x16.
 #pragma once
 
 #include "device_common.h"
+#include "key_tile.h"
 
 namespace egmla {
-
-// Byte of piece p (16 bytes: dims 8p ..) of a key's latent row, and of its
-// RoPE row: the low bits of the piece are swizzled by the key so that the 16
-// lanes of a 16-byte read cycle (keys) and the 32 lanes of a transposed 8-byte
-// read cycle hit distinct banks.
-__host__ __device__ __forceinline__ int prefix_latent_byte(int key, int p) {
-  return 256 * (p >> 4) + 16 * ((p & 15) ^ (((key & 3) << 2) | ((key >> 2) & 3)));
-}
-__host__ __device__ __forceinline__ int prefix_rope_byte(int key, int p) { return 16 * (p ^ ((key >> 1) & 7)); }
 
 typedef __attribute__((ext_vector_type(16))) float px_f32x16_t;
 
