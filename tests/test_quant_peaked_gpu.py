@@ -58,7 +58,11 @@ def check(P, seed):
 
 # d_c: heads, d_h, d_v, d_c, d_r; sequences, new tokens of each: blocks of 128 query rows (48 rows a sequence and more),
 # four tiles a run and more (tiles of 64 tokens and 512 runs up to d_c 128, of 32 and 256 runs above)
-ROWS_128 = {144: ((16, 64, 136, 144, 64), 8, 8), 320: ((16, 128, 128, 320, 64), 8, 8)}
+ROWS_128 = {64: ((12, 64, 64, 64, 64), 24, 11), 128: ((16, 128, 128, 128, 64), 24, 8), 144: ((16, 64, 136, 144, 64), 8, 8),
+            320: ((16, 128, 128, 320, 64), 8, 8), 512: ((16, 128, 128, 512, 64), 8, 8)}
+# blocks of 16 rows (fewer rows a sequence), three tiles a run and more (of 128 tokens up to d_c 128, of 64 above; 512 runs)
+ROWS_16 = {64: ((12, 64, 64, 64, 64), 40, 2), 128: ((16, 128, 128, 128, 64), 40, 1), 144: ((16, 64, 136, 144, 64), 24, 2),
+           320: ((16, 128, 128, 320, 64), 24, 1), 512: ((16, 128, 128, 512, 64), 24, 1)}
 
 
 @pytest.mark.parametrize("dc", ROWS_128)
@@ -67,3 +71,11 @@ def test_blocks_of_128_rows(gpu, dc, peaks):
     shape, b, new = ROWS_128[dc]
     lens = [4096 - 37 * i % 200 for i in range(b)]
     check(Peaked(dc, *shape, [new] * b, lens, peaks, 32), dc)
+
+
+@pytest.mark.parametrize("dc", ROWS_16)
+@pytest.mark.parametrize("peaks", ["rope", "latent"])
+def test_blocks_of_16_rows(gpu, dc, peaks):
+    shape, b, new = ROWS_16[dc]
+    lens = [4096 - 37 * i % 200 for i in range(b)]
+    check(Peaked(dc, *shape, [new] * b, lens, peaks, 4), dc)
