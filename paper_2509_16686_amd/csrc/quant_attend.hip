@@ -192,7 +192,8 @@ __global__ __launch_bounds__(256) void q8_prep_any_kernel(Q8Prep p, Q8Sched a) {
 // end.  The RoPE key stays bf16 and exact; the absorbed query and the
 // probabilities are rounded once to fp16; sums, maxima and products are fp32.  A
 // row that stands for NaN has zeros for values and a NaN RoPE key, so that it
-// reaches the rows that attend to it through their score, and no other.  Bound
+// reaches the rows that attend to it through their score, and no other; values
+// that are not finite: q8_only_finite.  Bound
 // by HBM for long calls: 256 sequences of 250-8192 tokens, 16 heads of d_c 128,
 // 57 us, 4.9 TB/s.
 // ---------------------------------------------------------------------------
@@ -264,6 +265,22 @@ __device__ __forceinline__ void q8_to_f16(u32x4_t w, float s, u32x4_t& lo, u32x4
   }
 }
 
+// Values that fp16 does not hold (past 63488, which round to codes past 240 2^8, and NaN codes) are infinities or NaN in a
+// tile.  Rows that attend to such a token become NaN, as their scores and values do.  One that does not has it in its value
+// products all the same where other rows of the block attend to it, with a probability of 0, which an infinity or NaN times
+// is none: in the tiles where some row's tokens end such values become zeros and the token's RoPE key a NaN, which reaches
+// through their scores the rows that attend to it, and no other.
+constexpr u32x4_t kQ8NanKey = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+__device__ __forceinline__ void q8_only_finite(u32x4_t* values, u32x4_t* key) {  // (8 fp16 values; a piece of their RoPE key)
+  const u32x4_t v = *values;
+  uint32_t full = 0;  // exponents of all ones carry
+#pragma unroll
+  for (int i = 0; i < 4; ++i) full |= (v[i] & 0x7fff7fffu) + 0x04000400u;
+  if ((full & 0x80008000u) == 0) return;
+  *values = u32x4_t{0u, 0u, 0u, 0u};
+  *key = kQ8NanKey;
+}
+
 // Eight values of a query row's part of n, zero behind its end.
 __device__ __forceinline__ u32x4_t q8_query(const uint16_t* part, int d, int n) {
   return d < n ? *reinterpret_cast<const u32x4_t*>(part + d) : u32x4_t{0u, 0u, 0u, 0u};
@@ -301,6 +318,7 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
     const int b = info.x, row0 = info.y, nrows = info.z, first = rw.y, len = rw.z;
     const int most = min(max(first + (row0 + nrows - 1) / a.H + 1, 0), len);
     const int j0 = (at - info.w) * C::TILE, j1 = min((min(end, next) - info.w) * C::TILE, most);
+    const int all = min(first + row0 / a.H + 1, len);  // tokens that every row attends to
     at = min(end, next);
 
     // this lane's query row (rows past the last repeat it and are not stored) and the tokens that it attends to
@@ -372,6 +390,14 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
           slot = slot_of(u + 2 * NW);
         }
         wave_lds_sync();
+        if (min(j0 + (u + 1) * U, j1) > all) {
+#pragma unroll 1
+          for (int p = lane; p < U * DCP / 8; p += 64) {
+            uint16_t* row = tile + p / (DCP / 8) * TS;
+            q8_only_finite(reinterpret_cast<u32x4_t*>(row + 8 * (p % (DCP / 8))), reinterpret_cast<u32x4_t*>(row + DCP));
+          }
+          wave_lds_sync();
+        }
         // S^T[token 16 kb + 4g + i][row r16]
         const int left = lim - (j0 + u * U);  // tokens of the unit that the row attends to
         float x[KB][4];

@@ -78,6 +78,7 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
     const int b = info.x, row0 = info.y, nrows = info.z, first = rw.y, len = rw.z;
     const int most = min(max(first + (row0 + nrows - 1) / a.H + 1, 0), len);
     const int j0 = (at - info.w) * C::KEYS, j1 = min((min(end, next) - info.w) * C::KEYS, most);
+    const int all = min(first + row0 / a.H + 1, len);  // tokens that every row attends to
     at = min(end, next);
 
     // this lane's query row (rows past the last repeat it and are not stored) and the tokens that it attends to
@@ -335,10 +336,21 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
     issue(0);
     convert_all(0);
     issue(1);
+    // (values that are not finite, of tokens that some row does not attend to; any place of a key's RoPE row serves)
+    auto only_finite = [&](unsigned char* tb) __attribute__((always_inline)) {
+#pragma unroll 1
+      for (int p = threadIdx.x; p < C::KEYS * (DC / 8); p += kQ8RowsThreads) {
+        const int key = p / (DC / 8);
+        q8_only_finite(reinterpret_cast<u32x4_t*>(tb + key * C::LROW + prefix_latent_byte(key, p % (DC / 8))),
+                       reinterpret_cast<u32x4_t*>(tb + C::ROPE + key * C::RROW));
+      }
+      __syncthreads();
+    };
     // tile i of the piece from `tb`; the next one's rows go to byte `next` on (last read in step i - 1), the one's after
     // are loaded
-    auto step = [&](int i, const unsigned char* tb, int next) __attribute__((always_inline)) {
+    auto step = [&](int i, unsigned char* tb, int next) __attribute__((always_inline)) {
       __syncthreads();
+      if (min(j0 + (i + 1) * C::KEYS, j1) > all) only_finite(tb);
       const int ln = lane_anew(i);
       if (w == 0 && ln < C::KEYS) list[(i + 3) & 3][ln] = make_int2(slot_next, q8_scale(scale_next));
       slot_next = a.cache.row(b, j_next, page_next);
