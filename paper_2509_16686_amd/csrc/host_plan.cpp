@@ -1016,8 +1016,8 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
     at += align_up(static_cast<size_t>(bytes));
     return here;
   };
-  // partial rows: bounds that grow with the batch and the queries, of either size of block (fp32 rows of blocks of 16,
-  // fp16 of 128), so that a workspace serves every smaller call
+  // partial rows: bounds that grow with the batch and the queries, of either size of block, so that a workspace serves
+  // every smaller call
   const int64_t small = 16 * (kQ8MaxRuns + rows / 16 + batch);
   const int64_t large = 128 * ((d.latent_dim > 128 ? 256 : kQ8MaxRuns) + rows / 128 + batch);
   p.off_q = take(rows * (d.latent_dim + d.rope_dim) * 2);
@@ -1028,7 +1028,7 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   p.off_tokens = take(n_queries * int64_t{8});
   p.off_head = take(16);
   p.off_ml = take(std::max(small, large) * 8);
-  p.off_o = take(std::max(4 * small, 2 * large) * d.latent_dim);
+  p.off_o = take(std::max(small, large) * 4 * d.latent_dim);
   p.bytes = at;
   *out = p;
   return EG_MLA_OK;

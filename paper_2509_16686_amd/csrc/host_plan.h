@@ -256,7 +256,7 @@ struct Q8Plan {
   size_t off_tokens = 0;  // int2 [T]
   size_t off_head = 0;    // int32 [4]
   size_t off_ml = 0;      // fp32 [runs + blocks][block_rows][2]
-  size_t off_o = 0;       // [runs + blocks][block_rows][d_c]: fp32 sums, or (128 rows) fp16 O / l
+  size_t off_o = 0;       // fp32 [runs + blocks][block_rows][d_c]
   size_t bytes = 0;
 };
 eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_queries, int32_t max_pages_per_seq, Q8Plan* out);

@@ -224,7 +224,7 @@ struct Q8Attend {
   const int4* rows;
   const int4* start;
   float* part_ml;  // [piece][block rows][2]
-  void* part_o;    // [piece][block rows][DC]: fp32 sums O, or (blocks of 128 rows) O / l in fp16
+  float* part_o;   // [piece][block rows][DC]: sums O
   int32_t H, DC, DR;
   float scale_log2;
 };
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(kQ8AttendThreads, DCP <= 320 ? 2 : 1) void q8_atten
 #pragma unroll
         for (int v = 1; v < NW; ++v) sum += obuf[(v * (NB / 2) + db) * 64 + lane];
         const int d = (half * (NB / 2) + db) * 16 + 4 * g;
-        if (r16 < nrows && d < a.DC) __builtin_nontemporal_store(sum, reinterpret_cast<f32x4_t*>(static_cast<float*>(a.part_o) + prow * a.DC + d));
+        if (r16 < nrows && d < a.DC) __builtin_nontemporal_store(sum, reinterpret_cast<f32x4_t*>(a.part_o + prow * a.DC + d));
       }
     }
     if (w == 0 && g == 0 && r16 < nrows) {
@@ -516,7 +516,7 @@ namespace egmla {
 // ---------------------------------------------------------------------------
 struct Q8Merge {
   const float* part_ml;
-  const void* part_o;
+  const void* part_o;  // fp32
   const int4* info;
   const int4* rows;
   const int2* tokens;
@@ -534,7 +534,7 @@ struct Q8MergeCfg {
   static_assert(TOKENS % WORKERS == 0, "whole rounds");
 };
 
-template <int LPR, bool HALF>
+template <int LPR>
 __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) void q8_merge_kernel(Q8Merge a) {
   using C = Q8MergeCfg<LPR>;
   constexpr int DCP = 8 * LPR, NKC = DCP / 32, OS = DCP + 8, GPW = 64 / LPR, TPW = C::TPW, U = LPR == 64 ? 2 : 4;
@@ -575,7 +575,7 @@ __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) voi
   // rows i, i + wps of a token (repeats of the last past its end)
   struct Rows {
     float2 ml[U];
-    u32x4_t x[U][HALF ? 1 : 2];
+    u32x4_t x[U][2];
   };
   auto load = [&](Rows& r, int64_t first, int i, int n) {
 #pragma unroll
@@ -583,11 +583,10 @@ __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) voi
       const int64_t row = first + static_cast<int64_t>(min(i + u * wps, n - 1)) * a.block_rows;
       r.ml[u] = *reinterpret_cast<const float2*>(a.part_ml + 2 * row);
 #pragma unroll
-      for (int q = 0; q < (HALF ? 1 : 2); ++q) {
+      for (int q = 0; q < 2; ++q) {
         r.x[u][q] = u32x4_t{0u, 0u, 0u, 0u};
         if (col < a.DC)
-          r.x[u][q] = *reinterpret_cast<const u32x4_t*>(static_cast<const unsigned char*>(a.part_o) +
-                                                        (row * a.DC + col) * (HALF ? 2 : 4) + 16 * q);
+          r.x[u][q] = *reinterpret_cast<const u32x4_t*>(static_cast<const unsigned char*>(a.part_o) + (row * a.DC + col) * 4 + 16 * q);
       }
     }
   };
@@ -635,15 +634,8 @@ __global__ __launch_bounds__(Q8MergeCfg<LPR>::WAVES * 64, LPR == 64 ? 2 : 4) voi
         if (i + u * wps >= n[j]) continue;
         const float x = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r.ml[u].x - ref);
         sum = fmaf(x, r.ml[u].y, sum);
-        if constexpr (HALF) {
-          const f16x8_t v = __builtin_bit_cast(f16x8_t, r.x[u][0]);
-          const float y = x * r.ml[u].y;
 #pragma unroll
-          for (int q = 0; q < 8; ++q) acc[q] = fmaf(y, static_cast<float>(v[q]), acc[q]);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q) acc[q] = fmaf(x, __uint_as_float(r.x[u][q / 4][q % 4]), acc[q]);
-        }
+        for (int q = 0; q < 8; ++q) acc[q] = fmaf(x, __uint_as_float(r.x[u][q / 4][q % 4]), acc[q]);
       }
       M = top;
     }
@@ -778,7 +770,7 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
   while ((int64_t{1} << (pages.shift - 31)) < d.page_size) ++pages.shift;  // l = ceil(log2 P): mul = ceil(2^(31+l) / P) < 2^32
   pages.mul = static_cast<uint32_t>(((uint64_t{1} << pages.shift) + d.page_size - 1) / d.page_size);
   const Q8Attend at{qrows, codes, scales, pages, sched.info, sched.rows, sched.start,
-                    reinterpret_cast<float*>(ws + p.off_ml), ws + p.off_o,
+                    reinterpret_cast<float*>(ws + p.off_ml), reinterpret_cast<float*>(ws + p.off_o),
                     d.num_heads, d.latent_dim, d.rope_dim, softmax_scale(d) * 1.4426950408889634f};
   const dim3 grid(p.runs), block(kQ8AttendThreads);
   if (p.block_rows == kQ8Rows) {
@@ -798,9 +790,7 @@ extern "C" eg_mla_status eg_mla_quant_attend(const eg_mla_dims* dims, int32_t ba
                    static_cast<uint16_t*>(out), n_queries, d.num_heads, d.latent_dim, d.v_head_dim, p.block_rows, spt};
   const dim3 mgrid(d.num_heads, (n_queries + spt - 1) / spt);
   const dim3 mblock(64 * (wide ? Q8MergeCfg<64>::WAVES : Q8MergeCfg<16>::WAVES));
-  const bool half = p.block_rows == kQ8Rows;
-  auto merge = wide ? (half ? q8_merge_kernel<64, true> : q8_merge_kernel<64, false>)
-                    : (half ? q8_merge_kernel<16, true> : q8_merge_kernel<16, false>);
+  auto merge = wide ? q8_merge_kernel<64> : q8_merge_kernel<16>;
   hipLaunchKernelGGL(merge, mgrid, mblock, 0, stream, mg);
   return hipGetLastError() == hipSuccess ? EG_MLA_OK : EG_MLA_ERR_HIP;
 }

@@ -370,22 +370,22 @@ __global__ __launch_bounds__(kQ8RowsThreads, DC <= 128 ? 2 : 1) void q8_rows_ker
 
     // lane holds dims 32 db + 16 j + 8 h + 0..7 of its row in o[db][8 j + 0..7]; a row that met no token (or whose scores
     // all overflowed to -inf) weighs nothing; a NaN among them stays one
-    const float l = half_sum(l_run), inv = l == 0.f ? 0.f : 1.0f / l;
+    const float l = half_sum(l_run);
     const int ln = lane_anew(n), he = ln >> 5, re = 32 * w + (ln & 31);
     if (re < nrows) {
       const int64_t prow = (static_cast<int64_t>(run) + k) * kQ8Rows + re;
       if (he == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * prow) = make_float2(l == 0.f ? -INFINITY : m_run, l);
-      uint16_t* orow = static_cast<uint16_t*>(a.part_o) + prow * a.DC + 8 * he;
+      float* orow = a.part_o + prow * a.DC + 8 * he;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          if (32 * db + 16 * j < a.DC)
-            *reinterpret_cast<u32x4_t*>(orow + 32 * db + 16 * j) =
-                u32x4_t{pack_f16x2(o[db][8 * j] * inv, o[db][8 * j + 1] * inv),
-                        pack_f16x2(o[db][8 * j + 2] * inv, o[db][8 * j + 3] * inv),
-                        pack_f16x2(o[db][8 * j + 4] * inv, o[db][8 * j + 5] * inv),
-                        pack_f16x2(o[db][8 * j + 6] * inv, o[db][8 * j + 7] * inv)};
+          if (32 * db + 16 * j < a.DC) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              *reinterpret_cast<f32x4_t*>(orow + 32 * db + 16 * j + 4 * q) =
+                  f32x4_t{o[db][8 * j + 4 * q], o[db][8 * j + 4 * q + 1], o[db][8 * j + 4 * q + 2], o[db][8 * j + 4 * q + 3]};
+          }
     }
   }
 #endif

@@ -9,7 +9,6 @@ output is one latent value of the merged row.  Bound of that output, o = sum p c
   scores: sums of d_c + d_r fp32 products, each addition off by at most 2^-24 of sum |q k|, the scale's product and the
     exponential by 2^-21 together; a weight moves by that, relatively, and so does their sum:  2 e sum p |c~|
   sums over keys, the merge and the merged row's two bf16 halves: 2^-15 sum p |c~|
-  a partial row of a block of 128 query rows rounds to fp16 once: 2^-11 sum p |c~|, and no less than 2^-25
   the output: half a step of bf16, 2^-8 |o|."""
 import math
 
@@ -102,7 +101,7 @@ class Peaked:
             if change is not None:
                 lat, p = change(b, lat.copy(), p.copy())
             o, size = p @ lat, p @ np.abs(lat)
-            limit = (2.0 ** -10 + 2 * e + 2.0 ** -15) * size + 2.0 ** -25 * (1 + np.abs(lat).sum(0)[None] / l) + 2.0 ** -8 * np.abs(o)
+            limit = (2.0 ** -11 + 2 * e + 2.0 ** -15) * size + 2.0 ** -25 * np.abs(lat).sum(0)[None] / l + 2.0 ** -8 * np.abs(o)
             pick = np.tile(self.pick_v, (n, 1))
             out.append(np.take_along_axis(o, pick, 1).reshape(n, self.h, self.dv))
             bound.append(np.take_along_axis(limit, pick, 1).reshape(n, self.h, self.dv))
