@@ -25,6 +25,7 @@
 #include "device_common.h"
 #include "eg_mla.h"
 #include "host_plan.h"
+#include "quant_blocks.h"
 
 namespace egmla {
 
@@ -88,19 +89,18 @@ __device__ __forceinline__ void q8_schedule(const Q8Sched& a) {
   auto first_token = [&](int b) { return a.cu ? clamp_len(a.cu[b], a.T) : min(b, a.T); };
   for (int t = tid; t < a.T; t += THREADS) a.tokens[t] = make_int2(-1, 0);
   for (int g = tid; g < a.runs; g += THREADS) a.start[3 * g] = make_int4(0, 0, 0, 0);  // no places
+  const int most = q8_most_blocks(a.T, a.H, a.block_rows, a.B);
   int total = 0, blocks = 0;
+  static_assert(THREADS <= 256, "sequences of a step of the count");
   for (int b0 = 0; b0 < a.B; b0 += THREADS) {
     const int b = b0 + tid;
-    const int64_t r = b < a.B ? static_cast<int64_t>(max(0, first_token(b + 1) - first_token(b))) * a.H : 0;
-    const int at = group_scan<THREADS>(static_cast<int>((r + a.block_rows - 1) / a.block_rows), tmp, total);
-    if (b < a.B) first_s[b] = blocks + at;
-    blocks += total;
+    const int mine = b < a.B ? q8_sequence_blocks(first_token(b), first_token(b + 1), a.H, a.block_rows) : 0;
+    const int at = group_scan<THREADS>(mine, tmp, total);
+    if (b < a.B) first_s[b] = q8_blocks_behind(blocks, at, most);
+    blocks = q8_blocks_behind(blocks, total, most);
   }
   if (tid == 0) first_s[a.B] = blocks;
   __syncthreads();
-  // (offsets that do not rise, which the call does not allow, could make more blocks than there is room for)
-  const int most = static_cast<int>(static_cast<int64_t>(a.T) * a.H / a.block_rows) + a.B;
-  blocks = min(blocks, most);
   int tiles = 0;
   for (int k0 = 0; k0 < blocks; k0 += THREADS) {
     const int k = k0 + tid;
