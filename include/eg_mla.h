@@ -635,7 +635,8 @@ eg_mla_status eg_mla_rope_frequencies(int32_t rope_dim, float theta, float facto
  *   positions [n_tokens] int32
  * Any sizes and alignment of whole elements (fastest where offset, half of the
  * part, the rest and the strides are multiples of 16 bytes).  rope_dim is even, at
- * most 640 (EG_MLA_ERR_UNSUPPORTED).  n_tokens == 0 is a no-op.
+ * most 640, and num_heads at most 2^30 (EG_MLA_ERR_UNSUPPORTED).  n_tokens == 0 is a
+ * no-op.
  * ------------------------------------------------------------------------- */
 eg_mla_status eg_mla_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t n_tokens, int32_t num_heads,
                                int32_t head_dim, int32_t rope_offset, int32_t rope_dim, const void* x,

@@ -890,6 +890,7 @@ eg_mla_status check_rope(const eg_mla_rope* r, int32_t rope_dim) {
 }
 
 constexpr int kMaxRopeDim = 640;
+constexpr int kMaxRowHeads = 1 << 30;  // (a head's number and a work-group's step of heads in 32 bits)
 constexpr int64_t kMaxRowStride = int64_t{1} << 32;
 constexpr int kQ8MaxLatent = 512, kQ8MaxRopeDim = 64;
 constexpr int64_t kQ8MaxTiles = int64_t{1} << 23;  // tiles of 16 queries, a head and 64 latent values (work-groups of the absorption)
@@ -917,6 +918,7 @@ eg_mla_status validate_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t
   if (n_tokens < 0 || num_heads < 1 || head_dim < 1 || rope_offset < 0 || rope_dim < 0 || rope_dim % 2 != 0 ||
       rope_dim > head_dim || rope_offset > head_dim - rope_dim)
     return EG_MLA_ERR_INVALID_ARG;
+  if (num_heads > kMaxRowHeads) return EG_MLA_ERR_UNSUPPORTED;
   const eg_mla_status st = rope_dim <= kMaxRopeDim ? check_rope(rope, rope_dim) : EG_MLA_ERR_UNSUPPORTED;
   if (st != EG_MLA_OK) return st;
   if (n_tokens == 0) return EG_MLA_OK;
