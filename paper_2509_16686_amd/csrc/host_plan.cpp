@@ -898,12 +898,14 @@ constexpr int kQ8MaxQueries = 1 << 19;
 // Blocks of 128 query rows instead of 16: from so many rows a sequence on average, and so many products (rows x capacity
 // x (2 d_c + d_r)), below which their longer start is the time.  us a call with blocks of 16 / 128, tokens of each
 // sequence in brackets:
-//   16 heads d_c 128, 32 x 4096:  [2] 28.7 / 35.2  [3] 38.1 / 37.0  [4] 36.3 / 36.4  [6] 48.9 / 40.6  [16] 83.6 / 53.5
-//   16 heads d_c 128, 8 x 500:    [4] 21.6 / 23.3  [16] 21.6 / 26.1;  4 x 32768:  [4] 38.7 / 41.8  [8] 53.7 / 48.4
-//   12 heads d_c 64, 32 x 4096:   [2] 25.3 / 28.4  [3] 32.0 / 28.0  [16] 62.5 / 38.3
-//   16 heads d_c 320, 32 x 4096:  [1] 34.2 / 49.4  [2] 44.9 / 52.8  [3] 67.5 / 61.7  [16] 161 / 93.7
-//   128 heads d_c 512, 8 x 4096:  [1] 80.4 / 55.4  [16] 761 / 213;  1 x 30000:  [1] 95.1 / 69.0
-//   5 heads d_c 48, 16 x 3000:    [16] 28.5 / 29.6
+//   16 heads d_c 128, 32 x 4096:  [2] 29.2 / 35.7  [3] 39.3 / 37.0  [4] 37.7 / 37.8  [6] 50.9 / 41.2  [16] 87.1 / 55.0
+//   16 heads d_c 128, 8 x 500:    [4] 21.3 / 24.7  [16] 22.3 / 29.0;  4 x 32768:  [4] 38.4 / 38.8  [8] 56.3 / 44.2
+//   12 heads d_c 64, 32 x 4096:   [2] 25.9 / 29.1  [3] 33.6 / 29.2  [4] 33.9 / 29.6  [16] 64.3 / 40.4
+//   16 heads d_c 320, 32 x 4096:  [1] 35.4 / 50.8  [2] 45.1 / 54.3  [3] 73.2 / 64.4  [4] 66.4 / 60.0  [16] 182 / 98.5
+//   128 heads d_c 512, 8 x 4096:  [1] 87.1 / 57.7  [16] 871 / 230;  1 x 30000:  [1] 98.0 / 55.6
+//   5 heads d_c 48, 16 x 3000:    [16] 23.3 / 24.5
+// (The capacity stands for the lengths, which only the device knows: a table for the longest context takes blocks of 128
+// for short ones too.)
 constexpr int kQ8ManyRows = 48;
 constexpr int64_t kQ8ManyProducts = 600000000;
 constexpr int kQ8MaxRuns = 512;
@@ -1007,8 +1009,8 @@ eg_mla_status make_q8_plan(const eg_mla_dims& d, int32_t batch, int32_t n_querie
   p.tile = many ? (d.latent_dim <= 128 ? 64 : 32) : d.latent_dim <= 128 ? 128 : 64;
   // one work-group a compute unit where registers or LDS leave room for one, else two
   p.runs = many && d.latent_dim > 128 ? 256 : kQ8MaxRuns;
-  // (us a call at lead 0, 4, 8, 12: 64 x 512-16384 x 128 heads 226, 214, 216, 216; chunks of 200-600 tokens x 16 heads
-  // 245, 201, 205, 209; blocks of 16, 256 x 250-8192: 71.4, 71.2, 71.3, 76.2)
+  // (us a call at lead 0, 4, 8, 12: 64 x 512-16384 x 128 heads 238, 226, 216, 219; chunks of 200-600 tokens x 16 heads
+  // 270, 203, 210, 216; blocks of 16, 256 x 250-8192: 70.7, 69.7, 71.7, 75.8)
   p.lead = many ? 4 : 0;
   p.blocks = rows / p.block_rows + batch;
   if (held_product(p.blocks, cap / p.tile + 1 + p.lead) >= (int64_t{1} << 31)) return EG_MLA_ERR_UNSUPPORTED;

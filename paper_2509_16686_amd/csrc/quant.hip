@@ -47,7 +47,7 @@ __device__ __forceinline__ void turn_of(uint64_t freq, int32_t position, float& 
 // heads; a thread takes two pieces of VEC values of a head's row, those of VEC
 // pairs or two to copy, for every hpar-th of them, so that its sines are formed
 // once, and four heads' loads are in flight (8192 tokens x 128 heads of 192 bf16
-// values: 152 us, 5.3 TB/s in and out, the rate of a copy; 208 us with one piece to
+// values: 152 us a call, 5.3 TB/s in and out, the rate of a copy; 208 us with one piece to
 // copy a thread, two heads in flight and waves that took both branches).
 // ---------------------------------------------------------------------------
 struct RopeArgs {

@@ -511,8 +511,9 @@ namespace egmla {
 // the merged row o / l goes to LDS as bf16 hi + lo, the B operands of out^T[v][token] =
 // W_UV[h] o^T on v_mfma_f32_16x16x32_bf16, so that the up-projection adds only
 // W_UV's own rounding.  Bound by its chain of loads (token, block, rows), behind
-// which W_UV's rows arrive: 7.5-8.8 us for 32 and 256 tokens of 16 heads, 22 for 64
-// of 128 heads (W_UV before the rows, 16 tokens a work-group: 37).
+// which W_UV's rows arrive: 8.6 us for 32 and 256 tokens of 16 heads, 28.5 for 64 of
+// 128 heads in blocks of 128 rows (half as many bytes a row, O / l in fp16: 23.8;
+// W_UV before the rows, 16 tokens a work-group, also in fp16: 37).
 // ---------------------------------------------------------------------------
 struct Q8Merge {
   const float* part_ml;

@@ -3,8 +3,8 @@
 //
 // Bound by the matrix cores, and at d_c up to 128 by the softmax's vector
 // instructions, once a few dozen rows share a key.  A work-group of 4 waves holds
-// 128 rows, 32 a wave, in registers, and takes its keys in tiles of 64 (32 from
-// d_c 320 on).  Rows are loaded into registers a tile ahead (through the caches:
+// 128 rows, 32 a wave, in registers, and takes its keys in tiles of 64 (32 above
+// d_c 128).  Rows are loaded into registers a tile ahead (through the caches:
 // blocks of a sequence share them; chunks 202 -> 195 us a call); the wave that loaded
 // a row turns it into fp16 with its scale, once for 128 rows, and writes it into one
 // of two tile buffers; scores S^T[key][row] on v_mfma_f32_32x32x16 (A: 32 keys from LDS,
@@ -12,8 +12,9 @@
 // and values O^T[dim][row] += C~^T P^T with the probabilities as the B operand as
 // they lie in the score accumulators and transposed LDS reads as the A operand: each
 // LDS byte feeds 32 rows.
-// 64 sequences of 512-16384 tokens x 128 heads of d_c 512: about 190 us (0.8 PFLOP/s);
-// 8 chunks of 200-600 tokens x 16 heads of d_c 128 over 600-8192: 150-165 us (0.9).
+// Kernel times under the profiler, median and best of 20: 64 sequences of 512-16384 tokens x
+// 128 heads of d_c 512 247 and 208 us (0.62 and 0.73 PFLOP/s); 8 chunks of 200-600 tokens x 16
+// heads of d_c 128 over 600-8192 193 and 171 us (0.72 and 0.82).
 #pragma once
 
 #include "rows32.h"
