@@ -701,9 +701,9 @@ eg_mla_status eg_mla_rope_rows(const eg_mla_rope* rope, int32_t dtype, int32_t n
  *      ordered.  The size query returns 0 where the call would refuse.
  * The absorbed query, c~ and the probabilities enter the matrix products in fp16
  * (the query's magnitudes below 65504), q^R and k^R in bf16; sums are fp32.  Codes
- * times their scale are exact in fp16 up to 61440 (values of c~ up to 63488 when
+ * times their scale are exact in fp16 up to 61440 (values of c~ below 63488 when
  * written) and in multiples of 2^-24 (every code where e >= -15; smaller ones round
- * to these).  A token with a larger value, or with codes that are NaN (0x7F, 0xFF,
+ * to these).  Scores below -1e30 may weigh nothing.  A token with a larger value, or with codes that are NaN (0x7F, 0xFF,
  * which no call writes), makes the rows that attend to it NaN.  Which tokens a row
  * does not attend to does not matter to it, whatever they hold.
  *

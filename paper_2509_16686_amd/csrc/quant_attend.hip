@@ -265,7 +265,7 @@ __device__ __forceinline__ void q8_to_f16(u32x4_t w, float s, u32x4_t& lo, u32x4
   }
 }
 
-// Values that fp16 does not hold (past 63488, which round to codes past 240 2^8, and NaN codes) are infinities or NaN in a
+// Values that fp16 does not hold (from 63488 on, which round to codes past 240 2^8, and NaN codes) are infinities or NaN in a
 // tile.  Rows that attend to such a token become NaN, as their scores and values do.  One that does not has it in its value
 // products all the same where other rows of the block attend to it, with a probability of 0, which an infinity or NaN times
 // is none: in the tiles where some row's tokens end such values become zeros and the token's RoPE key a NaN, which reaches

@@ -13,11 +13,11 @@ pytestmark = pytest.mark.gpu
 PAGE = 64
 
 
-def stage(P, seed):
-    """(dims, arguments of quant_attend) of the case, its rows in random pages."""
+def stage(P, seed, width=0):
+    """(dims, arguments of quant_attend) of the case, its rows in random pages, in a table of at least `width` of them."""
     r = np.random.default_rng(seed)
     pages = [-(-n // PAGE) for n in P.lens]
-    width, order = max(pages), r.permutation(sum(pages) + 3)
+    width, order = max(pages + [width]), r.permutation(sum(pages) + 3)
     table = np.full((len(P.lens), width), -1, dtype=np.int32)
     row = P.dc + 2 * P.dr
     codes = np.zeros((PAGE * len(order), row), dtype=np.uint8)
@@ -29,8 +29,8 @@ def stage(P, seed):
         j = np.arange(P.lens[b])
         slot = table[b, j // PAGE].astype(np.int64) * PAGE + j % PAGE
         codes[slot, : P.dc], scales[slot] = P.codes[b], P.scales[b]
-        rope = torch.from_numpy(P.rope[b]).to(BF).contiguous().view(torch.uint8).numpy()
-        codes[slot, P.dc:] = rope.reshape(len(j), 2 * P.dr)
+        if P.dr:
+            codes[slot, P.dc:] = torch.from_numpy(P.rope[b]).to(BF).contiguous().view(torch.uint8).numpy()
     dims = B.make_dims(num_heads=P.h, head_dim=P.dh, v_head_dim=P.dv, latent_dim=P.dc, rope_dim=P.dr, vocab_size=1,
                        page_size=PAGE, dtype=B.BF16)
     dev = lambda x: torch.from_numpy(x).to(BF).cuda()
@@ -46,8 +46,8 @@ def run(P, dims, args):
     return out
 
 
-def check(P, seed):
-    dims, args = stage(P, seed)
+def check(P, seed, width=0):
+    dims, args = stage(P, seed, width)
     first = run(P, dims, args)
     for _ in range(3):
         assert torch.equal(run(P, dims, args), first)
@@ -79,3 +79,14 @@ def test_blocks_of_16_rows(gpu, dc, peaks):
     shape, b, new = ROWS_16[dc]
     lens = [4096 - 37 * i % 200 for i in range(b)]
     check(Peaked(dc, *shape, [new] * b, lens, peaks, 4), dc)
+
+
+#                    h    d_h   d_v  d_c  d_r
+ODD = {"dv7": (16, 128, 7, 128, 64), "dv33": (5, 64, 33, 48, 24), "h700": (700, 16, 1, 64, 8), "dv130": (16, 64, 130, 320, 64),
+       "tall": (3, 1024, 1000, 512, 0), "h130": (130, 8, 12, 16, 0), "one": (1, 64, 64, 496, 8)}
+
+
+@pytest.mark.parametrize("width", [0, 1 << 14])  # (a table of 2^20 tokens: blocks of 128 where there are 48 rows a sequence)
+@pytest.mark.parametrize("shape", ODD)
+def test_odd_shapes(gpu, shape, width):
+    check(Peaked(70, *ODD[shape], [3, 60, 1, 17], [70, 333, 64, 17], "latent", 4), 70, width)
